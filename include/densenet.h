@@ -319,13 +319,97 @@ int densenet_maxpool(const void* d_in, int32_t n, int32_t H, int32_t W, int32_t 
  * (8 pairs written to hw[16]).  Returns DN_E_INVALID_ARG when the plane is too small for conv5. */
 int densenet_layer_sizes(int32_t H, int32_t W, int32_t* hw);
 
+/* A head learned on region descriptors: norm of their rows, softmax loss over a large vocabulary of classes or words, and
+ * the optimiser's step.  Rows of every operand are *_stride elements apart (>= C, elements next to each other); pointers
+ * need the alignment of one element only.  n may be 0.  Sums, row statistics, and states are held in 32 bits and results
+ * rounded once. */
+
+/* Storage of 8-bit outputs and states: e4m3 (OCP: 4 exponent and 3 mantissa bits, largest 448).  Only where an entry point
+ * says so. */
+#define DN_F8 ((dn_dtype)3)
+
+/* s = x + r;  y = s gamma / sqrt(mean(s^2) + eps), per row of C values (1 .. DN_MAX_NORM_C).
+ * d_x, d_res (NULL: s = x), d_sum (NULL: s is not stored): `dtype`.  d_gamma: fp32 [C], NULL: ones.  y is computed from the
+ * unrounded s.
+ * d_y: `y_dtype`, any of DN_F32, DN_F16, DN_BF16 whatever dtype is, or DN_F8: then y is stored as codes with a scale for
+ * every `block` values of a row (32, 64 or 128, the last block of a row cut short; 0: the whole row), so that
+ * y = code * scale: d_scale[n][ceil(C / block)], scale = max |y| / 448 over the block's values (a NaN is a NaN code and
+ * counts for no maximum; of a block below 1.4e-36 all codes are 0).  d_scale is NULL otherwise.
+ * The outputs may be the inputs' own memory (same type and stride). */
+#define DN_MAX_NORM_C 32768
+int densenet_rms_norm(const void* d_x, int64_t x_stride, const void* d_res, int64_t res_stride,
+                      const float* d_gamma, int64_t n, int32_t C, dn_dtype dtype, float eps, void* d_sum,
+                      int64_t sum_stride, void* d_y, int64_t y_stride, dn_dtype y_dtype, int32_t block,
+                      float* d_scale, void* stream);
+
+/* Gradient of densenet_rms_norm at s (d_sum, or d_x where there was no residual): with q = 1 / sqrt(mean(s^2) + eps) and
+ * a = dy gamma, dx = q (a - s q^2 mean(a s)) + dsum, the gradient of x and of r alike, and dgamma = sum over rows of
+ * dy s q.  d_dsum: gradient that reaches s past the norm (NULL: none).  d_dgamma: fp32 [C], NULL: not computed.  d_dy is of
+ * dy_dtype, d_sum, d_dsum and d_dx of dtype.  d_workspace: NULL for a size query into *bytes_needed. */
+int densenet_rms_norm_backward(const void* d_dy, int64_t dy_stride, dn_dtype dy_dtype, const void* d_sum,
+                               int64_t sum_stride, const void* d_dsum, int64_t dsum_stride,
+                               const float* d_gamma, int64_t n, int32_t C, dn_dtype dtype, float eps,
+                               void* d_dx, int64_t dx_stride, float* d_dgamma, void* d_workspace,
+                               size_t workspace_bytes, size_t* bytes_needed, void* stream);
+
+/* Softmax cross entropy of n rows h [n][C] over the products with w [V][C] (both `dtype`), the logits not kept:
+ * l_nv = h_n . w_v, lse_n = log sum_v exp l_nv, loss_n = lse_n - l_n,label.  d_label: int64 [n]; a row whose label lies
+ * outside [0, V) is masked: its loss and lse are 0, and nothing in its h reaches another row's results.
+ * d_loss, d_lse: fp32 [n].  d_workspace: NULL for a size query into *bytes_needed (which depends on the pointers' alignment
+ * and the strides: pass the same).  fp32 values are taken as three bf16 parts: they have to be finite, and below 2^-110
+ * they lose bits. */
+int densenet_softmax_loss(const void* d_h, int64_t h_stride, const void* d_w, int64_t w_stride,
+                          const int64_t* d_label, int64_t n, int32_t C, int32_t V, dn_dtype dtype,
+                          float* d_loss, float* d_lse, void* d_workspace, size_t workspace_bytes,
+                          size_t* bytes_needed, void* stream);
+
+/* Gradient of the loss: g_nv = dloss_n (exp(l_nv - lse_n) - [v = label_n]), dh = g w, dw = g^T h, from the forward pass's
+ * d_lse; the logits are computed again, a piece of the vocabulary at a time.  d_dloss: fp32 [n], or NULL for the mean over
+ * the unmasked rows (1 / their number each); `scale` multiplies it.  Masked rows: dh = 0, and their h does not reach dw.
+ * d_dh [n][C], d_dw [V][C]: `dtype`; dw is written, not added to.  g is rounded to `dtype` (16 bits: relative 2^-9 or 2^-12,
+ * of the order of the rounding of dh and dw) between the products. */
+int densenet_softmax_loss_backward(const void* d_h, int64_t h_stride, const void* d_w, int64_t w_stride,
+                                   const int64_t* d_label, const float* d_lse, const float* d_dloss,
+                                   float scale, int64_t n, int32_t C, int32_t V, dn_dtype dtype, void* d_dh,
+                                   int64_t dh_stride, void* d_dw, int64_t dw_stride, void* d_workspace,
+                                   size_t workspace_bytes, size_t* bytes_needed, void* stream);
+
+/* One AdamW step over `count` tensors (host table), in one launch per 72 of them, in place:
+ *   g' = g grad_scale;  m = b1 m + (1 - b1) g';  v = b2 v + (1 - b2) g'^2
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - b1^step)) / (sqrt(v / (1 - b2^step)) + eps)
+ * p, g: n values of p_dtype and g_dtype; copy (or NULL): the new p in copy_dtype (DN_F16 or DN_BF16).
+ * States: tensor i's start at value 256 * block of d_m and d_v and take ceil(n / 256) blocks of 256 values, what lies past
+ * n in the last one unused; ranges of different tensors must not meet.  n_blocks: blocks that d_m and d_v hold; both are
+ * aligned to 16 bytes.
+ * state_bits 32: fp32 m and v.  state_bits 8: DN_F8 codes of m and of sqrt(v), with a scale a block in d_m_scale and
+ * d_v_scale (fp32 [n_blocks]); value = code * scale, scale = the block's largest magnitude / 448.  A value between two codes
+ * takes the upper one with the chance of its place between them, by a hash of its place in the states and of `seed`
+ * (use another seed every step); a sqrt(v) above 0 is stored as at least the smallest code.  All zeros: a fresh state. */
+typedef struct {
+  void* p;
+  const void* g;
+  void* copy;
+  int64_t n;
+  int64_t block;
+} dn_adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay, grad_scale;
+  int64_t step; /* from 1 */
+  uint32_t seed;
+  int32_t state_bits;
+} dn_adamw_params;
+int densenet_adamw(const dn_adamw_tensor* tensors, int32_t count, dn_dtype p_dtype, dn_dtype g_dtype,
+                   dn_dtype copy_dtype, const dn_adamw_params* params, void* d_m, void* d_v,
+                   float* d_m_scale, float* d_v_scale, int64_t n_blocks, void* stream);
+
 /* Launch tracing.  While tracing is on, every kernel launch whose name matches `filter` (a
  * comma-separated list of names; NULL or "" = all) is bracketed by two hipEvents recorded on the
  * launch's own stream.  densenet_profile_stop() waits for the recorded events, writes per-name
  * totals (launches, summed elapsed ms) to out[max_entries] (*n_entries = number of names) and turns
  * tracing off.  Kernel names: build_planes, conv1..conv5, lrn_pool1, lrn_pool2, pool5, warp_regions,
  * region_windows, region_pool, pack_weights (a cross-image packed batch traces as build_planes,
- * region_windows, region_pool).  Events come from a pool owned by the library (no device memory). */
+ * region_windows, region_pool), rms_norm, rms_norm_backward, softmax_loss, softmax_loss_backward (all launches of a call
+ * as one) and adamw.  Events come from a pool owned by the library (no device memory). */
 typedef struct {
   char name[32];
   int32_t launches;

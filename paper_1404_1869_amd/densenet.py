@@ -20,18 +20,22 @@ LIB_PATH = os.path.join(_HERE, "libdensenet.so")
 DN_OK, DN_E_INVALID_ARG, DN_E_TOO_LARGE, DN_E_BUFFER_TOO_SMALL = 0, -1, -2, -3
 DN_E_UNSUPPORTED, DN_E_HIP, DN_E_INTERNAL = -4, -5, -6
 DN_F32, DN_F16, DN_BF16 = 0, 1, 2
+DN_F8 = 3   # e4m3: 8-bit outputs and optimiser states only
 DN_PAD_ZERO, DN_PAD_RAMP = 0, 1
 DN_MAX_SCALES, DN_MAX_PLANES_PER_IMAGE, DN_MAX_WARP_SIDE, DN_MAX_ASPECTS = 64, 64, 1024, 8
 DN_MAX_BATCH_ITEMS = 65536
 DN_STATIC_SCRATCH_BYTES = 64 << 20
+DN_MAX_NORM_C = 32768
+ADAMW_BLOCK = 256
 DTYPES = {"f32": DN_F32, "f16": DN_F16, "bf16": DN_BF16}
 
 EXPORTS = ("densenet_plan_pyramid", "densenet_build_pyramid", "densenet_pack_weights",
            "densenet_conv_features", "densenet_region_windows", "densenet_conv_layer",
            "densenet_lrn_pool", "densenet_maxpool", "densenet_layer_sizes", "densenet_warp_regions",
            "densenet_region_pool", "densenet_plan_batch", "densenet_build_batch",
-           "densenet_region_windows_batch", "densenet_build_pyramid_noalloc", "densenet_profile_start",
-           "densenet_profile_stop", "densenet_last_error")
+           "densenet_region_windows_batch", "densenet_build_pyramid_noalloc", "densenet_rms_norm",
+           "densenet_rms_norm_backward", "densenet_softmax_loss", "densenet_softmax_loss_backward",
+           "densenet_adamw", "densenet_profile_start", "densenet_profile_stop", "densenet_last_error")
 
 
 class dn_pyramid_params(ctypes.Structure):
@@ -61,6 +65,16 @@ class dn_net_params(ctypes.Structure):
 
 class dn_profile_entry(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 32), ("launches", ctypes.c_int32), ("total_ms", ctypes.c_double)]
+
+
+class dn_adamw_tensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("block", ctypes.c_int64)]
+
+
+class dn_adamw_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")] + \
+               [("step", ctypes.c_int64), ("seed", ctypes.c_uint32), ("state_bits", ctypes.c_int32)]
 
 
 class DenseNetError(RuntimeError):
@@ -105,6 +119,14 @@ def lib():
             "densenet_build_batch": [P, i32, i32, i32, pp, i32, pg, P, i32, P, sz, psz, P],
             "densenet_region_windows_batch": [P, pd, i32, i32, pg, P, i32, i32, i32, i32, P, P, i32, f32,
                                               i32, P, P, P, P],
+            "densenet_rms_norm": [P, i64, P, i64, P, i64, i32, i32, f32, P, i64, P, i64, i32, i32, P, P],
+            "densenet_rms_norm_backward": [P, i64, i32, P, i64, P, i64, P, i64, i32, i32, f32, P, i64, P, P,
+                                           sz, psz, P],
+            "densenet_softmax_loss": [P, i64, P, i64, P, i64, i32, i32, i32, P, P, P, sz, psz, P],
+            "densenet_softmax_loss_backward": [P, i64, P, i64, P, P, P, f32, i64, i32, i32, i32, P, i64, P,
+                                               i64, P, sz, psz, P],
+            "densenet_adamw": [ctypes.POINTER(dn_adamw_tensor), i32, i32, i32, i32,
+                               ctypes.POINTER(dn_adamw_params), P, P, P, P, i64, P],
             "densenet_profile_start": [ctypes.c_char_p],
             "densenet_profile_stop": [ctypes.POINTER(dn_profile_entry), i32, pi32],
         }
@@ -590,3 +612,250 @@ def convnet_featpyramid_batch(images, p: dn_pyramid_params, packed, dtype: int, 
     maps = cf.conv5_maps()
     feat = [maps[g.plane][g.r0:g.r1 + 1, g.c0:g.c1 + 1] for g in plan.geom]
     return Pyramid(feat, np.array([plan.geom[e].s for e in range(plan.E)]), plan, planes, cf, n_img)
+
+
+# ------------------------------------------------------------------------------------------------
+# A head learned on region descriptors: norm, softmax loss, AdamW
+# ------------------------------------------------------------------------------------------------
+_TYPES = None
+
+
+def _types():
+    """torch dtype -> dn_dtype, and back."""
+    global _TYPES
+    if _TYPES is None:
+        torch = _torch()
+        codes = {torch.float32: DN_F32, torch.float16: DN_F16, torch.bfloat16: DN_BF16,
+                 torch.float8_e4m3fn: DN_F8}
+        _TYPES = codes, {c: t for t, c in codes.items()}
+    return _TYPES
+
+
+def _bad(msg):
+    return DenseNetError(DN_E_INVALID_ARG, msg)
+
+
+def _code(t, what):
+    code = _types()[0].get(t.dtype, DN_F8)
+    if code == DN_F8:
+        raise DenseNetError(DN_E_UNSUPPORTED, f"{what}: fp32, fp16 or bf16 expected, not {t.dtype}")
+    return code
+
+
+def _rows(t, what, shape=None, dtype=None, device=None):
+    """Checks a matrix of rows (elements of a row next to each other, rows any distance apart); returns its
+    address and row stride."""
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+        raise _bad(f"{what}: a matrix{'' if shape is None else f' of {shape[0]} x {shape[1]}'} expected, not "
+                   f"{tuple(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise _bad(f"{what}: {dtype} expected, not {t.dtype}")
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise _bad(f"{what}: not on the operands' GPU")
+    row, col = t.stride()
+    if col != 1 and t.shape[1] > 1:
+        raise _bad(f"{what}: the elements of a row must be next to each other")
+    return t.data_ptr(), row if t.shape[0] > 1 else t.shape[1]
+
+
+def _vector(t, what, n, dtype, device):
+    if t is None:
+        return None
+    if tuple(t.shape) != (n,) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise _bad(f"{what}: {n} contiguous {dtype} values on the operands' GPU expected")
+    return t.data_ptr()
+
+
+def _on(device):
+    """The device's current stream; the device has to be the current one (the library launches there)."""
+    torch = _torch()
+    if device.index != torch.cuda.current_device():
+        raise _bad("the operands are not on the current GPU")
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def densenet_rms_norm(x, gamma=None, residual=None, eps=1e-6, out_dtype=None, block=0, out=None, sum_out=None,
+                      scale=None):
+    """Root-mean-square norm of the rows of s = x + residual.  x, residual: [n][C] (fp32, fp16 or bf16); gamma: fp32
+    [C].  out_dtype: DN_F32, DN_F16, DN_BF16 or DN_F8 (x's own by default); with DN_F8 a scale for every `block` values
+    of a row (0: the row).  Returns (y, s, scale): s is None without a residual or sum_out, scale without DN_F8."""
+    torch = _torch()
+    dt = _code(x, "x")
+    n, C = x.shape if x.dim() == 2 else (0, 0)
+    xp, xs = _rows(x, "x")
+    dev = x.device
+    ydt = dt if out_dtype is None else out_dtype
+    if ydt not in _types()[1]:
+        raise DenseNetError(DN_E_UNSUPPORTED, f"out_dtype {ydt}")
+    if block not in (0, 32, 64, 128) or (block and ydt != DN_F8):
+        raise DenseNetError(DN_E_UNSUPPORTED, "block: 0, or 32, 64 or 128 with DN_F8")
+    rp, rs = (None, 0) if residual is None else _rows(residual, "residual", (n, C), x.dtype, dev)
+    if residual is not None and sum_out is None:
+        sum_out = torch.empty((n, C), dtype=x.dtype, device=dev)
+    sp, ss = (None, 0) if sum_out is None else _rows(sum_out, "sum_out", (n, C), x.dtype, dev)
+    if out is None:
+        out = torch.empty((n, C), dtype=_types()[1][ydt], device=dev)
+    yp, ys = _rows(out, "out", (n, C), _types()[1][ydt], dev)
+    kp = None
+    if ydt == DN_F8:
+        blocks = -(-C // block) if block else 1
+        if scale is None:
+            scale = torch.empty((n, blocks), dtype=torch.float32, device=dev)
+        if tuple(scale.shape) != (n, blocks) or scale.dtype != torch.float32 or scale.device != dev or \
+                not scale.is_contiguous():
+            raise _bad(f"scale: contiguous fp32 [{n}][{blocks}] on the operands' GPU expected")
+        kp = scale.data_ptr()
+    elif scale is not None:
+        raise _bad("scale belongs to an 8-bit output")
+    check(lib().densenet_rms_norm(xp, xs, rp, rs, _vector(gamma, "gamma", C, torch.float32, dev), n, C, dt, eps, sp, ss,
+                                  yp, ys, ydt, block, kp, _on(dev)))
+    return out, sum_out, scale
+
+
+def densenet_rms_norm_backward(dy, s, gamma=None, dsum=None, eps=1e-6, dx=None, dgamma=None):
+    """Gradient of densenet_rms_norm at s (its second result, or x without a residual), from dy and from dsum, the
+    gradient that reaches s past the norm.  Returns (dx, dgamma); dx is the residual's gradient too."""
+    torch = _torch()
+    dt, ddt = _code(s, "s"), _code(dy, "dy")
+    sp, ss = _rows(s, "s")
+    n, C = s.shape
+    dev = s.device
+    dp, ds = _rows(dy, "dy", (n, C), None, dev)
+    ep, es = (None, 0) if dsum is None else _rows(dsum, "dsum", (n, C), s.dtype, dev)
+    if dx is None:
+        dx = torch.empty((n, C), dtype=s.dtype, device=dev)
+    xp, xs = _rows(dx, "dx", (n, C), s.dtype, dev)
+    if dgamma is None:
+        dgamma = torch.empty(C, dtype=torch.float32, device=dev)
+    gp = _vector(gamma, "gamma", C, torch.float32, dev)
+    op = _vector(dgamma, "dgamma", C, torch.float32, dev)
+    need = ctypes.c_size_t()
+    L, st = lib(), _on(dev)
+    args = (dp, ds, ddt, sp, ss, ep, es, gp, n, C, dt, eps, xp, xs, op)
+    check(L.densenet_rms_norm_backward(*args, None, 0, ctypes.byref(need), st))
+    ws = torch.empty(max(need.value, 1), dtype=torch.uint8, device=dev)
+    check(L.densenet_rms_norm_backward(*args, ws.data_ptr(), ws.numel(), ctypes.byref(need), st))
+    return dx, dgamma
+
+
+def _loss_operands(h, w, labels):
+    torch = _torch()
+    dt = _code(h, "h")
+    hp, hs = _rows(h, "h")
+    n, C = h.shape
+    dev = h.device
+    if w.dim() != 2:
+        raise _bad("w: a matrix expected")
+    V = w.shape[0]
+    wp, ws = _rows(w, "w", (V, C), h.dtype, dev)
+    return (hp, hs, wp, ws, _vector(labels, "labels", n, torch.int64, dev)), n, C, V, dt, dev
+
+
+def densenet_softmax_loss(h, w, labels, loss=None, lse=None):
+    """Softmax cross entropy of the rows of h [n][C] over the words of w [V][C].  labels: int64 [n]; outside [0, V) a row
+    is masked (loss 0).  Returns (loss [n], lse [n]) in fp32, not reduced."""
+    torch = _torch()
+    ops, n, C, V, dt, dev = _loss_operands(h, w, labels)
+    loss = torch.empty(n, dtype=torch.float32, device=dev) if loss is None else loss
+    lse = torch.empty(n, dtype=torch.float32, device=dev) if lse is None else lse
+    args = (*ops, n, C, V, dt, _vector(loss, "loss", n, torch.float32, dev), _vector(lse, "lse", n, torch.float32, dev))
+    need = ctypes.c_size_t()
+    L, st = lib(), _on(dev)
+    check(L.densenet_softmax_loss(*args, None, 0, ctypes.byref(need), st))
+    ws = torch.empty(max(need.value, 1), dtype=torch.uint8, device=dev)
+    check(L.densenet_softmax_loss(*args, ws.data_ptr(), ws.numel(), ctypes.byref(need), st))
+    return loss, lse
+
+
+def densenet_softmax_loss_backward(h, w, labels, lse, dloss=None, scale=1.0, dh=None, dw=None):
+    """Gradient of densenet_softmax_loss, from its lse: dloss, fp32 [n], or None for the mean over the unmasked rows,
+    times scale.  Returns (dh, dw) in h's type."""
+    torch = _torch()
+    ops, n, C, V, dt, dev = _loss_operands(h, w, labels)
+    dh = torch.empty((n, C), dtype=h.dtype, device=dev) if dh is None else dh
+    dw = torch.empty((V, C), dtype=h.dtype, device=dev) if dw is None else dw
+    args = (*ops, _vector(lse, "lse", n, torch.float32, dev), _vector(dloss, "dloss", n, torch.float32, dev), scale, n, C, V,
+            dt, *_rows(dh, "dh", (n, C), h.dtype, dev), *_rows(dw, "dw", (V, C), h.dtype, dev))
+    need = ctypes.c_size_t()
+    L, st = lib(), _on(dev)
+    check(L.densenet_softmax_loss_backward(*args, None, 0, ctypes.byref(need), st))
+    ws = torch.empty(max(need.value, 1), dtype=torch.uint8, device=dev)
+    check(L.densenet_softmax_loss_backward(*args, ws.data_ptr(), ws.numel(), ctypes.byref(need), st))
+    return dh, dw
+
+
+class AdamWPlan:
+    """Tensors that step together: parameters (one type, updated in place), their gradients' buffers (one type), 16-bit
+    copies of the parameters (optional; None entries allowed), and the optimiser's states.  state_bits: 32, or 8 (DN_F8
+    codes with a scale per 256 values); states are made as zeros, or given (m, v, and m_scale, v_scale in 8 bits): tensor
+    i's start at value ADAMW_BLOCK * blocks[i]."""
+
+    def __init__(self, params, grads, m=None, v=None, m_scale=None, v_scale=None, copies=None, state_bits=None):
+        torch = _torch()
+        self.params, self.grads = list(params), list(grads)
+        self.copies = list(copies) if copies is not None else [None] * len(self.params)
+        if not self.params or len(self.grads) != len(self.params) or len(self.copies) != len(self.params):
+            raise _bad("as many gradients (and copies) as parameters expected, one at least")
+        self.device = self.params[0].device
+        self.blocks, self.n_blocks = [], 0
+        for p in self.params:
+            self.blocks.append(self.n_blocks)
+            self.n_blocks += -(-p.numel() // ADAMW_BLOCK)
+        total = self.n_blocks * ADAMW_BLOCK
+        if state_bits is None:
+            state_bits = 8 if m is not None and m.dtype == torch.float8_e4m3fn else 32
+        if state_bits not in (8, 32):
+            raise DenseNetError(DN_E_UNSUPPORTED, "state_bits must be 8 or 32")
+        self.state_bits = state_bits
+        st = torch.float8_e4m3fn if state_bits == 8 else torch.float32
+
+        def state(t, what, n, dtype):
+            if t is None:
+                return torch.zeros(n * dtype.itemsize, dtype=torch.uint8, device=self.device).view(dtype)
+            _vector(t, what, n, dtype, self.device)
+            return t
+
+        self.m, self.v = state(m, "m", total, st), state(v, "v", total, st)
+        self.m_scale = self.v_scale = None
+        if state_bits == 8:
+            self.m_scale = state(m_scale, "m_scale", self.n_blocks, torch.float32)
+            self.v_scale = state(v_scale, "v_scale", self.n_blocks, torch.float32)
+        elif m_scale is not None or v_scale is not None:
+            raise _bad("scales belong to 8-bit states")
+        self.p_dtype = _code(self.params[0], "params")
+        given = [c for c in self.copies if c is not None]
+        self.copy_dtype = _code(given[0], "copies") if given else DN_BF16
+        self.table = (dn_adamw_tensor * len(self.params))()
+        for e, p, c, b in zip(self.table, self.params, self.copies, self.blocks):
+            self._fits(p, "params", p, self.params[0])
+            if c is not None:
+                self._fits(c, "copies", p, given[0])
+            e.p, e.copy, e.n, e.block = p.data_ptr(), None if c is None else c.data_ptr(), p.numel(), b
+        self.set_grads(self.grads)
+
+    def _fits(self, t, what, p, first):
+        if t.dtype != first.dtype or t.numel() != p.numel() or t.device != self.device or not t.is_cuda or \
+                not t.is_contiguous():
+            raise _bad(f"{what}: contiguous tensors of one type on one GPU, as large as their parameters, expected")
+
+    def set_grads(self, grads):
+        """Takes the gradients of the following steps from other tensors."""
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise _bad("as many gradients as parameters expected")
+        for g, p in zip(grads, self.params):
+            self._fits(g, "grads", p, grads[0])
+        self.grads, self.g_dtype = grads, _code(grads[0], "grads")
+        for e, g in zip(self.table, grads):
+            e.g = g.data_ptr()
+
+
+def densenet_adamw(plan: AdamWPlan, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grad_scale=1.0,
+                   seed=0):
+    """One AdamW step (the `step`-th, from 1) over a plan's tensors.  seed: of the 8-bit states' rounding, another one
+    every step."""
+    k = dn_adamw_params(lr, beta1, beta2, eps, weight_decay, grad_scale, step, seed & 0xFFFFFFFF, plan.state_bits)
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    check(lib().densenet_adamw(plan.table, len(plan.table), plan.p_dtype, plan.g_dtype, plan.copy_dtype, ctypes.byref(k),
+                               ptr(plan.m), ptr(plan.v), ptr(plan.m_scale), ptr(plan.v_scale), plan.n_blocks,
+                               _on(plan.device)))

@@ -1,0 +1,837 @@
+// Softmax cross entropy of rows h [n][C] over a large vocabulary w [V][C], and its gradient, without keeping the logits.
+//   l_nv = h_n . w_v;  lse_n = log sum_v exp l_nv;  loss_n = lse_n - l_n,label(n)
+//   g_nv = c_n (exp(l_nv - lse_n) - [v = label(n)]);  dh = g w;  dw = g^T h
+// The forward pass is one matrix product whose tiles end in a maximum and a sum of exponentials per row; a second launch
+// joins the tiles.  The gradient goes over the vocabulary in pieces: a piece's logits are computed again and leave as g in
+// 16 bits, and two more products take dh and dw from it: 6 n V C operations, the least without the logits.
+// 16-bit types: products on the matrix cores, 32-bit sums.  fp32: every operand (h, w, g) as three bf16 parts and six
+// products of parts, as the library's fp32 convolutions.
+// Rows whose label lies outside [0, V) are masked: loss and lse 0, g and dh 0, and what their h holds reaches nothing.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "head.h"
+
+namespace dn {
+namespace head {
+namespace {
+
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+constexpr uint32_t OOB = 0x80000000u;  // a buffer offset past every buffer: reads as 0
+constexpr int BK = 64;                 // k of one pipeline stage
+constexpr int64_t MAX_LD = 1 << 22;    // elements between rows: 256 rows stay within 32-bit byte offsets
+
+enum Epilogue { E_STATS, E_GRAD, E_SLAB, E_OUT };
+
+// D[m][n] = sum_k A(m, k) B(n, k).  An operand lies with k along its rows ([m][k], plain) or with k across them ([k][m],
+// turned); ld: elements from row to row.
+struct GemmArgs {
+  const void *a, *b;
+  int64_t lda, ldb, a_part, b_part;  // *_part: elements between the bf16 parts of fp32 operands
+  int32_t M, N, K;
+  int32_t a_rows, b_rows;  // rows of the operand that may be read (turned: columns, a multiple of 8)
+  int32_t tiles_m, tiles_n, products, splits;
+  // E_STATS, E_GRAD: M runs over the vocabulary from v0 on, N over rows
+  const int64_t* label;
+  int32_t v0, V;
+  float2* stats;  // [tiles_m][N]: maximum and sum of exponentials
+  float* at;      // [N]: the label's logit
+  const float *lse, *coef;
+  void* g;  // [N][ldg]
+  int64_t ldg, g_part;
+  // E_SLAB: sums of split s at slab + s slab_stride, [N][slab_ld]; accumulate: added to what is there
+  float* slab;
+  int64_t slab_ld, slab_stride;
+  int32_t accumulate;
+  // E_OUT: [N][ldo], times *unscale; rows with row_coef 0 are 0
+  void* out;
+  int64_t ldo;
+  const float *unscale, *row_coef;
+  int32_t out_vec;  // four values may be stored at once
+};
+
+__device__ inline void direct16(__amdgpu_buffer_rsrc_t rsrc, void* lds, uint32_t voff, uint32_t soff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds, 16, voff, soff, 0, 0);
+}
+// Wait until at most N (< 64) vector-memory accesses of this wave are outstanding, and all its LDS accesses are done.
+template <int N>
+__device__ inline void wait_loads() {
+  __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14));
+}
+__device__ inline void wave_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// One operand's tile of R rows x 64 k in LDS, loaded straight from memory in 16-byte slots (a wave instruction fills 1 KB).
+// Plain: rows of 8 slots, slot s of row r at place s ^ (r / 2) % 8, so that 16 consecutive rows' reads of one k meet 16
+// different 16-byte places modulo 256 bytes.  Turned: rows are k, R / 8 slots each, slot s of row k at place
+// s ^ 4 (k % 4): the transposing reads take 32 bytes from each of four k at a time.
+template <typename T, bool TR, int R, int NW>
+struct Operand {
+  static constexpr int BYTES = R * BK * 2, PIECES = BYTES / 1024, PER = PIECES / NW;
+  static constexpr int SLOTS = TR ? R / 8 : 8, LINES = 64 / SLOTS;  // slots of an LDS row, LDS rows of a piece
+  static_assert(PIECES % NW == 0 && (!TR || SLOTS >= 16), "whole pieces per wave");
+  uint32_t voff[PER];
+  const char* base;
+  int64_t ld;
+  int place;  // plain: first k of this lane's slot; turned: this lane's row within a piece
+
+  __device__ inline void init(const void* p, int64_t ld_, int row0, int rows, int wave, int lane) {
+    ld = ld_;
+    base = (const char*)p + (TR ? (int64_t)row0 : (int64_t)row0 * ld) * 2;
+    const int line = lane / SLOTS, slot = lane % SLOTS;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int row = (wave + i * NW) * LINES + line;
+      if constexpr (TR) {
+        const int s = slot ^ ((row & 3) << 2);
+        voff[i] = row0 + s * 8 < rows ? (uint32_t)(row * ld * 2 + s * 16) : OOB;
+      } else {
+        const int s = slot ^ ((row >> 1) & 7);
+        voff[i] = row0 + row < rows ? (uint32_t)(row * ld * 2 + s * 16) : OOB;
+        place = s * 8;  // the same for every i: NW is even, or there is one piece
+      }
+    }
+    if constexpr (TR) place = line;
+  }
+  __device__ inline void load(char* lds, int64_t part, int k0, int K, int wave) const {
+    const char* p = base + part * 2 + (TR ? (int64_t)k0 * ld * 2 : 0);
+    const __amdgpu_buffer_rsrc_t rsrc = uniform_rsrc(p, 0x7fffffffu);
+    const uint32_t soff = TR ? 0 : (uint32_t)k0 * 2;
+    if (k0 + BK <= K) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) direct16(rsrc, lds + (wave + i * NW) * 1024, voff[i], soff);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int k = k0 + (TR ? (wave + i * NW) * LINES + place : place);
+        direct16(rsrc, lds + (wave + i * NW) * 1024, k < K ? voff[i] : OOB, soff);
+      }
+    }
+  }
+};
+
+// Fragments of NT MFMA tiles (32 rows each) from row r0 of an operand's tile on: a lane's 8 k of row lane % 32.
+template <typename T, bool TR, int R, int NT>
+struct Fragments {
+  typedef typename Mfma<T>::frag frag;
+  uint32_t off[TR ? NT : 4];
+  __device__ inline void init(int r0, int lane) {
+    if constexpr (TR) {
+      const int q = (lane & 15) >> 2;  // k of the four that this lane's address is in
+      const int k = 8 * (lane >> 5) + q;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int slot = (r0 + t * 32) / 8 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+        off[t] = k * (R * 2) + (slot ^ (q << 2)) * 16 + (lane & 1) * 8;
+      }
+    } else {
+      const int row = r0 + (lane & 31);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) off[j] = row * 128 + (((2 * j + (lane >> 5)) ^ ((row >> 1) & 7)) * 16);
+    }
+  }
+  template <int J>
+  __device__ inline void read(const char* lds, frag (&f)[NT]) const {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      if constexpr (TR) {
+        typedef __attribute__((address_space(3))) i16x4* lds4;
+        const char* p = lds + off[t] + J * 16 * (R * 2);
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p);
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 4 * (R * 2)));
+        f[t] = __builtin_bit_cast(frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      } else {
+        f[t] = *(const frag*)(lds + off[J] + t * 32 * 128);
+      }
+    }
+  }
+};
+
+__device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896f); }
+
+// x as three bf16 parts, each the nearest of what the ones before leave.
+__device__ inline void split3(float x, __bf16 (&p)[3]) {
+  p[0] = (__bf16)x;
+  const float r = x - (float)p[0];
+  p[1] = (__bf16)r;
+  p[2] = (__bf16)(r - (float)p[1]);
+}
+
+// AT, BT: the operand is turned.  Waves: WM x WN, each (BM / WM) x (BN / WN).  NST: pipeline stages held in LDS.
+// G: parts that g is written in (E_GRAD).  O: type of E_OUT's results.
+template <typename T, bool AT, bool BT, int BM, int BN, int WM, int WN, int NST, Epilogue E, typename O>
+__global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
+  constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
+  using OA = Operand<T, AT, BM, NW>;
+  using OB = Operand<T, BT, BN, NW>;
+  constexpr int STAGE = OA::BYTES + OB::BYTES, PER = OA::PER + OB::PER;
+  constexpr int WROWS = BN / WN, WCOLS = BM / WM;
+  // E_GRAD: a wave's 32 rows x WCOLS values of g on their way out, rows 16 bytes apart in banks
+  constexpr int OUT_ROW = WCOLS * 2 + 16, OUT_BYTES = E == E_GRAD ? NW * 32 * OUT_ROW : E == E_STATS ? WM * BN * 8 : 0;
+  constexpr int LDS = NST * STAGE > OUT_BYTES ? NST * STAGE : OUT_BYTES;
+  __shared__ __align__(1024) char s_mem[LDS];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave % WM, wn = wave / WM, l32 = lane & 31, half = lane >> 5;
+  // Workgroups are dealt to the 8 XCDs in turn: each XCD takes a contiguous range of tiles, ordered as columns of 8 tiles
+  // along n, so that the tiles that run together share their operands in the XCD's L2.
+  const int nt = gridDim.x, xcd = blockIdx.x % 8, per = nt / 8, rem = nt % 8;
+  const int id = xcd * per + min(xcd, rem) + blockIdx.x / 8;
+  const int col = id / (8 * g.tiles_m), width = min(8, g.tiles_n - col * 8), in = id - col * 8 * g.tiles_m;
+  const int tile_m = in / width, tile_n = col * 8 + in % width;
+  const int m0 = tile_m * BM, n0 = tile_n * BN;
+
+  OA oa;
+  OB ob;
+  oa.init(g.a, g.lda, m0, g.a_rows, wave, lane);
+  ob.init(g.b, g.ldb, n0, g.b_rows, wave, lane);
+  Fragments<T, AT, BM, TM> fa;
+  Fragments<T, BT, BN, TN> fb;
+  fa.init(wm * WCOLS, lane);
+  fb.init(wn * WROWS, lane);
+
+  const int kt = (g.K + BK - 1) / BK, total = kt * g.products;
+  const int s0 = (int)((int64_t)total * blockIdx.y / g.splits), s1 = (int)((int64_t)total * (blockIdx.y + 1) / g.splits);
+  auto load = [&](int s, int buf) {
+    // products of parts from the smallest to the largest: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
+    const int pr = g.products == 1 ? 5 : s / kt, k0 = (g.products == 1 ? s : s - pr * kt) * BK;
+    const int pa = pr == 0 ? 2 : pr == 1 || pr == 3 ? 1 : 0, pb = pr == 2 ? 2 : pr == 1 || pr == 4 ? 1 : 0;
+    char* at = s_mem + buf * STAGE;
+    oa.load(at, pa * g.a_part, k0, g.K, wave);
+    ob.load(at + OA::BYTES, pb * g.b_part, k0, g.K, wave);
+  };
+
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int a = 0; a < TM; ++a)
+#pragma unroll
+    for (int t = 0; t < TN; ++t) acc[a][t] = f32x16{};
+
+  // Stage s computes from buffer (s - s0) % NST while the next NST - 1 stages' loads are on their way.  A wave reads the
+  // fragments of k-step j + 1 while the MFMAs of k-step j run; before the last k-step's MFMAs it waits for the next
+  // stage's loads, meets the others, and goes on to the next stage's first fragments, so that the wait and the reads lie
+  // behind MFMAs.  At that point every wave holds all of the stage in registers, so its buffer takes the loads of stage
+  // s + NST.
+  if (s1 > s0) {
+    typename Mfma<T>::frag a[2][TM], b[2][TN];
+#pragma unroll
+    for (int i = 0; i < NST; ++i)
+      if (s0 + i < s1) load(s0 + i, i);
+    if (s1 - s0 >= NST) wait_loads<PER * (NST - 1)>();
+    else wait_loads<0>();
+    wave_barrier();
+    fa.template read<0>(s_mem, a[0]);
+    fb.template read<0>(s_mem + OA::BYTES, b[0]);
+    int buf = 0;
+    for (int s = s0; s < s1; ++s) {
+      const char* at = s_mem + buf * STAGE;
+      const int next = buf + 1 == NST ? 0 : buf + 1;
+      auto mma = [&](int h) {
+#pragma unroll
+        for (int t = 0; t < TN; ++t)
+#pragma unroll
+          for (int i = 0; i < TM; ++i) acc[i][t] = Mfma<T>::mma(a[h][i], b[h][t], acc[i][t]);
+      };
+      fa.template read<1>(at, a[1]);
+      fb.template read<1>(at + OA::BYTES, b[1]);
+      mma(0);
+      fa.template read<2>(at, a[0]);
+      fb.template read<2>(at + OA::BYTES, b[0]);
+      mma(1);
+      fa.template read<3>(at, a[1]);
+      fb.template read<3>(at + OA::BYTES, b[1]);
+      mma(0);
+      if (s + 1 < s1) {
+        if (NST > 2 && s + NST <= s1) wait_loads<PER * (NST > 2 ? NST - 2 : 0)>();
+        else wait_loads<0>();
+        wave_barrier();
+        if (s + NST < s1) load(s + NST, buf);
+        const char* nx = s_mem + next * STAGE;
+        fa.template read<0>(nx, a[0]);
+        fb.template read<0>(nx + OA::BYTES, b[0]);
+      }
+      mma(1);
+      buf = next;
+    }
+  }
+
+  // Element r of acc[i][t]: m = m0 + wm WCOLS + 32 i + 8 (r / 4) + 4 half + r % 4, n = n0 + wn WROWS + 32 t + l32.
+  const int mw = m0 + wm * WCOLS + 4 * half, nw = n0 + wn * WROWS + l32;
+  if constexpr (E == E_STATS) {
+    float2* red = (float2*)s_mem;
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < TN; ++t) {
+      const int n = nw + 32 * t;
+      const int lab = n < g.N ? (int)std::min<int64_t>(std::max<int64_t>(g.label[n], -1), g.V) - g.v0 : -1;
+      float top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int m = mw + 32 * i + 8 * (r / 4) + r % 4;
+          if (m >= g.M) acc[i][t][r] = -INFINITY;
+          if (m == lab && m < g.M) g.at[n] = acc[i][t][r];
+          top = fmaxf(top, acc[i][t][r]);
+        }
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += exp_of(acc[i][t][r] - ref);
+      sum += __shfl_xor(sum, 32);
+      if (half == 0) red[wm * BN + wn * WROWS + 32 * t + l32] = float2{top, sum};
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < BN; c += 64 * NW)
+      if (n0 + c < g.N) {
+        float top = red[c].x, sum = 0.f;
+#pragma unroll
+        for (int w = 1; w < WM; ++w) top = fmaxf(top, red[w * BN + c].x);
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int w = 0; w < WM; ++w) {
+          const float2 o = red[w * BN + c];
+          sum += o.x == -INFINITY ? o.y : o.y * exp_of(o.x - ref);
+        }
+        g.stats[(int64_t)tile_m * g.N + n0 + c] = float2{top, sum};
+      }
+  } else if constexpr (E == E_GRAD) {
+    constexpr int PARTS = std::is_same<O, float>::value ? 3 : 1;
+    __syncthreads();
+    char* stg = s_mem + wave * 32 * OUT_ROW;
+    typedef T v4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int t = 0; t < TN; ++t) {
+      const int n = nw + 32 * t;
+      const bool row = n < g.N;
+      const int lab = row ? (int)std::min<int64_t>(std::max<int64_t>(g.label[n], -1), g.V) - g.v0 : -1;
+      const float c = row ? g.coef[n] : 0.f, lse = row ? g.lse[n] : 0.f;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int m = mw + 32 * i + 8 * (r / 4) + r % 4;
+          const float p = exp_of(acc[i][t][r] - lse) - (m == lab ? 1.f : 0.f);
+          acc[i][t][r] = c == 0.f || m >= g.M ? 0.f : c * p;
+        }
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            v4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              o[e] = (T)acc[i][t][4 * q + e];
+              if (PARTS > 1) acc[i][t][4 * q + e] -= (float)o[e];
+            }
+            *(v4*)(stg + l32 * OUT_ROW + (32 * i + 8 * q + 4 * half) * 2) = o;
+          }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        constexpr int LANES = WCOLS / 8, LINES = 64 / LANES;  // lanes of a row, rows of an instruction
+        typedef T v8 __attribute__((ext_vector_type(8)));
+        T* dst = (T*)g.g + part * g.g_part + m0 + wm * WCOLS + (lane % LANES) * 8;
+#pragma unroll
+        for (int k = 0; k < 32 / LINES; ++k) {
+          const int rr = k * LINES + lane / LANES, nn = n0 + wn * WROWS + 32 * t + rr;
+          const v8 o = *(const v8*)(stg + rr * OUT_ROW + (lane % LANES) * 16);
+          if (nn < g.N) *(v8*)(dst + nn * g.ldg) = o;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
+    }
+  } else {
+    const float u = E == E_OUT ? *g.unscale : 1.f;
+#pragma unroll
+    for (int t = 0; t < TN; ++t) {
+      const int n = nw + 32 * t;
+      if (n >= g.N) continue;
+      const bool zero = E == E_OUT && g.row_coef && g.row_coef[n] == 0.f;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int m = mw + 32 * i + 8 * q;
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = zero ? 0.f : acc[i][t][4 * q + e] * u;
+          if constexpr (E == E_SLAB) {  // rows are padded to whole tiles
+            f32x4* dst = (f32x4*)(g.slab + blockIdx.y * g.slab_stride + n * g.slab_ld + m);
+            *dst = g.accumulate ? *dst + v : v;
+          } else {
+            typedef O v4 __attribute__((ext_vector_type(4)));
+            O* dst = (O*)g.out + n * g.ldo + m;
+            if (g.out_vec && m + 4 <= g.M) {
+              *(v4*)dst = v4{(O)v[0], (O)v[1], (O)v[2], (O)v[3]};
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (m + e < g.M) dst[e] = (O)v[e];
+            }
+          }
+        }
+    }
+  }
+}
+
+// Joins the tiles of a row: 16 rows per workgroup, 16 tiles at a time.
+__global__ __launch_bounds__(256) void join_stats_kernel(const float2* __restrict__ stats, const float* __restrict__ at,
+                                                         const int64_t* __restrict__ label, int tiles, int n, int V,
+                                                         float* __restrict__ loss, float* __restrict__ lse) {
+  __shared__ float2 s_red[4][16];
+  const int row = blockIdx.x * 16 + (threadIdx.x & 15), t0 = threadIdx.x >> 4;
+  float top = -INFINITY, sum = 0.f;
+  auto add = [&](float2 o) {  // (0, -inf) adds nothing; a NaN sum stays
+    const float m = fmaxf(top, o.x), ref = m == -INFINITY ? 0.f : m;
+    sum = (top == -INFINITY ? sum : sum * exp_of(top - ref)) + (o.x == -INFINITY ? o.y : o.y * exp_of(o.x - ref));
+    top = m;
+  };
+  if (row < n)
+    for (int t = t0; t < tiles; t += 16) add(stats[(int64_t)t * n + row]);
+  add(float2{__shfl_xor(top, 16), __shfl_xor(sum, 16)});
+  add(float2{__shfl_xor(top, 32), __shfl_xor(sum, 32)});
+  if ((threadIdx.x & 63) < 16) s_red[threadIdx.x >> 6][threadIdx.x & 15] = float2{top, sum};
+  __syncthreads();
+  if (threadIdx.x < 16 && row < n) {
+    for (int w = 1; w < 4; ++w) add(s_red[w][threadIdx.x]);
+    const int64_t l = label[row];
+    const bool has = l >= 0 && l < V;
+    const float z = logf(sum) + top;
+    lse[row] = has ? z : 0.f;
+    loss[row] = has ? z - at[row] : 0.f;
+  }
+}
+
+// The few-tiles forward pass: logits of a row as `splits` partial sums, one workgroup per row.
+__global__ __launch_bounds__(1024) void join_logits_kernel(const float* __restrict__ slab, int64_t ld, int64_t stride,
+                                                           int splits, const int64_t* __restrict__ label, int V,
+                                                           float* __restrict__ loss, float* __restrict__ lse) {
+  __shared__ float s_top[16], s_sum[16];
+  __shared__ float s_at;
+  const int64_t row = blockIdx.x, l = label[row];
+  float top = -INFINITY, sum = 0.f;
+  for (int v = threadIdx.x; v < V; v += 1024) {
+    float x = 0.f;
+    for (int s = 0; s < splits; ++s) x += slab[s * stride + row * ld + v];
+    if (v == l) s_at = x;
+    const float m = fmaxf(top, x), ref = m == -INFINITY ? 0.f : m;
+    sum = (top == -INFINITY ? sum : sum * exp_of(top - ref)) + exp_of(x - ref);
+    top = m;
+  }
+  const float all = lanes_max<64>(top), ref = all == -INFINITY ? 0.f : all;
+  sum = lanes_sum<64>(top == -INFINITY ? sum : sum * exp_of(top - ref));
+  if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = all, s_sum[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float m = s_top[0], z = 0.f;
+    for (int w = 1; w < 16; ++w) m = fmaxf(m, s_top[w]);
+    const float mr = m == -INFINITY ? 0.f : m;
+    for (int w = 0; w < 16; ++w) z += s_top[w] == -INFINITY ? s_sum[w] : s_sum[w] * exp_of(s_top[w] - mr);
+    const bool has = l >= 0 && l < V;
+    z = logf(z) + m;
+    lse[row] = has ? z : 0.f;
+    loss[row] = has ? z - s_at : 0.f;
+  }
+}
+
+// A row's part in the gradient, coef[n], and the factor that is left for the end, *unscale.  Without dloss every unmasked
+// row counts 1 and unscale is scale / (their number).  With it the rows keep dloss / 2^e in (-2, 2) for the largest
+// finite |dloss| in [2^e, 2^(e + 1)).  boost: a power of two that moves fp16's g away from its smallest values.
+__global__ __launch_bounds__(1024) void coef_kernel(const int64_t* __restrict__ label, const float* __restrict__ dloss, int64_t n,
+                                                    int V, float scale, float boost, float* __restrict__ coef,
+                                                    float* __restrict__ unscale) {
+  __shared__ float s_red[16];
+  __shared__ float s_mul;
+  float v = 0.f;
+  for (int64_t i = threadIdx.x; i < n; i += 1024) {
+    const bool has = label[i] >= 0 && label[i] < V;
+    const float d = has ? (dloss ? fabsf(dloss[i]) : 1.f) : 0.f;
+    v = dloss ? (d < INFINITY ? fmaxf(v, d) : v) : v + d;
+  }
+  v = dloss ? lanes_max<64>(v) : lanes_sum<64>(v);
+  if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    v = s_red[0];
+    for (int w = 1; w < 16; ++w) v = dloss ? fmaxf(v, s_red[w]) : v + s_red[w];
+    if (dloss) {
+      int e = v > 0.f ? ilogbf(v) : 0;
+      e = e < -100 ? -100 : e > 100 ? 100 : e;
+      s_mul = ldexpf(boost, -e);
+      *unscale = scale * ldexpf(1.f / boost, e);
+    } else {
+      s_mul = boost;
+      *unscale = v > 0.f ? scale / (v * boost) : 0.f;
+    }
+  }
+  __syncthreads();
+  for (int64_t i = threadIdx.x; i < n; i += 1024) {
+    const bool has = label[i] >= 0 && label[i] < V;
+    coef[i] = has ? (dloss ? dloss[i] : 1.f) * s_mul : 0.f;
+  }
+}
+
+// Copies an operand into aligned rows of ldo elements (a multiple of 8), zeros past column C, as one 16-bit part or fp32's
+// three; rows whose label is outside [0, V) become 0 (label may be null).
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(const T* __restrict__ in, int64_t ld, int64_t rows, int C, void* __restrict__ out,
+                                                   int64_t ldo, int64_t part, const int64_t* __restrict__ label, int V) {
+  const int64_t per = ldo / 8, total = rows * per;
+  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
+    const int64_t row = u / per;
+    const int c = (int)(u - row * per) * 8;
+    float v[8];
+    load8(in + row * ld, c, C, v);
+    if (label && !(label[row] >= 0 && label[row] < V))
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    if constexpr (std::is_same<T, float>::value) {
+      float p[3][8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        __bf16 s[3];
+        split3(v[j], s);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) p[k][j] = (float)s[k];
+      }
+#pragma unroll
+      for (int k = 0; k < 3; ++k) store8((__bf16*)out + k * part + row * ldo + c, p[k]);
+    } else {
+      store8((T*)out + row * ldo + c, v);
+    }
+  }
+}
+
+// out = unscale (sum of the slabs), rounded; rows with row_coef 0 are 0.
+template <typename O>
+__global__ __launch_bounds__(256) void join_slabs_kernel(const float* __restrict__ slab, int64_t ld, int64_t stride, int splits,
+                                                         int64_t rows, int C, const float* __restrict__ unscale,
+                                                         const float* __restrict__ row_coef, O* __restrict__ out, int64_t ldo) {
+  const int per = (C + 7) / 8;
+  const int64_t total = rows * per;
+  const float u = *unscale;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per;
+    const int c = (int)(i - row * per) * 8;
+    float v[8] = {};
+    for (int s = 0; s < splits; ++s) {
+      float w[8];
+      load8(slab + s * stride + row * ld + c, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += w[j];
+    }
+    const bool zero = row_coef && row_coef[row] == 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = zero ? 0.f : v[j] * u;
+    store8(out + row * ldo, c, C, v);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void zero_rows_kernel(T* __restrict__ out, int64_t ld, int64_t rows, int C) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * C; i += (int64_t)gridDim.x * 256)
+    out[i / C * ld + i % C] = T{};
+}
+
+// -----------------------------------------------------------------------------------------------------------------
+// Host side: which tiles, how many splits and pieces, and where things lie in the workspace.
+// -----------------------------------------------------------------------------------------------------------------
+int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+struct Work {  // offsets in the workspace, 256-byte aligned
+  size_t total = 0;
+  size_t take(size_t bytes) {
+    const size_t at = total;
+    total += up((int64_t)bytes, 256);
+    return at;
+  }
+};
+
+// Whether the loads can take an operand as it lies: rows that start on 16 bytes and hold whole 16-byte slots.
+bool lies_well(const void* p, int64_t ld, int32_t C, dn_dtype dt) {
+  return dt != DN_F32 && (uintptr_t)p % 16 == 0 && ld % 8 == 0 && C % 8 == 0 && ld <= MAX_LD;
+}
+
+// Splits of a launch's k over workgroups: the fewest that minimise the rounds of workgroups per split, at `slots`
+// workgroups a round, each split at least `least` stages long.
+int splits_for(int64_t tiles, int64_t stages, int slots, int least) {
+  int best = 1;
+  double cost = 1e30;
+  for (int s = 1; s <= 64 && (s == 1 || stages / s >= least); ++s) {
+    const double c = (double)((tiles * s + slots - 1) / slots) / s * (1 + 0.02 * (s - 1)) + (s > 1 ? 0.05 : 0);
+    if (c < cost - 1e-9) cost = c, best = s;
+  }
+  return best;
+}
+
+struct Plan {
+  bool pack_h, pack_w;
+  int parts;
+  int64_t ldp;  // row length of packed operands
+  size_t h_at, w_at;
+};
+Plan plan_operands(const LossArgs& a, dn_dtype dt, bool backward, Work& w) {
+  Plan p{};
+  p.parts = dt == DN_F32 ? 3 : 1;
+  p.ldp = up(a.C, 8);
+  p.pack_h = backward || !lies_well(a.h, a.h_stride, a.C, dt);
+  p.pack_w = !lies_well(a.w, a.w_stride, a.C, dt);
+  if (p.pack_h) p.h_at = w.take((size_t)p.parts * a.n * p.ldp * 2);
+  if (p.pack_w) p.w_at = w.take((size_t)p.parts * a.V * p.ldp * 2);
+  return p;
+}
+
+template <typename T>
+int pack(const T* in, int64_t ld, int64_t rows, int C, void* out, int64_t ldo, const int64_t* label, int V, hipStream_t st) {
+  const int64_t total = rows * (ldo / 8);
+  const unsigned grid = (unsigned)std::min<int64_t>((total + 255) / 256, 8192);
+  pack_kernel<T><<<grid, 256, 0, st>>>(in, ld, rows, C, out, ldo, rows * ldo, label, V);
+  return (int)hipGetLastError();
+}
+int pack_any(dn_dtype dt, const void* in, int64_t ld, int64_t rows, int C, void* out, int64_t ldo, const int64_t* label, int V,
+             hipStream_t st) {
+  if (dt == DN_F32) return pack((const float*)in, ld, rows, C, out, ldo, label, V, st);
+  if (dt == DN_F16) return pack((const _Float16*)in, ld, rows, C, out, ldo, label, V, st);
+  return pack((const __bf16*)in, ld, rows, C, out, ldo, label, V, st);
+}
+
+// Tile shapes.
+enum Tile { T256, T128, T64, T32 };
+int tile_m(Tile t) { return t == T256 ? 256 : 128; }
+int tile_n(Tile t) { return t == T256 ? 256 : t == T128 ? 128 : t == T64 ? 64 : 32; }
+
+template <typename T, bool AT, bool BT, Epilogue E, typename O, int BM, int BN, int WM, int WN, int NST>
+int run_gemm(GemmArgs& g, hipStream_t st) {
+  g.tiles_m = (g.M + BM - 1) / BM, g.tiles_n = (g.N + BN - 1) / BN;
+  const dim3 grid((unsigned)(g.tiles_m * g.tiles_n), (unsigned)g.splits);
+  gemm_kernel<T, AT, BT, BM, BN, WM, WN, NST, E, O><<<grid, 64 * WM * WN, 0, st>>>(g);
+  return (int)hipGetLastError();
+}
+template <typename T, bool AT, bool BT, Epilogue E, typename O>
+int run_tile(Tile t, GemmArgs& g, hipStream_t st) {
+  if (t == T256) return run_gemm<T, AT, BT, E, O, 256, 256, 2, 4, 2>(g, st);
+  if constexpr (!AT && !BT && (E == E_STATS || E == E_SLAB)) {
+    if (t == T64) return run_gemm<T, AT, BT, E, O, 128, 64, 2, 2, 3>(g, st);
+    if (t == T32) return run_gemm<T, AT, BT, E, O, 128, 32, 4, 1, 4>(g, st);
+  }
+  return run_gemm<T, AT, BT, E, O, 128, 128, 2, 2, 2>(g, st);
+}
+
+struct FwdPlan {
+  Plan op;
+  Tile tile;
+  int splits;
+  bool logits;  // partial logits in memory (few tiles) instead of tile statistics
+  int64_t tiles_m, ld;
+  size_t stats_at, at_at, slab_at, total;
+};
+FwdPlan plan_forward(const LossArgs& a, dn_dtype dt) {
+  FwdPlan f{};
+  Work w;
+  f.op = plan_operands(a, dt, false, w);
+  const int64_t t256 = ((a.V + 255) / 256) * ((a.n + 255) / 256);
+  f.tile = a.n <= 32 ? T32 : a.n <= 64 ? T64 : t256 >= 200 ? T256 : T128;
+  f.tiles_m = (a.V + tile_m(f.tile) - 1) / tile_m(f.tile);
+  const int64_t tiles = f.tiles_m * ((a.n + tile_n(f.tile) - 1) / tile_n(f.tile));
+  const int64_t stages = (f.op.ldp + BK - 1) / BK * (f.op.parts == 3 ? 6 : 1);
+  f.splits = f.tile == T256 || tiles >= 192 ? 1 : splits_for(tiles, stages, 256, 4);
+  f.logits = f.splits > 1;
+  f.at_at = w.take((size_t)a.n * 4);
+  if (f.logits) {
+    f.ld = f.tiles_m * tile_m(f.tile);
+    f.slab_at = w.take((size_t)f.splits * a.n * f.ld * 4);
+  } else {
+    f.stats_at = w.take((size_t)f.tiles_m * a.n * 8);
+  }
+  f.total = w.total;
+  return f;
+}
+
+struct BackPlan {
+  Plan op;
+  int64_t vc, ldg;  // words of a piece (a multiple of 256)
+  Tile grad, dh, dw;
+  int dh_splits, dw_splits;
+  bool dh_slab, dw_slab;
+  int64_t slab_ld;
+  size_t coef_at, unscale_at, g_at, dh_at, dw_at, total;
+};
+constexpr int64_t PIECE_BYTES = 1LL << 29;  // of one part of g
+BackPlan plan_backward(const LossArgs& a, dn_dtype dt) {
+  BackPlan b{};
+  Work w;
+  b.op = plan_operands(a, dt, true, w);
+  const int pr = b.op.parts == 3 ? 6 : 1;
+  const int64_t v256 = up(a.V, 256);
+  b.vc = std::min(v256, std::max<int64_t>(256, PIECE_BYTES / (2 * a.n) / 256 * 256));
+  const int64_t pieces = (v256 + b.vc - 1) / b.vc;
+  b.vc = up((v256 + pieces - 1) / pieces, 256);
+  b.ldg = b.vc;
+  const auto tiles = [](int64_t m, int64_t n, int t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
+  const auto pick = [&](int64_t m, int64_t n, int64_t k, Tile& t, int& s) {
+    const int64_t stages = (k + BK - 1) / BK * pr;
+    const int64_t t256 = tiles(m, n, 256);
+    const int s256 = splits_for(t256, stages, 256, 16);
+    t = t256 * s256 >= 200 ? T256 : T128;
+    s = t == T256 ? s256 : splits_for(tiles(m, n, 128), stages, 512, 8);
+  };
+  b.grad = tiles(b.vc, a.n, 256) >= 200 ? T256 : T128;
+  pick(a.C, a.n, b.vc, b.dh, b.dh_splits);
+  pick(a.C, std::min<int64_t>(b.vc, a.V), a.n, b.dw, b.dw_splits);
+  b.dh_slab = pieces > 1 || b.dh_splits > 1;
+  b.dw_slab = b.dw_splits > 1;
+  b.slab_ld = up(a.C, 256);
+  b.coef_at = w.take((size_t)a.n * 4);
+  b.unscale_at = w.take(4);
+  b.g_at = w.take((size_t)b.op.parts * a.n * b.ldg * 2);
+  if (b.dh_slab) b.dh_at = w.take((size_t)b.dh_splits * a.n * b.slab_ld * 4);
+  if (b.dw_slab) b.dw_at = w.take((size_t)b.dw_splits * std::min<int64_t>(b.vc, a.V) * b.slab_ld * 4);
+  b.total = w.total;
+  return b;
+}
+
+struct Operands {
+  const void *h, *w;
+  int64_t ldh, ldw, h_part, w_part;
+};
+int lay_out(const LossArgs& a, dn_dtype dt, const Plan& p, char* work, bool mask, Operands& o, hipStream_t st) {
+  o = Operands{a.h, a.w, a.h_stride, a.w_stride, 0, 0};
+  int err = 0;
+  if (p.pack_h) {
+    o.h = work + p.h_at, o.ldh = p.ldp, o.h_part = a.n * p.ldp;
+    err = pack_any(dt, a.h, a.h_stride, a.n, a.C, work + p.h_at, p.ldp, mask ? a.label : nullptr, a.V, st);
+  }
+  if (p.pack_w && !err) {
+    o.w = work + p.w_at, o.ldw = p.ldp, o.w_part = (int64_t)a.V * p.ldp;
+    err = pack_any(dt, a.w, a.w_stride, a.V, a.C, work + p.w_at, p.ldp, nullptr, 0, st);
+  }
+  return err;
+}
+
+template <typename T>
+int forward(const LossArgs& a, const FwdPlan& f, const Operands& o, char* work, hipStream_t st) {
+  GemmArgs g{};
+  g.a = o.w, g.lda = o.ldw, g.a_part = o.w_part, g.a_rows = a.V;
+  g.b = o.h, g.ldb = o.ldh, g.b_part = o.h_part, g.b_rows = (int)a.n;
+  g.M = a.V, g.N = (int)a.n, g.K = (int)f.op.ldp, g.products = f.op.parts == 3 ? 6 : 1, g.splits = f.splits;
+  g.label = a.label, g.V = a.V;
+  g.at = (float*)(work + f.at_at);
+  int err;
+  if (f.logits) {
+    g.slab = (float*)(work + f.slab_at), g.slab_ld = f.ld, g.slab_stride = a.n * f.ld;
+    if ((err = run_tile<T, false, false, E_SLAB, T>(f.tile, g, st))) return err;
+    join_logits_kernel<<<dim3((unsigned)a.n), 1024, 0, st>>>(g.slab, f.ld, g.slab_stride, f.splits, a.label, a.V, a.loss, a.lse);
+  } else {
+    g.stats = (float2*)(work + f.stats_at);
+    if ((err = run_tile<T, false, false, E_STATS, T>(f.tile, g, st))) return err;
+    join_stats_kernel<<<dim3((unsigned)((a.n + 15) / 16)), 256, 0, st>>>(g.stats, g.at, a.label, g.tiles_m, (int)a.n, a.V, a.loss,
+                                                                        a.lse);
+  }
+  return (int)hipGetLastError();
+}
+
+// T: type of the products' operands; O: of the results (float where T holds fp32's parts).
+template <typename T, typename O>
+int backward(const LossArgs& a, const BackPlan& b, const Operands& o, char* work, float boost, hipStream_t st) {
+  float* coef = (float*)(work + b.coef_at);
+  float* unscale = (float*)(work + b.unscale_at);
+  coef_kernel<<<1, 1024, 0, st>>>(a.label, a.dloss, a.n, a.V, a.scale, boost, coef, unscale);
+  int err = (int)hipGetLastError();
+  if (err) return err;
+  const int products = b.op.parts == 3 ? 6 : 1;
+  const int64_t g_part = a.n * b.ldg;
+  for (int64_t v0 = 0; v0 < a.V; v0 += b.vc) {
+    const int vc = (int)std::min<int64_t>(b.vc, a.V - v0);
+    const char* w = (const char*)o.w + v0 * o.ldw * 2;
+    GemmArgs g{};  // the piece's logits, leaving as g
+    g.a = w, g.lda = o.ldw, g.a_part = o.w_part, g.a_rows = vc;
+    g.b = o.h, g.ldb = o.ldh, g.b_part = o.h_part, g.b_rows = (int)a.n;
+    g.M = vc, g.N = (int)a.n, g.K = (int)b.op.ldp, g.products = products, g.splits = 1;
+    g.label = a.label, g.v0 = (int)v0, g.V = a.V, g.lse = a.lse_in, g.coef = coef;
+    g.g = work + b.g_at, g.ldg = b.ldg, g.g_part = g_part;
+    if ((err = run_tile<T, false, false, E_GRAD, O>(b.grad, g, st))) return err;
+
+    GemmArgs d{};  // dh += g w
+    d.a = w, d.lda = o.ldw, d.a_part = o.w_part, d.a_rows = (int)b.op.ldp;
+    d.b = g.g, d.ldb = b.ldg, d.b_part = g_part, d.b_rows = (int)a.n;
+    d.M = a.C, d.N = (int)a.n, d.K = vc, d.products = products, d.splits = b.dh_splits;
+    d.unscale = unscale;
+    if (b.dh_slab) {
+      d.slab = (float*)(work + b.dh_at), d.slab_ld = b.slab_ld, d.slab_stride = a.n * b.slab_ld, d.accumulate = v0 > 0;
+      err = run_tile<T, true, false, E_SLAB, O>(b.dh, d, st);
+    } else {
+      d.out = a.dh, d.ldo = a.dh_stride, d.row_coef = coef;
+      d.out_vec = a.dh_stride % 4 == 0 && (uintptr_t)a.dh % 16 == 0;
+      err = run_tile<T, true, false, E_OUT, O>(b.dh, d, st);
+    }
+    if (err) return err;
+
+    GemmArgs e{};  // dw = g^T h
+    e.a = o.h, e.lda = o.ldh, e.a_part = o.h_part, e.a_rows = (int)b.op.ldp;
+    e.b = g.g, e.ldb = b.ldg, e.b_part = g_part, e.b_rows = (int)up(vc, 8);
+    e.M = a.C, e.N = vc, e.K = (int)a.n, e.products = products, e.splits = b.dw_splits;
+    e.unscale = unscale;
+    O* dw = (O*)a.dw + v0 * a.dw_stride;
+    if (b.dw_slab) {
+      e.slab = (float*)(work + b.dw_at), e.slab_ld = b.slab_ld, e.slab_stride = std::min<int64_t>(b.vc, a.V) * b.slab_ld;
+      if ((err = run_tile<T, true, true, E_SLAB, O>(b.dw, e, st))) return err;
+      const unsigned grid = (unsigned)std::min<int64_t>(((int64_t)vc * ((a.C + 7) / 8) + 255) / 256, 8192);
+      join_slabs_kernel<O><<<grid, 256, 0, st>>>(e.slab, e.slab_ld, e.slab_stride, b.dw_splits, vc, a.C, unscale, nullptr, dw,
+                                                 a.dw_stride);
+      err = (int)hipGetLastError();
+    } else {
+      e.out = dw, e.ldo = a.dw_stride;
+      e.out_vec = a.dw_stride % 4 == 0 && (uintptr_t)a.dw % 16 == 0;
+      err = run_tile<T, true, true, E_OUT, O>(b.dw, e, st);
+    }
+    if (err) return err;
+  }
+  if (b.dh_slab) {
+    const unsigned grid = (unsigned)std::min<int64_t>((a.n * ((a.C + 7) / 8) + 255) / 256, 8192);
+    join_slabs_kernel<O><<<grid, 256, 0, st>>>((const float*)(work + b.dh_at), b.slab_ld, a.n * b.slab_ld, b.dh_splits, a.n, a.C,
+                                               unscale, coef, (O*)a.dh, a.dh_stride);
+    err = (int)hipGetLastError();
+  }
+  return err;
+}
+
+}  // namespace
+
+size_t softmax_loss_bytes(const LossArgs& a, dn_dtype dt) { return plan_forward(a, dt).total; }
+size_t softmax_loss_backward_bytes(const LossArgs& a, dn_dtype dt) { return a.n ? plan_backward(a, dt).total : 0; }
+
+int launch_softmax_loss(const LossArgs& a, dn_dtype dt, void* d_work, void* stream) {
+  const FwdPlan f = plan_forward(a, dt);
+  const hipStream_t st = (hipStream_t)stream;
+  Operands o;
+  if (const int err = lay_out(a, dt, f.op, (char*)d_work, false, o, st)) return err;
+  return dt == DN_F16 ? forward<_Float16>(a, f, o, (char*)d_work, st) : forward<__bf16>(a, f, o, (char*)d_work, st);
+}
+
+int launch_softmax_loss_backward(const LossArgs& a, dn_dtype dt, void* d_work, void* stream) {
+  if (a.n == 0) {  // no rows: dw is 0
+    const unsigned grid = (unsigned)std::min<int64_t>(((int64_t)a.V * a.C + 255) / 256, 8192);
+    if (dt == DN_F32)
+      zero_rows_kernel<float><<<grid, 256, 0, (hipStream_t)stream>>>((float*)a.dw, a.dw_stride, a.V, a.C);
+    else
+      zero_rows_kernel<uint16_t><<<grid, 256, 0, (hipStream_t)stream>>>((uint16_t*)a.dw, a.dw_stride, a.V, a.C);
+    return (int)hipGetLastError();
+  }
+  const BackPlan b = plan_backward(a, dt);
+  const hipStream_t st = (hipStream_t)stream;
+  Operands o;
+  if (const int err = lay_out(a, dt, b.op, (char*)d_work, true, o, st)) return err;
+  if (dt == DN_F32) return backward<__bf16, float>(a, b, o, (char*)d_work, 1.f, st);
+  if (dt == DN_F16) return backward<_Float16, _Float16>(a, b, o, (char*)d_work, 1024.f, st);
+  return backward<__bf16, __bf16>(a, b, o, (char*)d_work, 1.f, st);
+}
+
+}  // namespace head
+}  // namespace dn
