@@ -484,25 +484,28 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
   }
 }
 
-// Joins the tiles of a row: 16 rows per workgroup, 16 tiles at a time.
+// Joins the tiles of a row: ROWS rows per workgroup, 256 / ROWS tiles at a time (16 rows share the lines that their
+// statistics lie in; of a few rows each takes a workgroup).
+template <int ROWS>
 __global__ __launch_bounds__(256) void join_stats_kernel(const float2* __restrict__ stats, const float* __restrict__ at,
                                                          const int64_t* __restrict__ label, int tiles, int n, int V,
                                                          float* __restrict__ loss, float* __restrict__ lse) {
-  __shared__ float2 s_red[4][16];
-  const int row = blockIdx.x * 16 + (threadIdx.x & 15), t0 = threadIdx.x >> 4;
+  __shared__ float2 s_red[4][ROWS];
+  const int row = blockIdx.x * ROWS + threadIdx.x % ROWS, t0 = threadIdx.x / ROWS;
   float top = -INFINITY, sum = 0.f;
-  auto add = [&](float2 o) {  // (0, -inf) adds nothing; a NaN sum stays
+  auto add = [&](float2 o) {  // (-inf, 0) adds nothing; a NaN sum stays
     const float m = fmaxf(top, o.x), ref = m == -INFINITY ? 0.f : m;
     sum = (top == -INFINITY ? sum : sum * exp_of(top - ref)) + (o.x == -INFINITY ? o.y : o.y * exp_of(o.x - ref));
     top = m;
   };
   if (row < n)
-    for (int t = t0; t < tiles; t += 16) add(stats[(int64_t)t * n + row]);
-  add(float2{__shfl_xor(top, 16), __shfl_xor(sum, 16)});
-  add(float2{__shfl_xor(top, 32), __shfl_xor(sum, 32)});
-  if ((threadIdx.x & 63) < 16) s_red[threadIdx.x >> 6][threadIdx.x & 15] = float2{top, sum};
+#pragma unroll 4
+    for (int t = t0; t < tiles; t += 256 / ROWS) add(stats[(int64_t)t * n + row]);
+#pragma unroll
+  for (int d = ROWS; d < 64; d *= 2) add(float2{__shfl_xor(top, d), __shfl_xor(sum, d)});
+  if ((threadIdx.x & 63) < ROWS) s_red[threadIdx.x >> 6][threadIdx.x & 63] = float2{top, sum};
   __syncthreads();
-  if (threadIdx.x < 16 && row < n) {
+  if (threadIdx.x < ROWS && row < n) {
     for (int w = 1; w < 4; ++w) add(s_red[w][threadIdx.x]);
     const int64_t l = label[row];
     const bool has = l >= 0 && l < V;
@@ -553,6 +556,7 @@ __global__ __launch_bounds__(1024) void coef_kernel(const int64_t* __restrict__ 
   __shared__ float s_red[16];
   __shared__ float s_mul;
   float v = 0.f;
+#pragma unroll 8
   for (int64_t i = threadIdx.x; i < n; i += 1024) {
     const bool has = label[i] >= 0 && label[i] < V;
     const float d = has ? (dloss ? fabsf(dloss[i]) : 1.f) : 0.f;
@@ -575,6 +579,7 @@ __global__ __launch_bounds__(1024) void coef_kernel(const int64_t* __restrict__ 
     }
   }
   __syncthreads();
+#pragma unroll 8
   for (int64_t i = threadIdx.x; i < n; i += 1024) {
     const bool has = label[i] >= 0 && label[i] < V;
     coef[i] = has ? (dloss ? dloss[i] : 1.f) * s_mul : 0.f;
@@ -624,6 +629,7 @@ __global__ __launch_bounds__(256) void join_slabs_kernel(const float* __restrict
     const int64_t row = i / per;
     const int c = (int)(i - row * per) * 8;
     float v[8] = {};
+#pragma unroll 4
     for (int s = 0; s < splits; ++s) {
       float w[8];
       load8(slab + s * stride + row * ld + c, w);
@@ -662,17 +668,37 @@ bool lies_well(const void* p, int64_t ld, int32_t C, dn_dtype dt) {
   return dt != DN_F32 && (uintptr_t)p % 16 == 0 && ld % 8 == 0 && C % 8 == 0 && ld <= MAX_LD;
 }
 
-// Splits of a launch's k over workgroups: the fewest that minimise the rounds of workgroups per split, at `slots`
-// workgroups a round, each split at least `least` stages long.
-int splits_for(int64_t tiles, int64_t stages, int slots, int least) {
-  int best = 1;
-  double cost = 1e30;
-  for (int s = 1; s <= 64 && (s == 1 || stages / s >= least); ++s) {
-    const double c = (double)((tiles * s + slots - 1) / slots) / s * (1 + 0.02 * (s - 1)) + (s > 1 ? 0.05 : 0);
-    if (c < cost - 1e-9) cost = c, best = s;
-  }
-  return best;
+// Tile shapes: T256 (8 waves, a workgroup per CU), T128 (4 waves, two per CU), and for the logits of few rows T64 and T32
+// (128 words x 64 or 32 rows).
+enum Tile { T256, T128, T64, T32 };
+int tile_m(Tile t) { return t == T256 ? 256 : 128; }
+int tile_n(Tile t) { return t == T256 ? 256 : t == T128 ? 128 : t == T64 ? 64 : 32; }
+
+// The time of a product [M][N] over `stages` of 64 k in us, by what launches of many shapes took: a stage of T256 takes 1.25
+// us on an idle chip and 1.85 on a full one, of T128 0.62 alone on a CU and 1.1 (turned operands: 1.2) for two, and a
+// workgroup's start and end 5 to 7.  In splits, the partial sums' traffic and the launch that adds them come on top.
+double product_us(Tile t, int64_t M, int64_t N, int64_t stages, int splits, bool turned) {
+  const int64_t tiles = ((M + tile_m(t) - 1) / tile_m(t)) * ((N + tile_n(t) - 1) / tile_n(t)) * splits;
+  const double st = (double)((stages + splits - 1) / splits), per_cu = (double)((tiles + 255) / 256);
+  double us;
+  if (t == T256)
+    us = per_cu * (st * (1.25 + 0.6 * std::min(1.0, tiles / 192.0)) + 7);
+  else if (t == T128)
+    us = tiles <= 256 ? st * (0.62 + 0.25 * tiles / 256.0) + 5 : per_cu / 2 * (st * (turned ? 1.2 : 1.1) + 6);
+  else  // at least the time that reading M x k takes
+    us = std::max(tiles <= 256 ? st * 0.5 + 4 : per_cu / 2 * (st * 0.6 + 4), (double)M * stages * 128 / 5e6);
+  return us + (splits > 1 ? 5 + (double)splits * M * N * 6 / 5e6 : 0);
 }
+// The tile and the splits with the least time (splits of at least 4 stages; one split unless `split`).
+void choose(const Tile* of, int n_tiles, int64_t M, int64_t N, int64_t stages, bool split, bool turned, Tile& tile, int& splits) {
+  double best = 1e300;
+  for (int i = 0; i < n_tiles; ++i)
+    for (int s = 1; s <= 64 && (s == 1 || (split && stages / s >= 4)); ++s) {
+      const double us = product_us(of[i], M, N, stages, s, turned);
+      if (us < best * 0.999) best = us, tile = of[i], splits = s;
+    }
+}
+int64_t stages_of(int64_t k, int parts) { return (k + BK - 1) / BK * (parts == 3 ? 6 : 1); }
 
 struct Plan {
   bool pack_h, pack_w;
@@ -705,11 +731,6 @@ int pack_any(dn_dtype dt, const void* in, int64_t ld, int64_t rows, int C, void*
   return pack((const __bf16*)in, ld, rows, C, out, ldo, label, V, st);
 }
 
-// Tile shapes.
-enum Tile { T256, T128, T64, T32 };
-int tile_m(Tile t) { return t == T256 ? 256 : 128; }
-int tile_n(Tile t) { return t == T256 ? 256 : t == T128 ? 128 : t == T64 ? 64 : 32; }
-
 template <typename T, bool AT, bool BT, Epilogue E, typename O, int BM, int BN, int WM, int WN, int NST>
 int run_gemm(GemmArgs& g, hipStream_t st) {
   g.tiles_m = (g.M + BM - 1) / BM, g.tiles_n = (g.N + BN - 1) / BN;
@@ -739,12 +760,9 @@ FwdPlan plan_forward(const LossArgs& a, dn_dtype dt) {
   FwdPlan f{};
   Work w;
   f.op = plan_operands(a, dt, false, w);
-  const int64_t t256 = ((a.V + 255) / 256) * ((a.n + 255) / 256);
-  f.tile = a.n <= 32 ? T32 : a.n <= 64 ? T64 : t256 >= 200 ? T256 : T128;
+  const Tile few[] = {a.n <= 32 ? T32 : T64}, many[] = {T256, T128};
+  choose(a.n <= 64 ? few : many, a.n <= 64 ? 1 : 2, a.V, a.n, stages_of(f.op.ldp, f.op.parts), true, false, f.tile, f.splits);
   f.tiles_m = (a.V + tile_m(f.tile) - 1) / tile_m(f.tile);
-  const int64_t tiles = f.tiles_m * ((a.n + tile_n(f.tile) - 1) / tile_n(f.tile));
-  const int64_t stages = (f.op.ldp + BK - 1) / BK * (f.op.parts == 3 ? 6 : 1);
-  f.splits = f.tile == T256 || tiles >= 192 ? 1 : splits_for(tiles, stages, 256, 4);
   f.logits = f.splits > 1;
   f.at_at = w.take((size_t)a.n * 4);
   if (f.logits) {
@@ -771,23 +789,17 @@ BackPlan plan_backward(const LossArgs& a, dn_dtype dt) {
   BackPlan b{};
   Work w;
   b.op = plan_operands(a, dt, true, w);
-  const int pr = b.op.parts == 3 ? 6 : 1;
   const int64_t v256 = up(a.V, 256);
   b.vc = std::min(v256, std::max<int64_t>(256, PIECE_BYTES / (2 * a.n) / 256 * 256));
   const int64_t pieces = (v256 + b.vc - 1) / b.vc;
   b.vc = up((v256 + pieces - 1) / pieces, 256);
   b.ldg = b.vc;
-  const auto tiles = [](int64_t m, int64_t n, int t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
-  const auto pick = [&](int64_t m, int64_t n, int64_t k, Tile& t, int& s) {
-    const int64_t stages = (k + BK - 1) / BK * pr;
-    const int64_t t256 = tiles(m, n, 256);
-    const int s256 = splits_for(t256, stages, 256, 16);
-    t = t256 * s256 >= 200 ? T256 : T128;
-    s = t == T256 ? s256 : splits_for(tiles(m, n, 128), stages, 512, 8);
-  };
-  b.grad = tiles(b.vc, a.n, 256) >= 200 ? T256 : T128;
-  pick(a.C, a.n, b.vc, b.dh, b.dh_splits);
-  pick(a.C, std::min<int64_t>(b.vc, a.V), a.n, b.dw, b.dw_splits);
+  const Tile any[] = {T256, T128};
+  const int64_t words = std::min<int64_t>(b.vc, a.V);
+  int one;
+  choose(any, 2, words, a.n, stages_of(b.op.ldp, b.op.parts), false, false, b.grad, one);
+  choose(any, 2, a.C, a.n, stages_of(words, b.op.parts), true, true, b.dh, b.dh_splits);
+  choose(any, 2, a.C, words, stages_of(a.n, b.op.parts), true, true, b.dw, b.dw_splits);
   b.dh_slab = pieces > 1 || b.dh_splits > 1;
   b.dw_slab = b.dw_splits > 1;
   b.slab_ld = up(a.C, 256);
@@ -834,8 +846,11 @@ int forward(const LossArgs& a, const FwdPlan& f, const Operands& o, char* work, 
   } else {
     g.stats = (float2*)(work + f.stats_at);
     if ((err = run_tile<T, false, false, E_STATS, T>(f.tile, g, st))) return err;
-    join_stats_kernel<<<dim3((unsigned)((a.n + 15) / 16)), 256, 0, st>>>(g.stats, g.at, a.label, g.tiles_m, (int)a.n, a.V, a.loss,
-                                                                        a.lse);
+    if (a.n <= 64)
+      join_stats_kernel<1><<<dim3((unsigned)a.n), 256, 0, st>>>(g.stats, g.at, a.label, g.tiles_m, (int)a.n, a.V, a.loss, a.lse);
+    else
+      join_stats_kernel<16><<<dim3((unsigned)((a.n + 15) / 16)), 256, 0, st>>>(g.stats, g.at, a.label, g.tiles_m, (int)a.n, a.V,
+                                                                              a.loss, a.lse);
   }
   return (int)hipGetLastError();
 }
