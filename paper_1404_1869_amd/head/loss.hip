@@ -675,19 +675,19 @@ int tile_m(Tile t) { return t == T256 ? 256 : 128; }
 int tile_n(Tile t) { return t == T256 ? 256 : t == T128 ? 128 : t == T64 ? 64 : 32; }
 
 // The time of a product [M][N] over `stages` of 64 k in us, by what launches of many shapes took: a stage of T256 takes 1.25
-// us on an idle chip and 1.85 on a full one, of T128 0.62 alone on a CU and 1.1 (turned operands: 1.2) for two, and a
-// workgroup's start and end 5 to 7.  In splits, the partial sums' traffic and the launch that adds them come on top.
+// us on an idle chip and 1.75 on a full one, of T128 0.62 alone on a CU and 1.1 (turned operands: 1.2) for two, and a
+// workgroup's start and end 5 to 10.  In splits, the partial sums' traffic and the launch that adds them come on top.
 double product_us(Tile t, int64_t M, int64_t N, int64_t stages, int splits, bool turned) {
   const int64_t tiles = ((M + tile_m(t) - 1) / tile_m(t)) * ((N + tile_n(t) - 1) / tile_n(t)) * splits;
   const double st = (double)((stages + splits - 1) / splits), per_cu = (double)((tiles + 255) / 256);
   double us;
   if (t == T256)
-    us = per_cu * (st * (1.25 + 0.6 * std::min(1.0, tiles / 192.0)) + 7);
+    us = per_cu * (st * (1.25 + 0.5 * std::min(1.0, tiles / 256.0)) + 10);
   else if (t == T128)
     us = tiles <= 256 ? st * (0.62 + 0.25 * tiles / 256.0) + 5 : per_cu / 2 * (st * (turned ? 1.2 : 1.1) + 6);
   else  // at least the time that reading M x k takes
     us = std::max(tiles <= 256 ? st * 0.5 + 4 : per_cu / 2 * (st * 0.6 + 4), (double)M * stages * 128 / 5e6);
-  return us + (splits > 1 ? 5 + (double)splits * M * N * 6 / 5e6 : 0);
+  return us + (splits > 1 ? 5 + (double)splits * M * N * 8 / 5e6 : 0);
 }
 // The tile and the splits with the least time (splits of at least 4 stages; one split unless `split`).
 void choose(const Tile* of, int n_tiles, int64_t M, int64_t N, int64_t stages, bool split, bool turned, Tile& tile, int& splits) {

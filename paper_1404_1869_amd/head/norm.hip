@@ -12,15 +12,16 @@ namespace dn {
 namespace head {
 namespace {
 
-// Sum of K values per thread over the TPR threads of a row, in every one of them.  TPR = 64: a wave.  Else the
-// waves' sums meet in LDS; `buf` alternates between calls, so that one barrier separates a call's reads from the
-// next but one's writes.
-template <int TPR, int K, bool MAX = false>
-__device__ inline void row_reduce(float (&v)[K], float (*buf)[TPR / 64]) {
+// Sum (or maximum) of K values per thread over the threads of a row, in every one of them: a wave (WAVE), or the whole
+// workgroup, whose waves' sums meet in LDS.  `buf` alternates between calls, so that one barrier separates a call's reads
+// from the next but one's writes.
+constexpr int MAX_WAVES = 16;
+template <bool WAVE, int K, bool MAX = false>
+__device__ inline void row_reduce(float (&v)[K], float (*buf)[MAX_WAVES]) {
 #pragma unroll
   for (int k = 0; k < K; ++k) v[k] = MAX ? lanes_max<64>(v[k]) : lanes_sum<64>(v[k]);
-  if constexpr (TPR > 64) {
-    const int wave = threadIdx.x >> 6;
+  if constexpr (!WAVE) {
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
       for (int k = 0; k < K; ++k) buf[k][wave] = v[k];
@@ -28,51 +29,58 @@ __device__ inline void row_reduce(float (&v)[K], float (*buf)[TPR / 64]) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float t = buf[k][0];
-#pragma unroll
-      for (int w = 1; w < TPR / 64; ++w) t = MAX ? fmaxf(t, buf[k][w]) : t + buf[k][w];
+      for (int w = 1; w < waves; ++w) t = MAX ? fmaxf(t, buf[k][w]) : t + buf[k][w];
       v[k] = t;
     }
   }
 }
 
-// Threads of a workgroup: TPR per row, at least 256.
-template <int TPR>
-constexpr int threads() { return TPR < 256 ? 256 : TPR; }
+// Eight values of a row as they are stored, 0 past its end.
+template <typename T>
+using Raw = typename Vec8<T>::type;
+template <typename T>
+__device__ inline Raw<T> load_raw(const T* row, int i, int C) {
+  if (i + 8 <= C) return *(const Raw<T>*)(row + i);
+  Raw<T> r;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r[j] = i + j < C ? row[i + j] : (T)0.f;
+  return r;
+}
 
-// Thread t of a row holds elements 8 (k TPR + t) .. + 7, k < NV: 16-byte accesses of consecutive threads.
-template <typename T, typename O, int TPR, int NV>
-__global__ __launch_bounds__(threads<TPR>()) void rms_norm_kernel(NormArgs a) {
-  constexpr int ROWS = threads<TPR>() / TPR;
-  __shared__ float s_buf[2][1][TPR / 64];
-  const int t = threadIdx.x % TPR, C = a.C;
-  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
-  if (row >= a.n) return;  // whole waves, and only where TPR = 64 (no barriers)
+// Thread t of a row's TPR threads holds elements 8 (k TPR + t) .. + 7, k < NV: 16-byte accesses of consecutive threads.
+// WAVE: a wave per row, four rows per workgroup, no barriers; else the workgroup.
+// THREADS: the most threads of a workgroup of this shape.
+template <typename T, typename O, bool WAVE, int NV, int THREADS>
+__global__ __launch_bounds__(THREADS) void rms_norm_kernel(NormArgs a) {
+  __shared__ float s_buf[2][1][MAX_WAVES];
+  const int TPR = WAVE ? 64 : blockDim.x, t = WAVE ? threadIdx.x & 63 : threadIdx.x, C = a.C;
+  const int64_t row = WAVE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  if (row >= a.n) return;  // whole waves, and only where WAVE (no barriers)
   const T* x = (const T*)a.x + row * a.x_stride;
   const T* res = (const T*)a.res + row * a.res_stride;
-  float v[NV][8], r[NV][8], w[NV][8];
+  Raw<T> xr[NV], rr[NV];
 #pragma unroll
-  for (int k = 0; k < NV; ++k) load8(x, 8 * (k * TPR + t), C, v[k]);
+  for (int k = 0; k < NV; ++k) xr[k] = load_raw(x, 8 * (k * TPR + t), C);
   if (a.res)
 #pragma unroll
-    for (int k = 0; k < NV; ++k) load8(res, 8 * (k * TPR + t), C, r[k]);
+    for (int k = 0; k < NV; ++k) rr[k] = load_raw(res, 8 * (k * TPR + t), C);
+  float v[NV][8], w[NV][8];
   if (a.gamma)
 #pragma unroll
     for (int k = 0; k < NV; ++k) load8(a.gamma, 8 * (k * TPR + t), C, w[k]);
-  if (a.res)
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[k][j] += r[k][j];
-  if (a.sum)
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-      store8((T*)a.sum + row * a.sum_stride, 8 * (k * TPR + t), C, v[k]);
   float ss[1] = {0.f};
 #pragma unroll
   for (int k = 0; k < NV; ++k)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) ss[0] += v[k][j] * v[k][j];
-  row_reduce<TPR>(ss, s_buf[0]);
+    for (int j = 0; j < 8; ++j) {
+      v[k][j] = a.res ? (float)xr[k][j] + (float)rr[k][j] : (float)xr[k][j];
+      ss[0] += v[k][j] * v[k][j];
+    }
+  if (a.sum)
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      store8((T*)a.sum + row * a.sum_stride, 8 * (k * TPR + t), C, v[k]);
+  row_reduce<WAVE>(ss, s_buf[0]);
   const float q = 1.f / sqrtf(ss[0] / (float)C + a.eps);
 #pragma unroll
   for (int k = 0; k < NV; ++k)
@@ -91,7 +99,7 @@ __global__ __launch_bounds__(threads<TPR>()) void rms_norm_kernel(NormArgs a) {
       float m[1] = {top[0]};
 #pragma unroll
       for (int k = 1; k < NV; ++k) m[0] = fmaxf(m[0], top[k]);
-      row_reduce<TPR, 1, true>(m, s_buf[1]);
+      row_reduce<WAVE, 1, true>(m, s_buf[1]);
 #pragma unroll
       for (int k = 0; k < NV; ++k) top[k] = m[0];
       if (t == 0) a.scale[row] = m[0] * (1.f / 448.f);
@@ -117,56 +125,83 @@ __global__ __launch_bounds__(threads<TPR>()) void rms_norm_kernel(NormArgs a) {
   for (int k = 0; k < NV; ++k) store8(y, 8 * (k * TPR + t), C, v[k]);
 }
 
-// Gradient: a workgroup takes rows blockIdx.x, blockIdx.x + gridDim.x, ... (groups of ROWS rows), keeps its sums of
-// dy s q per column in registers over them, and writes them as one row of part (ROWS rows of it where TPR = 64).
-template <typename T, typename D, int TPR, int NV>
-__global__ __launch_bounds__(threads<TPR>()) void rms_norm_back_kernel(NormBackArgs a) {
-  constexpr int ROWS = threads<TPR>() / TPR;
-  __shared__ float s_buf[2][2][TPR / 64];
-  const int t = threadIdx.x % TPR, C = a.C, sub = threadIdx.x / TPR;
-  float dg[NV][8], w[NV][8];
+// Gradient: a workgroup (WAVE: each of its waves) takes rows at a fixed distance, loads a row while it works on the one
+// before (AHEAD), keeps its sums of dy s q per column in registers over them, and writes them as one row of part.
+// THREADS: the most threads of a workgroup of this shape, which bounds its registers.
+template <typename T, typename D, bool WAVE, int NV, int THREADS, bool AHEAD>
+__global__ __launch_bounds__(THREADS) void rms_norm_back_kernel(NormBackArgs a) {
+  constexpr bool HOLD = NV < 4;  // gamma stays in registers
+  __shared__ float s_buf[2][2][MAX_WAVES];
+  const int TPR = WAVE ? 64 : blockDim.x, t = WAVE ? threadIdx.x & 63 : threadIdx.x, C = a.C;
+  const int64_t first = WAVE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  const int64_t step = a.groups;
+  float dg[NV][8], held[HOLD ? NV : 1][8];
+  auto gamma = [&](int k, float (&w)[8]) {
+    if (a.gamma) {
+      load8(a.gamma, 8 * (k * TPR + t), C, w);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = 1.f;
+    }
+  };
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) dg[k][j] = 0.f, w[k][j] = 1.f;
-    if (a.gamma) load8(a.gamma, 8 * (k * TPR + t), C, w[k]);
+    for (int j = 0; j < 8; ++j) dg[k][j] = 0.f;
+    if constexpr (HOLD) gamma(k, held[k]);
   }
-  int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + sub; row < a.n; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
-    const T* s = (const T*)a.s + row * a.s_stride;
-    const D* dy = (const D*)a.dy + row * a.dy_stride;
-    float v[NV][8], d[NV][8], e[NV][8];
+  struct Row {
+    Raw<T> s[NV], e[NV];
+    Raw<D> d[NV];
+  };
+  auto load = [&](int64_t row, Row& r) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      load8(s, 8 * (k * TPR + t), C, v[k]);
-      load8(dy, 8 * (k * TPR + t), C, d[k]);
-      if (a.dsum) load8((const T*)a.dsum + row * a.dsum_stride, 8 * (k * TPR + t), C, e[k]);
+      const int i = 8 * (k * TPR + t);
+      r.s[k] = load_raw((const T*)a.s + row * a.s_stride, i, C);
+      r.d[k] = load_raw((const D*)a.dy + row * a.dy_stride, i, C);
+      if (a.dsum) r.e[k] = load_raw((const T*)a.dsum + row * a.dsum_stride, i, C);
     }
+  };
+  Row next;
+  if (AHEAD && first < a.n) load(first, next);
+  int turn = 0;
+  for (int64_t row = first; row < a.n; row += step, turn ^= 1) {
+    Row r;
+    if constexpr (AHEAD) r = next;
+    else load(row, r);
     float z[2] = {0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
+      float w[8];
+      if constexpr (!HOLD) gamma(k, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        z[0] += v[k][j] * v[k][j];
-        z[1] += d[k][j] * w[k][j] * v[k][j];
+        const float v = (float)r.s[k][j];
+        z[0] += v * v;
+        z[1] += (float)r.d[k][j] * (HOLD ? held[HOLD ? k : 0][j] : w[j]) * v;
       }
-    row_reduce<TPR>(z, s_buf[turn]);
+    }
+    if (AHEAD && row + step < a.n) load(row + step, next);
+    row_reduce<WAVE>(z, s_buf[turn]);
     const float q = 1.f / sqrtf(z[0] / (float)C + a.eps), f = q * q * (z[1] / (float)C);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
+      float w[8], x[8];
+      if constexpr (!HOLD) gamma(k, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        dg[k][j] += d[k][j] * (v[k][j] * q);
-        const float g = q * (d[k][j] * w[k][j] - v[k][j] * f);
-        v[k][j] = a.dsum ? g + e[k][j] : g;
+        const float v = (float)r.s[k][j], g = (float)r.d[k][j];
+        dg[k][j] += g * (v * q);
+        x[j] = q * (g * (HOLD ? held[HOLD ? k : 0][j] : w[j]) - v * f);
+        if (a.dsum) x[j] += (float)r.e[k][j];
       }
-      store8((T*)a.dx + row * a.dx_stride, 8 * (k * TPR + t), C, v[k]);
+      store8((T*)a.dx + row * a.dx_stride, 8 * (k * TPR + t), C, x);
     }
   }
   if (a.dgamma)
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-      store8(a.part + ((int64_t)blockIdx.x * ROWS + sub) * C, 8 * (k * TPR + t), C, dg[k]);
+    for (int k = 0; k < NV; ++k) store8(a.part + first * C, 8 * (k * TPR + t), C, dg[k]);
 }
 
 // Sums of the columns of part ([rows][C]), always in the same order: 32 columns per workgroup, 8 rows at a time.
@@ -195,22 +230,14 @@ __global__ __launch_bounds__(256) void column_sum_kernel(const float* __restrict
   }
 }
 
-// The fewest threads and registers that hold a row: f(integral_constant TPR, integral_constant NV).
-template <int TPR, int NV>
+// The most threads of a workgroup whose threads hold NV times eight values of rows of up to C.
+template <bool WAVE_, int NV_, int C>
 struct Shape {
-  static constexpr int tpr = TPR, nv = NV;
+  static constexpr bool wave = WAVE_;
+  static constexpr int nv = NV_, most = WAVE_ ? 256 : C / (8 * NV_);
+  // whole waves that hold a row of C_ values
+  static int threads(int C_) { return WAVE_ ? 256 : (C_ + 512 * NV_ - 1) / (512 * NV_) * 64; }
 };
-template <typename F>
-int with_shape(int C, F&& f) {
-  if (C <= 512) return f(Shape<64, 1>{});
-  if (C <= 1024) return f(Shape<64, 2>{});
-  if (C <= 2048) return f(Shape<256, 1>{});
-  if (C <= 4096) return f(Shape<256, 2>{});
-  if (C <= 8192) return f(Shape<512, 2>{});
-  if (C <= 12288) return f(Shape<512, 3>{});
-  if (C <= 16384) return f(Shape<1024, 2>{});
-  return f(Shape<1024, 4>{});
-}
 template <typename F>
 int with_type(dn_dtype dt, F&& f) {
   if (dt == DN_F32) return f(float{});
@@ -220,41 +247,63 @@ int with_type(dn_dtype dt, F&& f) {
 
 }  // namespace
 
+// A wave per row where its lanes can hold it in up to four times eight values each, else a workgroup.
 int launch_rms_norm(const NormArgs& a, dn_dtype dt, dn_dtype y_dt, void* stream) {
-  return with_shape(a.C, [&](auto shape) {
-    constexpr int TPR = decltype(shape)::tpr, NV = decltype(shape)::nv, ROWS = threads<TPR>() / TPR;
+  const auto with = [&](auto shape) {
+    using S = decltype(shape);
     return with_type(dt, [&](auto x) {
       using T = decltype(x);
-      const dim3 grid((unsigned)((a.n + ROWS - 1) / ROWS));
+      const dim3 grid((unsigned)(S::wave ? (a.n + 3) / 4 : a.n));
+      const int threads = S::threads(a.C);
       if (y_dt == DN_F8)
-        rms_norm_kernel<T, F8, TPR, NV><<<grid, threads<TPR>(), 0, (hipStream_t)stream>>>(a);
+        rms_norm_kernel<T, F8, S::wave, S::nv, S::most><<<grid, threads, 0, (hipStream_t)stream>>>(a);
       else
         with_type(y_dt, [&](auto y) {
-          rms_norm_kernel<T, decltype(y), TPR, NV><<<grid, threads<TPR>(), 0, (hipStream_t)stream>>>(a);
+          rms_norm_kernel<T, decltype(y), S::wave, S::nv, S::most><<<grid, threads, 0, (hipStream_t)stream>>>(a);
           return 0;
         });
       return (int)hipGetLastError();
     });
-  });
+  };
+  if (a.C <= 512) return with(Shape<true, 1, 512>{});
+  if (a.C <= 1024) return with(Shape<true, 2, 1024>{});
+  if (a.C <= 2048) return with(Shape<true, 4, 2048>{});
+  if (a.C <= 8192) return with(Shape<false, 2, 8192>{});
+  if (a.C <= 16384) return with(Shape<false, 2, 16384>{});
+  return with(Shape<false, 4, DN_MAX_NORM_C>{});
 }
 
-// Rows of part: one per workgroup (or wave) of the gradient's launch.
+// Rows of part: one per workgroup (or wave) of the gradient's launch.  More workgroups cover each other's waits, and each
+// costs a row of part: 2 to 4 per CU (of 512, 768, 1024 and 2048 workgroups, 32000 rows of 4096 took 217, 211, 211 and 234 us).
 int32_t norm_back_groups(int64_t n, int32_t C) {
-  const int64_t rows = C <= 1024 ? 4 : 1, most = 1024;
+  const int64_t rows = C <= 1024 ? 4 : 1, most = C <= 1024 || C > 4096 ? 512 : 768;
   return (int32_t)(std::min((n + rows - 1) / rows, most) * rows);
 }
 
 int launch_rms_norm_backward(const NormBackArgs& a, dn_dtype dt, dn_dtype dy_dt, void* stream) {
-  const int err = a.n == 0 ? 0 : with_shape(a.C, [&](auto shape) {
-    constexpr int TPR = decltype(shape)::tpr, NV = decltype(shape)::nv, ROWS = threads<TPR>() / TPR;
+  const auto with = [&](auto shape) {
+    using S = decltype(shape);
     return with_type(dt, [&](auto x) {
       return with_type(dy_dt, [&](auto d) {
-        rms_norm_back_kernel<decltype(x), decltype(d), TPR, NV>
-            <<<dim3((unsigned)(a.groups / ROWS)), threads<TPR>(), 0, (hipStream_t)stream>>>(a);
+        using T = decltype(x);
+        using D = decltype(d);
+        // a second row in registers where they suffice: fp32 rows of over 12288 values, and rows of over 16384, would spill
+        constexpr bool AHEAD = S::nv < 4 && (S::most <= 768 || sizeof(T) == 2);
+        rms_norm_back_kernel<T, D, S::wave, S::nv, S::most, AHEAD>
+            <<<dim3((unsigned)(a.groups / (S::wave ? 4 : 1))), S::threads(a.C), 0, (hipStream_t)stream>>>(a);
         return (int)hipGetLastError();
       });
     });
-  });
+  };
+  int err = 0;
+  if (a.n == 0) err = 0;
+  else if (a.C <= 512) err = with(Shape<true, 1, 512>{});
+  else if (a.C <= 1024) err = with(Shape<true, 2, 1024>{});
+  else if (a.C <= 2048) err = with(Shape<false, 1, 2048>{});
+  else if (a.C <= 8192) err = with(Shape<false, 2, 8192>{});
+  else if (a.C <= 12288) err = with(Shape<false, 2, 12288>{});
+  else if (a.C <= 16384) err = with(Shape<false, 2, 16384>{});
+  else err = with(Shape<false, 4, DN_MAX_NORM_C>{});
   if (err || !a.dgamma) return err;
   column_sum_kernel<<<dim3((unsigned)((a.C + 31) / 32)), 256, 0, (hipStream_t)stream>>>(a.part, a.dgamma, a.groups, a.C);
   return (int)hipGetLastError();
