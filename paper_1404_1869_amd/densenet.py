@@ -9,6 +9,7 @@ On top of the raw entry points, ``convnet_featpyramid`` mirrors the paper's inte
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -645,23 +646,24 @@ def _code(t, what):
 def _rows(t, what, shape=None, dtype=None, device=None):
     """Checks a matrix of rows (elements of a row next to each other, rows any distance apart); returns its
     address and row stride."""
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+    size = t.shape
+    if len(size) != 2 or (shape is not None and size != shape):
         raise _bad(f"{what}: a matrix{'' if shape is None else f' of {shape[0]} x {shape[1]}'} expected, not "
-                   f"{tuple(t.shape)}")
+                   f"{tuple(size)}")
     if dtype is not None and t.dtype != dtype:
         raise _bad(f"{what}: {dtype} expected, not {t.dtype}")
-    if not t.is_cuda or (device is not None and t.device != device):
+    if (t.device != device) if device is not None else not t.is_cuda:
         raise _bad(f"{what}: not on the operands' GPU")
     row, col = t.stride()
-    if col != 1 and t.shape[1] > 1:
+    if col != 1 and size[1] > 1:
         raise _bad(f"{what}: the elements of a row must be next to each other")
-    return t.data_ptr(), row if t.shape[0] > 1 else t.shape[1]
+    return t.data_ptr(), row if size[0] > 1 else size[1]
 
 
 def _vector(t, what, n, dtype, device):
     if t is None:
         return None
-    if tuple(t.shape) != (n,) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if t.shape != (n,) or t.dtype != dtype or t.device != device or not t.is_contiguous():
         raise _bad(f"{what}: {n} contiguous {dtype} values on the operands' GPU expected")
     return t.data_ptr()
 
@@ -671,7 +673,17 @@ def _on(device):
     torch = _torch()
     if device.index != torch.cuda.current_device():
         raise _bad("the operands are not on the current GPU")
-    return torch.cuda.current_stream(device).cuda_stream
+    # the stream's address without a Stream object around it, 2 us less in a call of 13
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+@functools.lru_cache(maxsize=1024)
+def _work_bytes(entry, *args):
+    """The workspace that an entry point asks for: its size query, whose answer depends on sizes, strides and alignment."""
+    need = ctypes.c_size_t()
+    check(getattr(lib(), entry)(*args, None, 0, ctypes.byref(need), None))
+    return need.value
 
 
 def densenet_rms_norm(x, gamma=None, residual=None, eps=1e-6, out_dtype=None, block=0, out=None, sum_out=None,
@@ -681,11 +693,12 @@ def densenet_rms_norm(x, gamma=None, residual=None, eps=1e-6, out_dtype=None, bl
     of a row (0: the row).  Returns (y, s, scale): s is None without a residual or sum_out, scale without DN_F8."""
     torch = _torch()
     dt = _code(x, "x")
-    n, C = x.shape if x.dim() == 2 else (0, 0)
     xp, xs = _rows(x, "x")
+    n, C = x.shape
     dev = x.device
     ydt = dt if out_dtype is None else out_dtype
-    if ydt not in _types()[1]:
+    yt = _types()[1].get(ydt)
+    if yt is None:
         raise DenseNetError(DN_E_UNSUPPORTED, f"out_dtype {ydt}")
     if block not in (0, 32, 64, 128) or (block and ydt != DN_F8):
         raise DenseNetError(DN_E_UNSUPPORTED, "block: 0, or 32, 64 or 128 with DN_F8")
@@ -694,8 +707,8 @@ def densenet_rms_norm(x, gamma=None, residual=None, eps=1e-6, out_dtype=None, bl
         sum_out = torch.empty((n, C), dtype=x.dtype, device=dev)
     sp, ss = (None, 0) if sum_out is None else _rows(sum_out, "sum_out", (n, C), x.dtype, dev)
     if out is None:
-        out = torch.empty((n, C), dtype=_types()[1][ydt], device=dev)
-    yp, ys = _rows(out, "out", (n, C), _types()[1][ydt], dev)
+        out = torch.empty((n, C), dtype=yt, device=dev)
+    yp, ys = _rows(out, "out", (n, C), yt, dev)
     kp = None
     if ydt == DN_F8:
         blocks = -(-C // block) if block else 1
@@ -729,12 +742,11 @@ def densenet_rms_norm_backward(dy, s, gamma=None, dsum=None, eps=1e-6, dx=None, 
         dgamma = torch.empty(C, dtype=torch.float32, device=dev)
     gp = _vector(gamma, "gamma", C, torch.float32, dev)
     op = _vector(dgamma, "dgamma", C, torch.float32, dev)
-    need = ctypes.c_size_t()
-    L, st = lib(), _on(dev)
-    args = (dp, ds, ddt, sp, ss, ep, es, gp, n, C, dt, eps, xp, xs, op)
-    check(L.densenet_rms_norm_backward(*args, None, 0, ctypes.byref(need), st))
-    ws = torch.empty(max(need.value, 1), dtype=torch.uint8, device=dev)
-    check(L.densenet_rms_norm_backward(*args, ws.data_ptr(), ws.numel(), ctypes.byref(need), st))
+    # (the size depends on n and C alone, after the checks of both)
+    need = _work_bytes("densenet_rms_norm_backward", None, 0, ddt, None, 0, None, 0, None, n, C, dt, eps, None, 0, None)
+    ws = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    check(lib().densenet_rms_norm_backward(dp, ds, ddt, sp, ss, ep, es, gp, n, C, dt, eps, xp, xs, op, ws.data_ptr(), need, None,
+                                           _on(dev)))
     return dx, dgamma
 
 
@@ -751,6 +763,12 @@ def _loss_operands(h, w, labels):
     return (hp, hs, wp, ws, _vector(labels, "labels", n, torch.int64, dev)), n, C, V, dt, dev
 
 
+def _any_address(ops):
+    """h, w and labels as a size query sees them: addresses of the same alignment (to 16 bytes) in place of their own."""
+    hp, hs, wp, ws, lp = ops
+    return 4096 + hp % 16 if hp else None, hs, 4096 + wp % 16, ws, lp and 4096
+
+
 def densenet_softmax_loss(h, w, labels, loss=None, lse=None):
     """Softmax cross entropy of the rows of h [n][C] over the words of w [V][C].  labels: int64 [n]; outside [0, V) a row
     is masked (loss 0).  Returns (loss [n], lse [n]) in fp32, not reduced."""
@@ -758,12 +776,11 @@ def densenet_softmax_loss(h, w, labels, loss=None, lse=None):
     ops, n, C, V, dt, dev = _loss_operands(h, w, labels)
     loss = torch.empty(n, dtype=torch.float32, device=dev) if loss is None else loss
     lse = torch.empty(n, dtype=torch.float32, device=dev) if lse is None else lse
-    args = (*ops, n, C, V, dt, _vector(loss, "loss", n, torch.float32, dev), _vector(lse, "lse", n, torch.float32, dev))
-    need = ctypes.c_size_t()
-    L, st = lib(), _on(dev)
-    check(L.densenet_softmax_loss(*args, None, 0, ctypes.byref(need), st))
-    ws = torch.empty(max(need.value, 1), dtype=torch.uint8, device=dev)
-    check(L.densenet_softmax_loss(*args, ws.data_ptr(), ws.numel(), ctypes.byref(need), st))
+    at = _any_address(ops)
+    need = _work_bytes("densenet_softmax_loss", *at, n, C, V, dt, None, None)
+    ws = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    check(lib().densenet_softmax_loss(*ops, n, C, V, dt, _vector(loss, "loss", n, torch.float32, dev),
+                                      _vector(lse, "lse", n, torch.float32, dev), ws.data_ptr(), need, None, _on(dev)))
     return loss, lse
 
 
@@ -774,13 +791,12 @@ def densenet_softmax_loss_backward(h, w, labels, lse, dloss=None, scale=1.0, dh=
     ops, n, C, V, dt, dev = _loss_operands(h, w, labels)
     dh = torch.empty((n, C), dtype=h.dtype, device=dev) if dh is None else dh
     dw = torch.empty((V, C), dtype=h.dtype, device=dev) if dw is None else dw
-    args = (*ops, _vector(lse, "lse", n, torch.float32, dev), _vector(dloss, "dloss", n, torch.float32, dev), scale, n, C, V,
-            dt, *_rows(dh, "dh", (n, C), h.dtype, dev), *_rows(dw, "dw", (V, C), h.dtype, dev))
-    need = ctypes.c_size_t()
-    L, st = lib(), _on(dev)
-    check(L.densenet_softmax_loss_backward(*args, None, 0, ctypes.byref(need), st))
-    ws = torch.empty(max(need.value, 1), dtype=torch.uint8, device=dev)
-    check(L.densenet_softmax_loss_backward(*args, ws.data_ptr(), ws.numel(), ctypes.byref(need), st))
+    at = _any_address(ops)
+    need = _work_bytes("densenet_softmax_loss_backward", *at, None, None, 1.0, n, C, V, dt, None, 0, None, 0)
+    ws = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    check(lib().densenet_softmax_loss_backward(
+        *ops, _vector(lse, "lse", n, torch.float32, dev), _vector(dloss, "dloss", n, torch.float32, dev), scale, n, C, V, dt,
+        *_rows(dh, "dh", (n, C), h.dtype, dev), *_rows(dw, "dw", (V, C), h.dtype, dev), ws.data_ptr(), need, None, _on(dev)))
     return dh, dw
 
 

@@ -4,8 +4,13 @@
 // The forward pass is one matrix product whose tiles end in a maximum and a sum of exponentials per row; a second launch
 // joins the tiles.  The gradient goes over the vocabulary in pieces: a piece's logits are computed again and leave as g in
 // 16 bits, and two more products take dh and dw from it: 6 n V C operations, the least without the logits.
-// 16-bit types: products on the matrix cores, 32-bit sums.  fp32: every operand (h, w, g) as three bf16 parts and six
-// products of parts, as the library's fp32 convolutions.
+// 16-bit types: products on the matrix cores, 32-bit sums.  fp32, by what the product can take:
+//  logits: rows as two fp16 parts, x 2^k = a + b with 2^k such that the row's largest value lies in [2^13, 2^14), and three
+//    products a a' + a b' + b a'.  a and b hold 22 bits of a value, down to 2^-39 of the row's largest; what is left out is at
+//    most 2^-22 of a product and of either sign, as an fp32 product's and sum's roundings.  The row factors are powers of two.
+//  logits of up to 64 rows: bound by reading w, which fp32 MFMAs keep up with, so w is read as it lies and not laid out first.
+//  dh, dw: the sums run across rows, which have no common factor: three bf16 parts of every value (h, w, g) and six products,
+//    as the library's fp32 convolutions.
 // Rows whose label lies outside [0, V) are masked: loss and lse 0, g and dh 0, and what their h holds reaches nothing.
 #include <hip/hip_runtime.h>
 
@@ -14,28 +19,41 @@
 #include "head.h"
 
 namespace dn {
+// fp32 fragments: a lane's 16 bytes are four k of its row (k 4 (lane / 32) .. + 3 of eight), which four MFMAs of two k
+// take one after the other; A and B agree on the order of k.
+template <>
+struct Mfma<float> {
+  typedef f32x4 frag;
+  __device__ static inline f32x16 mma(frag a, frag b, f32x16 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+  }
+};
+
 namespace head {
 namespace {
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 constexpr uint32_t OOB = 0x80000000u;  // a buffer offset past every buffer: reads as 0
-constexpr int BK = 64;                 // k of one pipeline stage
+constexpr int BK = 64;                 // k of one pipeline stage (of 16-bit values; fp32: 32)
 constexpr int64_t MAX_LD = 1 << 22;    // elements between rows: 256 rows stay within 32-bit byte offsets
 
 enum Epilogue { E_STATS, E_GRAD, E_SLAB, E_OUT };
 
 // D[m][n] = sum_k A(m, k) B(n, k).  An operand lies with k along its rows ([m][k], plain) or with k across them ([k][m],
-// turned); ld: elements from row to row.
+// turned); ld: elements from row to row.  Elements are 16-bit ones; fp32 operands as they lie count two for each.
 struct GemmArgs {
   const void *a, *b;
-  int64_t lda, ldb, a_part, b_part;  // *_part: elements between the bf16 parts of fp32 operands
+  int64_t lda, ldb, a_part, b_part;  // *_part: elements between the parts of fp32 operands
   int32_t M, N, K;
   int32_t a_rows, b_rows;  // rows of the operand that may be read (turned: columns, a multiple of 8)
+  const float *a_factor, *b_factor;  // of the operands' rows (both or none): D[m][n] is multiplied by both
   int32_t tiles_m, tiles_n, products, splits;
   // E_STATS, E_GRAD: M runs over the vocabulary from v0 on, N over rows
   const int64_t* label;
   int32_t v0, V;
-  float2* stats;  // [tiles_m][N]: maximum and sum of exponentials
+  float2* stats;  // [tiles_m][N]: maximum, in base 2, and sum of exponentials over it
   float* at;      // [N]: the label's logit
   const float *lse, *coef;
   void* g;  // [N][ldg]
@@ -192,7 +210,9 @@ struct Fragments {
   }
 };
 
-__device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896f); }
+// Exponentials are taken to base 2 (the hardware's): exp x = 2^(x LOG2E).
+constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
+__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // x as three bf16 parts, each the nearest of what the ones before leave.
 __device__ inline void split3(float x, __bf16 (&p)[3]) {
@@ -203,10 +223,11 @@ __device__ inline void split3(float x, __bf16 (&p)[3]) {
 }
 
 // AT, BT: the operand is turned.  Waves: WM x WN, each (BM / WM) x (BN / WN).  NST: pipeline stages held in LDS.
-// G: parts that g is written in (E_GRAD).  O: type of E_OUT's results.
+// O: type of the operator's operands and results (float where T holds parts of fp32 values).
 template <typename T, bool AT, bool BT, int BM, int BN, int WM, int WN, int NST, Epilogue E, typename O>
 __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
   constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
+  constexpr bool MULTI = std::is_same<O, float>::value && !std::is_same<T, float>::value;  // parts of fp32 values
   using OA = Operand<T, AT, BM, NW>;
   using OB = Operand<T, BT, BN, NW>;
   constexpr int STAGE = OA::BYTES + OB::BYTES, PER = OA::PER + OB::PER;
@@ -237,11 +258,11 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
   fa.init(wm * WCOLS, lane);
   fb.init(wn * WROWS, lane);
 
-  const int kt = (g.K + BK - 1) / BK, total = kt * g.products;
+  const int kt = (g.K + BK - 1) / BK, total = MULTI ? kt * g.products : kt;
   const int s0 = (int)((int64_t)total * split / g.splits), s1 = (int)((int64_t)total * (split + 1) / g.splits);
   auto load = [&](int s, int buf) {
-    // products of parts from the smallest to the largest: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
-    const int pr = g.products == 1 ? 5 : s / kt, k0 = (g.products == 1 ? s : s - pr * kt) * BK;
+    // products of parts from the smallest to the largest, the last `products` of (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
+    const int turn = MULTI ? s / kt : 0, pr = MULTI ? 6 - g.products + turn : 5, k0 = (s - turn * kt) * BK;
     const int pa = pr == 0 ? 2 : pr == 1 || pr == 3 ? 1 : 0, pb = pr == 2 ? 2 : pr == 1 || pr == 4 ? 1 : 0;
     char* at = s_mem + buf * STAGE;
     oa.load(at, pa * g.a_part, k0, g.K, wave);
@@ -364,29 +385,69 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
 
   // Element r of acc[i][t]: m = m0 + wm WCOLS + 32 i + 8 (r / 4) + 4 half + r % 4, n = n0 + wn WROWS + 32 t + l32.
   const int mw = m0 + wm * WCOLS + 4 * half, nw = n0 + wn * WROWS + l32;
+  // fp32's logits from two fp16 parts: the rows' factors
+  if constexpr ((E == E_STATS || E == E_GRAD || E == E_SLAB) && !AT && std::is_same<T, _Float16>::value && std::is_same<O, float>::value) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int m = mw + 32 * i + 8 * q;
+        f32x4 f;
+        if (m + 4 <= g.M) {
+          f = *(const f32x4*)(g.a_factor + m);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[e] = m + e < g.M ? g.a_factor[m + e] : 0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < TN; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][t][4 * q + e] *= f[e];
+      }
+#pragma unroll
+    for (int t = 0; t < TN; ++t) {
+      const float f = nw + 32 * t < g.N ? g.b_factor[nw + 32 * t] : 0.f;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][t][r] *= f;
+    }
+  }
   if constexpr (E == E_STATS) {
     float2* red = (float2*)s_mem;
     __syncthreads();
+    if (m0 + BM > g.M)  // the last tile: what lies past the vocabulary counts for nothing
+#pragma unroll
+      for (int t = 0; t < TN; ++t)
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (mw + 32 * i + 8 * (r / 4) + r % 4 >= g.M) acc[i][t][r] = -INFINITY;
 #pragma unroll
     for (int t = 0; t < TN; ++t) {
       const int n = nw + 32 * t;
       const int lab = n < g.N ? (int)std::min<int64_t>(std::max<int64_t>(g.label[n], -1), g.V) - g.v0 : -1;
+      // the label's logit, where the wave has one: word lab is value (i, r) of the lanes of one half
+      const int d = lab - mw;
+      if (__any(d >= 0 && d < WCOLS && lab < g.M && !(d & 4)))
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (d == 32 * i + 8 * (r / 4) + r % 4 && lab < g.M) g.at[n] = acc[i][t][r];
       float top = -INFINITY, sum = 0.f;
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int m = mw + 32 * i + 8 * (r / 4) + r % 4;
-          if (m >= g.M) acc[i][t][r] = -INFINITY;
-          if (m == lab && m < g.M) g.at[n] = acc[i][t][r];
-          top = fmaxf(top, acc[i][t][r]);
-        }
-      top = fmaxf(top, __shfl_xor(top, 32));
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][t][r]);
+      // the maximum in base 2, rounded: what is subtracted here is added again by the join, to the bit
+      top = fmaxf(top, __shfl_xor(top, 32)) * LOG2E;
       const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum += exp_of(acc[i][t][r] - ref);
+        for (int r = 0; r < 16; ++r) sum += exp2_of(__builtin_fmaf(acc[i][t][r], LOG2E, -ref));
       sum += __shfl_xor(sum, 32);
       if (half == 0) red[wm * BN + wn * WROWS + 32 * t + l32] = float2{top, sum};
     }
@@ -400,29 +461,36 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
 #pragma unroll
         for (int w = 0; w < WM; ++w) {
           const float2 o = red[w * BN + c];
-          sum += o.x == -INFINITY ? o.y : o.y * exp_of(o.x - ref);
+          sum += o.x == -INFINITY ? o.y : o.y * exp2_of(o.x - ref);
         }
         g.stats[(int64_t)tile_m * g.N + n0 + c] = float2{top, sum};
       }
   } else if constexpr (E == E_GRAD) {
     constexpr int PARTS = std::is_same<O, float>::value ? 3 : 1;
+    using S = std::conditional_t<PARTS == 3, __bf16, T>;  // g as it is stored
     __syncthreads();
     char* stg = s_mem + wave * 32 * OUT_ROW;
-    typedef T v4 __attribute__((ext_vector_type(4)));
+    typedef S v4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int t = 0; t < TN; ++t) {
       const int n = nw + 32 * t;
       const bool row = n < g.N;
       const int lab = row ? (int)std::min<int64_t>(std::max<int64_t>(g.label[n], -1), g.V) - g.v0 : -1;
-      const float c = row ? g.coef[n] : 0.f, lse = row ? g.lse[n] : 0.f;
+      const float c = row ? g.coef[n] : 0.f, lse = row ? g.lse[n] * LOG2E : 0.f;
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int m = mw + 32 * i + 8 * (r / 4) + r % 4;
-          const float p = exp_of(acc[i][t][r] - lse) - (m == lab ? 1.f : 0.f);
-          acc[i][t][r] = c == 0.f || m >= g.M ? 0.f : c * p;
+          const float p = exp2_of(__builtin_fmaf(acc[i][t][r], LOG2E, -lse)) - (m == lab ? 1.f : 0.f);
+          acc[i][t][r] = c == 0.f ? 0.f : c * p;  // (a masked row's p may be anything)
         }
+      if (m0 + BM > g.M)  // the last tile: zeros past the vocabulary
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (mw + 32 * i + 8 * (r / 4) + r % 4 >= g.M) acc[i][t][r] = 0.f;
 #pragma unroll
       for (int part = 0; part < PARTS; ++part) {
 #pragma unroll
@@ -432,15 +500,15 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
             v4 o;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              o[e] = (T)acc[i][t][4 * q + e];
+              o[e] = (S)acc[i][t][4 * q + e];
               if (PARTS > 1) acc[i][t][4 * q + e] -= (float)o[e];
             }
             *(v4*)(stg + l32 * OUT_ROW + (32 * i + 8 * q + 4 * half) * 2) = o;
           }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         constexpr int LANES = WCOLS / 8, LINES = 64 / LANES;  // lanes of a row, rows of an instruction
-        typedef T v8 __attribute__((ext_vector_type(8)));
-        T* dst = (T*)g.g + part * g.g_part + m0 + wm * WCOLS + (lane % LANES) * 8;
+        typedef S v8 __attribute__((ext_vector_type(8)));
+        S* dst = (S*)g.g + part * g.g_part + m0 + wm * WCOLS + (lane % LANES) * 8;
 #pragma unroll
         for (int k = 0; k < 32 / LINES; ++k) {
           const int rr = k * LINES + lane / LANES, nn = n0 + wn * WROWS + 32 * t + rr;
@@ -495,7 +563,7 @@ __global__ __launch_bounds__(256) void join_stats_kernel(const float2* __restric
   float top = -INFINITY, sum = 0.f;
   auto add = [&](float2 o) {  // (-inf, 0) adds nothing; a NaN sum stays
     const float m = fmaxf(top, o.x), ref = m == -INFINITY ? 0.f : m;
-    sum = (top == -INFINITY ? sum : sum * exp_of(top - ref)) + (o.x == -INFINITY ? o.y : o.y * exp_of(o.x - ref));
+    sum = (top == -INFINITY ? sum : sum * exp2_of(top - ref)) + (o.x == -INFINITY ? o.y : o.y * exp2_of(o.x - ref));
     top = m;
   };
   if (row < n)
@@ -509,7 +577,7 @@ __global__ __launch_bounds__(256) void join_stats_kernel(const float2* __restric
     for (int w = 1; w < 4; ++w) add(s_red[w][threadIdx.x]);
     const int64_t l = label[row];
     const bool has = l >= 0 && l < V;
-    const float z = logf(sum) + top;
+    const float z = (log2f(sum) + top) * LN2;
     lse[row] = has ? z : 0.f;
     loss[row] = has ? z - at[row] : 0.f;
   }
@@ -528,18 +596,18 @@ __global__ __launch_bounds__(1024) void join_logits_kernel(const float* __restri
     for (int s = 0; s < splits; ++s) x += slab[s * stride + row * ld + v];
     if (v == l) s_at = x;
     const float m = fmaxf(top, x), ref = m == -INFINITY ? 0.f : m;
-    sum = (top == -INFINITY ? sum : sum * exp_of(top - ref)) + exp_of(x - ref);
+    sum = (top == -INFINITY ? sum : sum * exp2_of((top - ref) * LOG2E)) + exp2_of((x - ref) * LOG2E);
     top = m;
   }
   const float all = lanes_max<64>(top), ref = all == -INFINITY ? 0.f : all;
-  sum = lanes_sum<64>(top == -INFINITY ? sum : sum * exp_of(top - ref));
+  sum = lanes_sum<64>(top == -INFINITY ? sum : sum * exp2_of((top - ref) * LOG2E));
   if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = all, s_sum[threadIdx.x >> 6] = sum;
   __syncthreads();
   if (threadIdx.x == 0) {
     float m = s_top[0], z = 0.f;
     for (int w = 1; w < 16; ++w) m = fmaxf(m, s_top[w]);
     const float mr = m == -INFINITY ? 0.f : m;
-    for (int w = 0; w < 16; ++w) z += s_top[w] == -INFINITY ? s_sum[w] : s_sum[w] * exp_of(s_top[w] - mr);
+    for (int w = 0; w < 16; ++w) z += s_top[w] == -INFINITY ? s_sum[w] : s_sum[w] * exp2_of((s_top[w] - mr) * LOG2E);
     const bool has = l >= 0 && l < V;
     z = logf(z) + m;
     lse[row] = has ? z : 0.f;
@@ -614,6 +682,65 @@ __global__ __launch_bounds__(256) void pack_kernel(const T* __restrict__ in, int
     } else {
       store8((T*)out + row * ldo + c, v);
     }
+  }
+}
+
+// fp32 rows at any alignment as aligned ones of ldo elements, zeros past column C.
+__global__ __launch_bounds__(256) void copy_rows_kernel(const float* __restrict__ in, int64_t ld, int64_t rows, int C,
+                                                        float* __restrict__ out, int64_t ldo) {
+  const int64_t per = ldo / 4, total = rows * per;
+  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
+    const int64_t row = u / per;
+    const int c = (int)(u - row * per) * 4;
+    f32x4 v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = c + j < C ? in[row * ld + c + j] : 0.f;
+    *(f32x4*)(out + row * ldo + c) = v;
+  }
+}
+
+// fp32 rows as two fp16 parts [2][rows][ldo] of x 2^k and a factor 2^-k, one workgroup per row.  Rows whose label is outside
+// [0, V) become 0 (label may be null).  A row that is not finite keeps k = 0 and so its infinities and NaN.
+__global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict__ in, int64_t ld, int C, _Float16* __restrict__ out,
+                                                         int64_t ldo, int64_t part, float* __restrict__ factor,
+                                                         const int64_t* __restrict__ label, int V) {
+  __shared__ float s_top[4];
+  const int64_t row = blockIdx.x;
+  const float* x = in + row * ld;
+  const bool zero = label && !(label[row] >= 0 && label[row] < V);
+  float top = 0.f, first[8];
+  for (int c = threadIdx.x * 8; c < ldo; c += 2048) {
+    float v[8];
+    load8(x, c, C, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[j]));
+    if (c == (int)threadIdx.x * 8)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) first[j] = v[j];
+  }
+  top = lanes_max<64>(top);
+  if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+  int k = 0;
+  if (!zero && top > 0.f && top < INFINITY) k = 13 - max(ilogbf(top), -100);
+  const float mul = ldexpf(1.f, k);
+  if (threadIdx.x == 0) factor[row] = ldexpf(1.f, -k);
+  for (int c = threadIdx.x * 8; c < ldo; c += 2048) {
+    float v[8], lo[8];
+    if (c == (int)threadIdx.x * 8) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = first[j];
+    } else {
+      load8(x, c, C, v);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      v[j] = zero ? 0.f : v[j] * mul;
+      lo[j] = v[j] - (float)(_Float16)v[j];
+    }
+    store8(out + row * ldo + c, v);
+    store8(out + part + row * ldo + c, lo);
   }
 }
 
@@ -698,23 +825,33 @@ void choose(const Tile* of, int n_tiles, int64_t M, int64_t N, int64_t stages, b
       if (us < best * 0.999) best = us, tile = of[i], splits = s;
     }
 }
-int64_t stages_of(int64_t k, int parts) { return (k + BK - 1) / BK * (parts == 3 ? 6 : 1); }
+int64_t stages_of(int64_t k, int products) { return (k + BK - 1) / BK * products; }
 
-struct Plan {
-  bool pack_h, pack_w;
-  int parts;
-  int64_t ldp;  // row length of packed operands
-  size_t h_at, w_at;
+// An operand as a product reads it: 16-bit elements (or fp32 ones, two for each) from p on, rows ld apart, `part` between
+// its parts, a factor for each row.
+struct Matrix {
+  const void* p;
+  int64_t ld, part;
+  const float* factor;
 };
-Plan plan_operands(const LossArgs& a, dn_dtype dt, bool backward, Work& w) {
-  Plan p{};
-  p.parts = dt == DN_F32 ? 3 : 1;
-  p.ldp = up(a.C, 8);
-  p.pack_h = backward || !lies_well(a.h, a.h_stride, a.C, dt);
-  p.pack_w = !lies_well(a.w, a.w_stride, a.C, dt);
-  if (p.pack_h) p.h_at = w.take((size_t)p.parts * a.n * p.ldp * 2);
-  if (p.pack_w) p.w_at = w.take((size_t)p.parts * a.V * p.ldp * 2);
-  return p;
+// How operands are laid out for products: as they lie (16-bit types; fp32 where `wide`), as three bf16 or two fp16 parts.
+enum Layout { AS_IS, WIDE, THREE, TWO };
+struct Pack {
+  bool copy;       // laid out in the workspace
+  Layout how;
+  int64_t rows, ld;  // elements of a row there
+  size_t at, factor_at;
+};
+Pack plan_pack(const void* p, int64_t ld, int64_t rows, int32_t C, dn_dtype dt, Layout how, bool always, Work& w) {
+  Pack k{};
+  k.how = how, k.rows = rows, k.ld = how == WIDE ? up(C, 4) * 2 : up(C, 8);
+  if (how == AS_IS) k.copy = always || !lies_well(p, ld, C, dt);
+  else if (how == WIDE) k.copy = always || (uintptr_t)p % 16 || ld % 4 || C % 4 || 2 * ld > MAX_LD;
+  else k.copy = true;
+  const int parts = how == THREE ? 3 : how == TWO ? 2 : 1;
+  if (k.copy) k.at = w.take((size_t)parts * rows * k.ld * 2);
+  if (how == TWO) k.factor_at = w.take((size_t)rows * 4);
+  return k;
 }
 
 template <typename T>
@@ -740,16 +877,21 @@ int run_gemm(GemmArgs& g, hipStream_t st) {
 }
 template <typename T, bool AT, bool BT, Epilogue E, typename O>
 int run_tile(Tile t, GemmArgs& g, hipStream_t st) {
-  if (t == T256) return run_gemm<T, AT, BT, E, O, 256, 256, 2, 4, 2>(g, st);
+  if constexpr (!std::is_same<T, float>::value) {  // fp32 as it lies: few rows only
+    if (t == T256) return run_gemm<T, AT, BT, E, O, 256, 256, 2, 4, 2>(g, st);
+    if (t == T128) return run_gemm<T, AT, BT, E, O, 128, 128, 2, 2, 2>(g, st);
+  }
   if constexpr (!AT && !BT && (E == E_STATS || E == E_SLAB)) {
     if (t == T64) return run_gemm<T, AT, BT, E, O, 128, 64, 2, 2, 3>(g, st);
     if (t == T32) return run_gemm<T, AT, BT, E, O, 128, 32, 4, 1, 4>(g, st);
   }
-  return run_gemm<T, AT, BT, E, O, 128, 128, 2, 2, 2>(g, st);
+  return (int)hipErrorInvalidValue;  // no plan asks for another tile
 }
 
 struct FwdPlan {
-  Plan op;
+  Layout how;
+  Pack h, w;
+  int products;
   Tile tile;
   int splits;
   bool logits;  // partial logits in memory (few tiles) instead of tile statistics
@@ -759,9 +901,12 @@ struct FwdPlan {
 FwdPlan plan_forward(const LossArgs& a, dn_dtype dt) {
   FwdPlan f{};
   Work w;
-  f.op = plan_operands(a, dt, false, w);
+  f.how = dt != DN_F32 ? AS_IS : a.n <= 64 ? WIDE : TWO;
+  f.h = plan_pack(a.h, a.h_stride, a.n, a.C, dt, f.how, false, w);
+  f.w = plan_pack(a.w, a.w_stride, a.V, a.C, dt, f.how, false, w);
+  f.products = f.how == TWO ? 3 : 1;
   const Tile few[] = {a.n <= 32 ? T32 : T64}, many[] = {T256, T128};
-  choose(a.n <= 64 ? few : many, a.n <= 64 ? 1 : 2, a.V, a.n, stages_of(f.op.ldp, f.op.parts), true, false, f.tile, f.splits);
+  choose(a.n <= 64 ? few : many, a.n <= 64 ? 1 : 2, a.V, a.n, stages_of(f.w.ld, f.products), true, false, f.tile, f.splits);
   f.tiles_m = (a.V + tile_m(f.tile) - 1) / tile_m(f.tile);
   f.logits = f.splits > 1;
   f.at_at = w.take((size_t)a.n * 4);
@@ -776,7 +921,10 @@ FwdPlan plan_forward(const LossArgs& a, dn_dtype dt) {
 }
 
 struct BackPlan {
-  Plan op;
+  Pack h, w;    // for dh and dw, and for the logits but where these have
+  Pack lh, lw;  // fp32 rows of two parts
+  bool two;
+  int parts, products;
   int64_t vc, ldg;  // words of a piece (a multiple of 256)
   Tile grad, dh, dw;
   int dh_splits, dw_splits;
@@ -785,10 +933,21 @@ struct BackPlan {
   size_t coef_at, unscale_at, g_at, dh_at, dw_at, total;
 };
 constexpr int64_t PIECE_BYTES = 1LL << 29;  // of one part of g
+// fp32: from this many rows on, a second layout of w for the logits (12 bytes a value) costs less than three of the six
+// products: 1001 rows x 1024 over 10007 words 16 us against 75.
+constexpr int64_t TWO_ROWS = 400;
 BackPlan plan_backward(const LossArgs& a, dn_dtype dt) {
   BackPlan b{};
   Work w;
-  b.op = plan_operands(a, dt, true, w);
+  const Layout how = dt == DN_F32 ? THREE : AS_IS;
+  b.parts = dt == DN_F32 ? 3 : 1, b.products = dt == DN_F32 ? 6 : 1;
+  b.h = plan_pack(a.h, a.h_stride, a.n, a.C, dt, how, true, w);  // always: masked rows become 0
+  b.w = plan_pack(a.w, a.w_stride, a.V, a.C, dt, how, false, w);
+  b.two = dt == DN_F32 && a.n >= TWO_ROWS;
+  if (b.two) {
+    b.lh = plan_pack(a.h, a.h_stride, a.n, a.C, dt, TWO, true, w);
+    b.lw = plan_pack(a.w, a.w_stride, a.V, a.C, dt, TWO, true, w);
+  }
   const int64_t v256 = up(a.V, 256);
   b.vc = std::min(v256, std::max<int64_t>(256, PIECE_BYTES / (2 * a.n) / 256 * 256));
   const int64_t pieces = (v256 + b.vc - 1) / b.vc;
@@ -797,55 +956,65 @@ BackPlan plan_backward(const LossArgs& a, dn_dtype dt) {
   const Tile any[] = {T256, T128};
   const int64_t words = std::min<int64_t>(b.vc, a.V);
   int one;
-  choose(any, 2, words, a.n, stages_of(b.op.ldp, b.op.parts), false, false, b.grad, one);
-  choose(any, 2, a.C, a.n, stages_of(words, b.op.parts), true, true, b.dh, b.dh_splits);
-  choose(any, 2, a.C, words, stages_of(a.n, b.op.parts), true, true, b.dw, b.dw_splits);
+  choose(any, 2, words, a.n, stages_of(b.w.ld, b.two ? 3 : b.products), false, false, b.grad, one);
+  choose(any, 2, a.C, a.n, stages_of(words, b.products), true, true, b.dh, b.dh_splits);
+  choose(any, 2, a.C, words, stages_of(a.n, b.products), true, true, b.dw, b.dw_splits);
   b.dh_slab = pieces > 1 || b.dh_splits > 1;
   b.dw_slab = b.dw_splits > 1;
   b.slab_ld = up(a.C, 256);
   b.coef_at = w.take((size_t)a.n * 4);
   b.unscale_at = w.take(4);
-  b.g_at = w.take((size_t)b.op.parts * a.n * b.ldg * 2);
+  b.g_at = w.take((size_t)b.parts * a.n * b.ldg * 2);
   if (b.dh_slab) b.dh_at = w.take((size_t)b.dh_splits * a.n * b.slab_ld * 4);
   if (b.dw_slab) b.dw_at = w.take((size_t)b.dw_splits * std::min<int64_t>(b.vc, a.V) * b.slab_ld * 4);
   b.total = w.total;
   return b;
 }
 
-struct Operands {
-  const void *h, *w;
-  int64_t ldh, ldw, h_part, w_part;
-};
-int lay_out(const LossArgs& a, dn_dtype dt, const Plan& p, char* work, bool mask, Operands& o, hipStream_t st) {
-  o = Operands{a.h, a.w, a.h_stride, a.w_stride, 0, 0};
-  int err = 0;
-  if (p.pack_h) {
-    o.h = work + p.h_at, o.ldh = p.ldp, o.h_part = a.n * p.ldp;
-    err = pack_any(dt, a.h, a.h_stride, a.n, a.C, work + p.h_at, p.ldp, mask ? a.label : nullptr, a.V, st);
+// Lays an operand out as planned; label: rows whose label is outside [0, V) become 0.
+int lay_out(const Pack& k, const void* p, int64_t ld, int32_t C, dn_dtype dt, const int64_t* label, int V, char* work, Matrix& m,
+            hipStream_t st) {
+  m = Matrix{p, k.how == WIDE ? 2 * ld : ld, 0, nullptr};
+  if (!k.copy) return 0;
+  m.p = work + k.at, m.ld = k.ld, m.part = k.rows * k.ld;
+  if (k.how == TWO) {
+    m.factor = (const float*)(work + k.factor_at);
+    split_rows_kernel<<<dim3((unsigned)k.rows), 256, 0, st>>>((const float*)p, ld, C, (_Float16*)m.p, k.ld, m.part, (float*)m.factor,
+                                                             label, V);
+    return (int)hipGetLastError();
   }
-  if (p.pack_w && !err) {
-    o.w = work + p.w_at, o.ldw = p.ldp, o.w_part = (int64_t)a.V * p.ldp;
-    err = pack_any(dt, a.w, a.w_stride, a.V, a.C, work + p.w_at, p.ldp, nullptr, 0, st);
+  if (k.how == WIDE) {
+    const unsigned grid = (unsigned)std::min<int64_t>((k.rows * (k.ld / 8) + 255) / 256, 8192);
+    copy_rows_kernel<<<grid, 256, 0, st>>>((const float*)p, ld, k.rows, C, (float*)m.p, k.ld / 2);
+    return (int)hipGetLastError();
   }
-  return err;
+  return pack_any(dt, p, ld, k.rows, C, (void*)m.p, k.ld, label, V, st);
 }
 
-template <typename T>
-int forward(const LossArgs& a, const FwdPlan& f, const Operands& o, char* work, hipStream_t st) {
+void set_operands(GemmArgs& g, const Matrix& a, int a_rows, const Matrix& b, int b_rows) {
+  g.a = a.p, g.lda = a.ld, g.a_part = a.part, g.a_rows = a_rows, g.a_factor = a.factor;
+  g.b = b.p, g.ldb = b.ld, g.b_part = b.part, g.b_rows = b_rows, g.b_factor = b.factor;
+}
+
+// T: type of the products' operands; O: of h and w.
+template <typename T, typename O>
+int forward(const LossArgs& a, dn_dtype dt, const FwdPlan& f, char* work, hipStream_t st) {
+  Matrix h, w;
+  int err;
+  if ((err = lay_out(f.h, a.h, a.h_stride, a.C, dt, nullptr, 0, work, h, st))) return err;
+  if ((err = lay_out(f.w, a.w, a.w_stride, a.C, dt, nullptr, 0, work, w, st))) return err;
   GemmArgs g{};
-  g.a = o.w, g.lda = o.ldw, g.a_part = o.w_part, g.a_rows = a.V;
-  g.b = o.h, g.ldb = o.ldh, g.b_part = o.h_part, g.b_rows = (int)a.n;
-  g.M = a.V, g.N = (int)a.n, g.K = (int)f.op.ldp, g.products = f.op.parts == 3 ? 6 : 1, g.splits = f.splits;
+  set_operands(g, w, a.V, h, (int)a.n);
+  g.M = a.V, g.N = (int)a.n, g.K = (int)f.w.ld, g.products = f.products, g.splits = f.splits;
   g.label = a.label, g.V = a.V;
   g.at = (float*)(work + f.at_at);
-  int err;
   if (f.logits) {
     g.slab = (float*)(work + f.slab_at), g.slab_ld = f.ld, g.slab_stride = a.n * f.ld;
-    if ((err = run_tile<T, false, false, E_SLAB, T>(f.tile, g, st))) return err;
+    if ((err = run_tile<T, false, false, E_SLAB, O>(f.tile, g, st))) return err;
     join_logits_kernel<<<dim3((unsigned)a.n), 1024, 0, st>>>(g.slab, f.ld, g.slab_stride, f.splits, a.label, a.V, a.loss, a.lse);
   } else {
     g.stats = (float2*)(work + f.stats_at);
-    if ((err = run_tile<T, false, false, E_STATS, T>(f.tile, g, st))) return err;
+    if ((err = run_tile<T, false, false, E_STATS, O>(f.tile, g, st))) return err;
     if (a.n <= 64)
       join_stats_kernel<1><<<dim3((unsigned)a.n), 256, 0, st>>>(g.stats, g.at, a.label, g.tiles_m, (int)a.n, a.V, a.loss, a.lse);
     else
@@ -857,29 +1026,41 @@ int forward(const LossArgs& a, const FwdPlan& f, const Operands& o, char* work, 
 
 // T: type of the products' operands; O: of the results (float where T holds fp32's parts).
 template <typename T, typename O>
-int backward(const LossArgs& a, const BackPlan& b, const Operands& o, char* work, float boost, hipStream_t st) {
+int backward(const LossArgs& a, dn_dtype dt, const BackPlan& b, char* work, float boost, hipStream_t st) {
+  Matrix h, w, lh, lw;
+  int err;
+  if ((err = lay_out(b.h, a.h, a.h_stride, a.C, dt, a.label, a.V, work, h, st))) return err;
+  if ((err = lay_out(b.w, a.w, a.w_stride, a.C, dt, nullptr, 0, work, w, st))) return err;
+  if (b.two) {
+    if ((err = lay_out(b.lh, a.h, a.h_stride, a.C, dt, a.label, a.V, work, lh, st))) return err;
+    if ((err = lay_out(b.lw, a.w, a.w_stride, a.C, dt, nullptr, 0, work, lw, st))) return err;
+  }
   float* coef = (float*)(work + b.coef_at);
   float* unscale = (float*)(work + b.unscale_at);
   coef_kernel<<<1, 1024, 0, st>>>(a.label, a.dloss, a.n, a.V, a.scale, boost, coef, unscale);
-  int err = (int)hipGetLastError();
-  if (err) return err;
-  const int products = b.op.parts == 3 ? 6 : 1;
-  const int64_t g_part = a.n * b.ldg;
+  if ((err = (int)hipGetLastError())) return err;
+  Matrix gm{work + b.g_at, b.ldg, a.n * b.ldg, nullptr};
   for (int64_t v0 = 0; v0 < a.V; v0 += b.vc) {
     const int vc = (int)std::min<int64_t>(b.vc, a.V - v0);
-    const char* w = (const char*)o.w + v0 * o.ldw * 2;
+    const auto piece = [&](Matrix m) {  // rows v0 on
+      m.p = (const char*)m.p + v0 * m.ld * 2;
+      if (m.factor) m.factor += v0;
+      return m;
+    };
     GemmArgs g{};  // the piece's logits, leaving as g
-    g.a = w, g.lda = o.ldw, g.a_part = o.w_part, g.a_rows = vc;
-    g.b = o.h, g.ldb = o.ldh, g.b_part = o.h_part, g.b_rows = (int)a.n;
-    g.M = vc, g.N = (int)a.n, g.K = (int)b.op.ldp, g.products = products, g.splits = 1;
+    set_operands(g, piece(b.two ? lw : w), vc, b.two ? lh : h, (int)a.n);
+    g.M = vc, g.N = (int)a.n, g.K = (int)b.w.ld, g.products = b.two ? 3 : b.products, g.splits = 1;
     g.label = a.label, g.v0 = (int)v0, g.V = a.V, g.lse = a.lse_in, g.coef = coef;
-    g.g = work + b.g_at, g.ldg = b.ldg, g.g_part = g_part;
-    if ((err = run_tile<T, false, false, E_GRAD, O>(b.grad, g, st))) return err;
+    g.g = work + b.g_at, g.ldg = b.ldg, g.g_part = gm.part;
+    if constexpr (std::is_same<O, float>::value)
+      err = b.two ? run_tile<_Float16, false, false, E_GRAD, O>(b.grad, g, st) : run_tile<T, false, false, E_GRAD, O>(b.grad, g, st);
+    else
+      err = run_tile<T, false, false, E_GRAD, O>(b.grad, g, st);
+    if (err) return err;
 
     GemmArgs d{};  // dh += g w
-    d.a = w, d.lda = o.ldw, d.a_part = o.w_part, d.a_rows = (int)b.op.ldp;
-    d.b = g.g, d.ldb = b.ldg, d.b_part = g_part, d.b_rows = (int)a.n;
-    d.M = a.C, d.N = (int)a.n, d.K = vc, d.products = products, d.splits = b.dh_splits;
+    set_operands(d, piece(w), (int)b.w.ld, gm, (int)a.n);
+    d.M = a.C, d.N = (int)a.n, d.K = vc, d.products = b.products, d.splits = b.dh_splits;
     d.unscale = unscale;
     if (b.dh_slab) {
       d.slab = (float*)(work + b.dh_at), d.slab_ld = b.slab_ld, d.slab_stride = a.n * b.slab_ld, d.accumulate = v0 > 0;
@@ -892,9 +1073,8 @@ int backward(const LossArgs& a, const BackPlan& b, const Operands& o, char* work
     if (err) return err;
 
     GemmArgs e{};  // dw = g^T h
-    e.a = o.h, e.lda = o.ldh, e.a_part = o.h_part, e.a_rows = (int)b.op.ldp;
-    e.b = g.g, e.ldb = b.ldg, e.b_part = g_part, e.b_rows = (int)up(vc, 8);
-    e.M = a.C, e.N = vc, e.K = (int)a.n, e.products = products, e.splits = b.dw_splits;
+    set_operands(e, h, (int)b.h.ld, gm, (int)up(vc, 8));
+    e.M = a.C, e.N = vc, e.K = (int)a.n, e.products = b.products, e.splits = b.dw_splits;
     e.unscale = unscale;
     O* dw = (O*)a.dw + v0 * a.dw_stride;
     if (b.dw_slab) {
@@ -928,9 +1108,10 @@ size_t softmax_loss_backward_bytes(const LossArgs& a, dn_dtype dt) { return a.n 
 int launch_softmax_loss(const LossArgs& a, dn_dtype dt, void* d_work, void* stream) {
   const FwdPlan f = plan_forward(a, dt);
   const hipStream_t st = (hipStream_t)stream;
-  Operands o;
-  if (const int err = lay_out(a, dt, f.op, (char*)d_work, false, o, st)) return err;
-  return dt == DN_F16 ? forward<_Float16>(a, f, o, (char*)d_work, st) : forward<__bf16>(a, f, o, (char*)d_work, st);
+  if (f.how == WIDE) return forward<float, float>(a, dt, f, (char*)d_work, st);
+  if (f.how == TWO) return forward<_Float16, float>(a, dt, f, (char*)d_work, st);
+  if (dt == DN_F16) return forward<_Float16, _Float16>(a, dt, f, (char*)d_work, st);
+  return forward<__bf16, __bf16>(a, dt, f, (char*)d_work, st);
 }
 
 int launch_softmax_loss_backward(const LossArgs& a, dn_dtype dt, void* d_work, void* stream) {
@@ -944,11 +1125,9 @@ int launch_softmax_loss_backward(const LossArgs& a, dn_dtype dt, void* d_work, v
   }
   const BackPlan b = plan_backward(a, dt);
   const hipStream_t st = (hipStream_t)stream;
-  Operands o;
-  if (const int err = lay_out(a, dt, b.op, (char*)d_work, true, o, st)) return err;
-  if (dt == DN_F32) return backward<__bf16, float>(a, b, o, (char*)d_work, 1.f, st);
-  if (dt == DN_F16) return backward<_Float16, _Float16>(a, b, o, (char*)d_work, 1024.f, st);
-  return backward<__bf16, __bf16>(a, b, o, (char*)d_work, 1.f, st);
+  if (dt == DN_F32) return backward<__bf16, float>(a, dt, b, (char*)d_work, 1.f, st);
+  if (dt == DN_F16) return backward<_Float16, _Float16>(a, dt, b, (char*)d_work, 1024.f, st);
+  return backward<__bf16, __bf16>(a, dt, b, (char*)d_work, 1.f, st);
 }
 
 }  // namespace head
