@@ -388,7 +388,7 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
   // fp32's logits from two fp16 parts: the rows' factors
   if constexpr ((E == E_STATS || E == E_GRAD || E == E_SLAB) && !AT && std::is_same<T, _Float16>::value && std::is_same<O, float>::value) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < TM; ++i) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int m = mw + 32 * i + 8 * q;
@@ -404,6 +404,8 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[i][t][4 * q + e] *= f[e];
       }
+      __builtin_amdgcn_sched_barrier(0);  // 16 factors at a time: the registers are full of sums
+    }
 #pragma unroll
     for (int t = 0; t < TN; ++t) {
       const float f = nw + 32 * t < g.N ? g.b_factor[nw + 32 * t] : 0.f;
@@ -504,16 +506,17 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
               if (PARTS > 1) acc[i][t][4 * q + e] -= (float)o[e];
             }
             *(v4*)(stg + l32 * OUT_ROW + (32 * i + 8 * q + 4 * half) * 2) = o;
-          }
+            }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         constexpr int LANES = WCOLS / 8, LINES = 64 / LANES;  // lanes of a row, rows of an instruction
         typedef S v8 __attribute__((ext_vector_type(8)));
-        S* dst = (S*)g.g + part * g.g_part + m0 + wm * WCOLS + (lane % LANES) * 8;
+        int nn = n0 + wn * WROWS + 32 * t + lane / LANES;
+        S* dst = (S*)g.g + part * g.g_part + m0 + wm * WCOLS + (lane % LANES) * 8 + nn * g.ldg;
 #pragma unroll
         for (int k = 0; k < 32 / LINES; ++k) {
-          const int rr = k * LINES + lane / LANES, nn = n0 + wn * WROWS + 32 * t + rr;
-          const v8 o = *(const v8*)(stg + rr * OUT_ROW + (lane % LANES) * 16);
-          if (nn < g.N) __builtin_nontemporal_store(o, (v8*)(dst + nn * g.ldg));  // read by later launches only
+          const v8 o = *(const v8*)(stg + (k * LINES + lane / LANES) * OUT_ROW + (lane % LANES) * 16);
+          if (nn < g.N) __builtin_nontemporal_store(o, (v8*)dst);  // read by later launches only
+          nn += LINES, dst += LINES * g.ldg;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
@@ -877,8 +880,12 @@ int run_gemm(GemmArgs& g, hipStream_t st) {
 }
 template <typename T, bool AT, bool BT, Epilogue E, typename O>
 int run_tile(Tile t, GemmArgs& g, hipStream_t st) {
-  if constexpr (!std::is_same<T, float>::value) {  // fp32 as it lies: few rows only
+  // fp32 as it lies: few rows only.  Its g, which leaves as three parts: T256's registers do not hold that (1001 rows over 10007
+  // words: 116 us, T128 99).
+  constexpr bool wide = std::is_same<T, float>::value, parts_out = E == E_GRAD && std::is_same<O, float>::value;
+  if constexpr (!wide && !parts_out)
     if (t == T256) return run_gemm<T, AT, BT, E, O, 256, 256, 2, 4, 2>(g, st);
+  if constexpr (!wide) {
     if (t == T128) return run_gemm<T, AT, BT, E, O, 128, 128, 2, 2, 2>(g, st);
   }
   if constexpr (!AT && !BT && (E == E_STATS || E == E_SLAB)) {
@@ -956,7 +963,8 @@ BackPlan plan_backward(const LossArgs& a, dn_dtype dt) {
   const Tile any[] = {T256, T128};
   const int64_t words = std::min<int64_t>(b.vc, a.V);
   int one;
-  choose(any, 2, words, a.n, stages_of(b.w.ld, b.two ? 3 : b.products), false, false, b.grad, one);
+  const int from = dt == DN_F32 ? 1 : 0;  // fp32: T128 (see run_tile)
+  choose(any + from, 2 - from, words, a.n, stages_of(b.w.ld, b.two ? 3 : b.products), false, false, b.grad, one);
   choose(any, 2, a.C, a.n, stages_of(words, b.products), true, true, b.dh, b.dh_splits);
   choose(any, 2, a.C, words, stages_of(a.n, b.products), true, true, b.dw, b.dw_splits);
   b.dh_slab = pieces > 1 || b.dh_splits > 1;
