@@ -492,3 +492,67 @@ def test_region_head_learns(D, dt, bits):
     codes, scale = head.store(desc)
     y = a / (a.square().mean(1, keepdim=True) + 1e-6).sqrt() * head.gamma.double()
     within(codes.double() * scale.double(), y, (2.0 ** -4 + 1e-3) * y.abs() + scale.double() * 2.0 ** -9, "stored")
+
+
+def test_step_in_a_graph(D):
+    """A training step's calls captured in a graph: every replay, with other work between, gives what eager calls give."""
+    n, C, V = 130, 264, 1000
+    g = gen(8)
+    x, r = torch.empty(n, C, device="cuda"), torch.empty(n, C, device="cuda")
+    w, labels = rows(g, V, C, "bf16", 0, 0.1), torch.randint(-1, V, (n,), generator=g, device="cuda")
+    gamma = torch.ones(C, device="cuda")
+
+    def step(plans):
+        y, s, _ = D.densenet_rms_norm(x, gamma, residual=r, out_dtype=D.DN_BF16)
+        loss, lse = D.densenet_softmax_loss(y, w, labels)
+        dy, dw = D.densenet_softmax_loss_backward(y, w, labels, lse, dw=plans[0].grads[0])
+        dx, _ = D.densenet_rms_norm_backward(dy, s, gamma, dgamma=plans[1].grads[0])
+        for p in plans:
+            D.densenet_adamw(p, lr=1e-3, step=1, seed=3)
+        return loss, dx, dw
+    make = lambda: (D.AdamWPlan([w.clone()], [torch.zeros_like(w)], state_bits=8), D.AdamWPlan([gamma.clone()], [torch.zeros_like(gamma)]))  # noqa: E731
+    plans, eager = make(), make()
+    x.normal_(generator=g), r.normal_(generator=g)
+    step(make())  # warm up outside the capture
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(plans)
+    for _ in range(4):
+        x.normal_(generator=g), r.normal_(generator=g)
+        graph.replay()
+        want = step(eager)
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
+        for p, q in zip(plans, eager):
+            assert torch.equal(p.params[0], q.params[0]) and torch.equal(p.m.view(torch.uint8), q.m.view(torch.uint8))
+
+
+def test_loss_past_32_bit_offsets(D):
+    """Weights of more than 2^31 values: the words at the end count, and get their gradient, like those at the start."""
+    n, C, V = 3, 8200, 262144
+    assert V * C > 2 ** 31
+    g = gen(4)
+    h = torch.randn(n, C, generator=g, device="cuda").bfloat16()
+    w = torch.empty(V, C, device="cuda", dtype=torch.bfloat16)
+    for part in w.split(16384):
+        part.copy_(torch.randn(part.shape, generator=g, device="cuda") * (2 / math.sqrt(C)))
+    labels = torch.tensor([V - 1, 5, V - 3], device="cuda")
+    loss, lse = D.densenet_softmax_loss(h, w, labels)
+    logits = torch.cat([h.double() @ part.double().T for part in w.split(16384)], 1)
+    err = sum_err(C) * max(float((h.double().abs() @ part.double().abs().T).max()) for part in w[:65536].split(16384)) * 1.1
+    want = torch.logsumexp(logits, 1)
+    bound = torch.full_like(want, 2 * err + 2.0 ** -21 * 32)
+    within(lse, want, bound, "lse")
+    within(loss, want - logits.gather(1, labels[:, None])[:, 0], 2 * bound, "loss")
+    dh, dw = D.densenet_softmax_loss_backward(h, w, labels, lse)
+    p = (logits - want[:, None]).exp()
+    p.scatter_add_(1, labels[:, None], -torch.ones_like(p[:, :1]))
+    p /= n
+    for rng in (slice(0, 50), slice(V - 50, V)):
+        ref, terms = p[:, rng].T @ h.double(), p[:, rng].abs().T @ h.double().abs()
+        within(dw[rng], ref, UNIT["bf16"] * ref.abs() * 1.01 + (UNIT["bf16"] + 4 * err + 1e-5) * terms, "dw")
+    ref = sum(p[:, i:i + 16384] @ w[i:i + 16384].double() for i in range(0, V, 16384))
+    terms = sum(p[:, i:i + 16384].abs() @ w[i:i + 16384].double().abs() for i in range(0, V, 16384))
+    within(dh, ref, UNIT["bf16"] * ref.abs() * 1.01 + (UNIT["bf16"] + 4 * err + sum_err(V)) * terms, "dh")
