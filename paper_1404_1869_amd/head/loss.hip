@@ -586,52 +586,73 @@ __global__ __launch_bounds__(256) void join_stats_kernel(const float2* __restric
   }
 }
 
-// The few-tiles forward pass: logits of a row as `splits` partial sums, one workgroup per row.
-__global__ __launch_bounds__(1024) void join_logits_kernel(const float* __restrict__ slab, int64_t ld, int64_t stride,
-                                                           int splits, const int64_t* __restrict__ label, int V,
-                                                           float* __restrict__ loss, float* __restrict__ lse) {
+// The few-tiles forward pass: logits of a row as `splits` partial sums; a workgroup per row, or (WAVE) a wave.
+template <bool WAVE>
+__global__ __launch_bounds__(WAVE ? 256 : 1024) void join_logits_kernel(const float* __restrict__ slab, int64_t ld, int64_t stride,
+                                                                        int splits, const int64_t* __restrict__ label, int64_t n, int V,
+                                                                        float* __restrict__ loss, float* __restrict__ lse) {
+  constexpr int TPR = WAVE ? 64 : 1024;
   __shared__ float s_top[16], s_sum[16];
-  __shared__ float s_at;
-  const int64_t row = blockIdx.x, l = label[row];
+  __shared__ float s_at[4];
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const int64_t row = (int64_t)blockIdx.x * (WAVE ? 4 : 1) + sub;
+  if (WAVE && row >= n) return;  // no barriers follow
+  const int64_t l = label[row];
   float top = -INFINITY, sum = 0.f;
-  for (int v = threadIdx.x; v < V; v += 1024) {
+  for (int v = t; v < V; v += TPR) {
     float x = 0.f;
+#pragma unroll 4
     for (int s = 0; s < splits; ++s) x += slab[s * stride + row * ld + v];
-    if (v == l) s_at = x;
+    if (v == l) s_at[sub] = x;
     const float m = fmaxf(top, x), ref = m == -INFINITY ? 0.f : m;
     sum = (top == -INFINITY ? sum : sum * exp2_of((top - ref) * LOG2E)) + exp2_of((x - ref) * LOG2E);
     top = m;
   }
-  const float all = lanes_max<64>(top), ref = all == -INFINITY ? 0.f : all;
-  sum = lanes_sum<64>(top == -INFINITY ? sum : sum * exp2_of((top - ref) * LOG2E));
-  if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = all, s_sum[threadIdx.x >> 6] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    float m = s_top[0], z = 0.f;
-    for (int w = 1; w < 16; ++w) m = fmaxf(m, s_top[w]);
-    const float mr = m == -INFINITY ? 0.f : m;
-    for (int w = 0; w < 16; ++w) z += s_top[w] == -INFINITY ? s_sum[w] : s_sum[w] * exp2_of((s_top[w] - mr) * LOG2E);
+  float m = lanes_max<64>(top);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float z = lanes_sum<64>(top == -INFINITY ? sum : sum * exp2_of((top - ref) * LOG2E));
+  if constexpr (WAVE) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // s_at is the wave's own
+  } else {
+    if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = m, s_sum[threadIdx.x >> 6] = z;
+    __syncthreads();
+  }
+  if (t == 0) {
+    if constexpr (!WAVE) {
+      m = s_top[0], z = 0.f;
+      for (int w = 1; w < 16; ++w) m = fmaxf(m, s_top[w]);
+      const float mr = m == -INFINITY ? 0.f : m;
+      for (int w = 0; w < 16; ++w) z += s_top[w] == -INFINITY ? s_sum[w] : s_sum[w] * exp2_of((s_top[w] - mr) * LOG2E);
+    }
     const bool has = l >= 0 && l < V;
     z = logf(z) + m;
     lse[row] = has ? z : 0.f;
-    loss[row] = has ? z - s_at : 0.f;
+    loss[row] = has ? z - s_at[sub] : 0.f;
   }
 }
 
 // A row's part in the gradient, coef[n], and the factor that is left for the end, *unscale.  Without dloss every unmasked
 // row counts 1 and unscale is scale / (their number).  With it the rows keep dloss / 2^e in (-2, 2) for the largest
 // finite |dloss| in [2^e, 2^(e + 1)).  boost: a power of two that moves fp16's g away from its smallest values.
-__global__ __launch_bounds__(1024) void coef_kernel(const int64_t* __restrict__ label, const float* __restrict__ dloss, int64_t n,
-                                                    int V, float scale, float boost, float* __restrict__ coef,
-                                                    float* __restrict__ unscale) {
+__global__ __launch_bounds__(1024) void weight_kernel(const int64_t* __restrict__ label, const float* __restrict__ dloss, int64_t n,
+                                                      int V, float scale, float boost, float* __restrict__ mul,
+                                                      float* __restrict__ unscale) {
   __shared__ float s_red[16];
-  __shared__ float s_mul;
   float v = 0.f;
-#pragma unroll 8
-  for (int64_t i = threadIdx.x; i < n; i += 1024) {
-    const bool has = label[i] >= 0 && label[i] < V;
-    const float d = has ? (dloss ? fabsf(dloss[i]) : 1.f) : 0.f;
-    v = dloss ? (d < INFINITY ? fmaxf(v, d) : v) : v + d;
+  for (int64_t i0 = threadIdx.x; i0 < n; i0 += 8 * 1024) {
+    int64_t l[8];
+    float d[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {  // eight loads at a time
+      const int64_t i = i0 + k * 1024;
+      l[k] = i < n ? label[i] : -1;
+      d[k] = dloss && i < n ? fabsf(dloss[i]) : 1.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (!(l[k] >= 0 && l[k] < V)) d[k] = 0.f;
+      v = dloss ? (d[k] < INFINITY ? fmaxf(v, d[k]) : v) : v + d[k];
+    }
   }
   v = dloss ? lanes_max<64>(v) : lanes_sum<64>(v);
   if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = v;
@@ -642,19 +663,20 @@ __global__ __launch_bounds__(1024) void coef_kernel(const int64_t* __restrict__ 
     if (dloss) {
       int e = v > 0.f ? ilogbf(v) : 0;
       e = e < -100 ? -100 : e > 100 ? 100 : e;
-      s_mul = ldexpf(boost, -e);
+      *mul = ldexpf(boost, -e);
       *unscale = scale * ldexpf(1.f / boost, e);
     } else {
-      s_mul = boost;
+      *mul = boost;
       *unscale = v > 0.f ? scale / (v * boost) : 0.f;
     }
   }
-  __syncthreads();
-#pragma unroll 8
-  for (int64_t i = threadIdx.x; i < n; i += 1024) {
-    const bool has = label[i] >= 0 && label[i] < V;
-    coef[i] = has ? (dloss ? dloss[i] : 1.f) * s_mul : 0.f;
-  }
+}
+__global__ __launch_bounds__(256) void coef_kernel(const int64_t* __restrict__ label, const float* __restrict__ dloss, int64_t n, int V,
+                                                   const float* __restrict__ mul, float* __restrict__ coef) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const bool has = label[i] >= 0 && label[i] < V;
+  coef[i] = has ? (dloss ? dloss[i] : 1.f) * *mul : 0.f;
 }
 
 // Copies an operand into aligned rows of ldo elements (a multiple of 8), zeros past column C, as one 16-bit part or fp32's
@@ -799,10 +821,11 @@ bool lies_well(const void* p, int64_t ld, int32_t C, dn_dtype dt) {
 }
 
 // Tile shapes: T256 (8 waves, a workgroup per CU), T128 (4 waves, two per CU), and for the logits of few rows T64 and T32
-// (128 words x 64 or 32 rows).
-enum Tile { T256, T128, T64, T32 };
-int tile_m(Tile t) { return t == T256 ? 256 : 128; }
-int tile_n(Tile t) { return t == T256 ? 256 : t == T128 ? 128 : t == T64 ? 64 : 32; }
+// (128 words x 64 or 32 rows), of few words W64 and W32 (64 or 32 words x 128 rows).
+enum Tile { T256, T128, T64, T32, W64, W32 };
+int tile_m(Tile t) { return t == T256 ? 256 : t == W64 ? 64 : t == W32 ? 32 : 128; }
+int tile_n(Tile t) { return t == T256 ? 256 : t == T64 ? 64 : t == T32 ? 32 : 128; }
+constexpr int FEW = 64;  // rows or words that these are for
 
 // The time of a product [M][N] over `stages` of 64 k in us, by what launches of many shapes took: a stage of T256 takes 1.25
 // us on an idle chip and 1.75 on a full one, of T128 0.62 alone on a CU and 1.1 (turned operands: 1.2) for two, and a
@@ -815,9 +838,16 @@ double product_us(Tile t, int64_t M, int64_t N, int64_t stages, int splits, bool
     us = per_cu * (st * (1.25 + 0.5 * std::min(1.0, tiles / 256.0)) + 10);
   else if (t == T128)
     us = tiles <= 256 ? st * (0.62 + 0.25 * tiles / 256.0) + 5 : per_cu / 2 * (st * (turned ? 1.2 : 1.1) + 6);
-  else  // at least the time that reading M x k takes
-    us = std::max(tiles <= 256 ? st * 0.5 + 4 : per_cu / 2 * (st * 0.6 + 4), (double)M * stages * 128 / 5e6);
+  else  // at least the time that reading the long operand takes
+    us = std::max(tiles <= 256 ? st * 0.5 + 4 : per_cu / 2 * (st * 0.6 + 4), (double)std::max(M, N) * stages * 128 / 5e6);
   return us + (splits > 1 ? 5 + (double)splits * M * N * 8 / 5e6 : 0);
+}
+// The only tile for the logits of few rows or words, or the number of those to choose from.
+int logit_tiles(int64_t V, int64_t n, Tile (&of)[2]) {
+  of[0] = T256, of[1] = T128;
+  if (n > FEW && V > FEW) return 2;
+  of[0] = V <= 32 && n > 32 ? W32 : n <= 32 ? T32 : n <= FEW ? T64 : W64;
+  return 1;
 }
 // The tile and the splits with the least time (splits of at least 4 stages; one split unless `split`).
 void choose(const Tile* of, int n_tiles, int64_t M, int64_t N, int64_t stages, bool split, bool turned, Tile& tile, int& splits) {
@@ -888,9 +918,12 @@ int run_tile(Tile t, GemmArgs& g, hipStream_t st) {
   if constexpr (!wide) {
     if (t == T128) return run_gemm<T, AT, BT, E, O, 128, 128, 2, 2, 2>(g, st);
   }
-  if constexpr (!AT && !BT && (E == E_STATS || E == E_SLAB)) {
+  // fp32's g comes from fp32 as it lies or from parts
+  if constexpr (!AT && !BT && !(parts_out && !wide)) {
     if (t == T64) return run_gemm<T, AT, BT, E, O, 128, 64, 2, 2, 3>(g, st);
     if (t == T32) return run_gemm<T, AT, BT, E, O, 128, 32, 4, 1, 4>(g, st);
+    if (t == W64) return run_gemm<T, AT, BT, E, O, 64, 128, 1, 4, 3>(g, st);
+    if (t == W32) return run_gemm<T, AT, BT, E, O, 32, 128, 1, 4, 4>(g, st);
   }
   return (int)hipErrorInvalidValue;  // no plan asks for another tile
 }
@@ -908,12 +941,13 @@ struct FwdPlan {
 FwdPlan plan_forward(const LossArgs& a, dn_dtype dt) {
   FwdPlan f{};
   Work w;
-  f.how = dt != DN_F32 ? AS_IS : a.n <= 64 ? WIDE : TWO;
+  f.how = dt != DN_F32 ? AS_IS : a.n <= FEW || a.V <= FEW ? WIDE : TWO;
   f.h = plan_pack(a.h, a.h_stride, a.n, a.C, dt, f.how, false, w);
   f.w = plan_pack(a.w, a.w_stride, a.V, a.C, dt, f.how, false, w);
   f.products = f.how == TWO ? 3 : 1;
-  const Tile few[] = {a.n <= 32 ? T32 : T64}, many[] = {T256, T128};
-  choose(a.n <= 64 ? few : many, a.n <= 64 ? 1 : 2, a.V, a.n, stages_of(f.w.ld, f.products), true, false, f.tile, f.splits);
+  Tile of[2];
+  const int tiles = logit_tiles(a.V, a.n, of);
+  choose(of, tiles, a.V, a.n, stages_of(f.w.ld, f.products), true, false, f.tile, f.splits);
   f.tiles_m = (a.V + tile_m(f.tile) - 1) / tile_m(f.tile);
   f.logits = f.splits > 1;
   f.at_at = w.take((size_t)a.n * 4);
@@ -929,8 +963,8 @@ FwdPlan plan_forward(const LossArgs& a, dn_dtype dt) {
 
 struct BackPlan {
   Pack h, w;    // for dh and dw, and for the logits but where these have
-  Pack lh, lw;  // fp32 rows of two parts
-  bool two;
+  Pack lh, lw;  // fp32: for the logits, in two parts or as they lie
+  Layout logits;
   int parts, products;
   int64_t vc, ldg;  // words of a piece (a multiple of 256)
   Tile grad, dh, dw;
@@ -940,9 +974,7 @@ struct BackPlan {
   size_t coef_at, unscale_at, g_at, dh_at, dw_at, total;
 };
 constexpr int64_t PIECE_BYTES = 1LL << 29;  // of one part of g
-// fp32: from this many rows on, a second layout of w for the logits (12 bytes a value) costs less than three of the six
-// products: 1001 rows x 1024 over 10007 words 16 us against 75.
-constexpr int64_t TWO_ROWS = 400;
+int logit_products(const BackPlan& b) { return b.logits == THREE ? 6 : b.logits == TWO ? 3 : 1; }
 BackPlan plan_backward(const LossArgs& a, dn_dtype dt) {
   BackPlan b{};
   Work w;
@@ -950,10 +982,14 @@ BackPlan plan_backward(const LossArgs& a, dn_dtype dt) {
   b.parts = dt == DN_F32 ? 3 : 1, b.products = dt == DN_F32 ? 6 : 1;
   b.h = plan_pack(a.h, a.h_stride, a.n, a.C, dt, how, true, w);  // always: masked rows become 0
   b.w = plan_pack(a.w, a.w_stride, a.V, a.C, dt, how, false, w);
-  b.two = dt == DN_F32 && a.n >= TWO_ROWS;
-  if (b.two) {
-    b.lh = plan_pack(a.h, a.h_stride, a.n, a.C, dt, TWO, true, w);
-    b.lw = plan_pack(a.w, a.w_stride, a.V, a.C, dt, TWO, true, w);
+  // fp32: with few rows or words the logits need no layout; from 400 rows on a second layout of w for them (12 bytes a value)
+  // costs less than three of the six products (1001 rows x 1024 over 10007 words: 16 us against 75).
+  b.logits = how;
+  if (dt == DN_F32 && (a.n <= FEW || a.V <= FEW)) b.logits = WIDE;
+  else if (dt == DN_F32 && a.n >= 400) b.logits = TWO;
+  if (b.logits != how) {
+    b.lh = plan_pack(a.h, a.h_stride, a.n, a.C, dt, b.logits, false, w);
+    b.lw = plan_pack(a.w, a.w_stride, a.V, a.C, dt, b.logits, false, w);
   }
   const int64_t v256 = up(a.V, 256);
   b.vc = std::min(v256, std::max<int64_t>(256, PIECE_BYTES / (2 * a.n) / 256 * 256));
@@ -963,15 +999,17 @@ BackPlan plan_backward(const LossArgs& a, dn_dtype dt) {
   const Tile any[] = {T256, T128};
   const int64_t words = std::min<int64_t>(b.vc, a.V);
   int one;
-  const int from = dt == DN_F32 ? 1 : 0;  // fp32: T128 (see run_tile)
-  choose(any + from, 2 - from, words, a.n, stages_of(b.w.ld, b.two ? 3 : b.products), false, false, b.grad, one);
+  Tile of[2];
+  int tiles = logit_tiles(words, a.n, of);
+  if (dt == DN_F32 && tiles == 2) of[0] = T128, tiles = 1;  // see run_tile
+  choose(of, tiles, words, a.n, stages_of(b.logits != how ? b.lw.ld : b.w.ld, logit_products(b)), false, false, b.grad, one);
   choose(any, 2, a.C, a.n, stages_of(words, b.products), true, true, b.dh, b.dh_splits);
   choose(any, 2, a.C, words, stages_of(a.n, b.products), true, true, b.dw, b.dw_splits);
   b.dh_slab = pieces > 1 || b.dh_splits > 1;
   b.dw_slab = b.dw_splits > 1;
   b.slab_ld = up(a.C, 256);
   b.coef_at = w.take((size_t)a.n * 4);
-  b.unscale_at = w.take(4);
+  b.unscale_at = w.take(8);
   b.g_at = w.take((size_t)b.parts * a.n * b.ldg * 2);
   if (b.dh_slab) b.dh_at = w.take((size_t)b.dh_splits * a.n * b.slab_ld * 4);
   if (b.dw_slab) b.dw_at = w.take((size_t)b.dw_splits * std::min<int64_t>(b.vc, a.V) * b.slab_ld * 4);
@@ -1019,11 +1057,16 @@ int forward(const LossArgs& a, dn_dtype dt, const FwdPlan& f, char* work, hipStr
   if (f.logits) {
     g.slab = (float*)(work + f.slab_at), g.slab_ld = f.ld, g.slab_stride = a.n * f.ld;
     if ((err = run_tile<T, false, false, E_SLAB, O>(f.tile, g, st))) return err;
-    join_logits_kernel<<<dim3((unsigned)a.n), 1024, 0, st>>>(g.slab, f.ld, g.slab_stride, f.splits, a.label, a.V, a.loss, a.lse);
+    if (a.V <= 2048 && a.n > FEW)
+      join_logits_kernel<true><<<dim3((unsigned)((a.n + 3) / 4)), 256, 0, st>>>(g.slab, f.ld, g.slab_stride, f.splits, a.label, a.n, a.V,
+                                                                               a.loss, a.lse);
+    else
+      join_logits_kernel<false><<<dim3((unsigned)a.n), 1024, 0, st>>>(g.slab, f.ld, g.slab_stride, f.splits, a.label, a.n, a.V, a.loss,
+                                                                     a.lse);
   } else {
     g.stats = (float2*)(work + f.stats_at);
     if ((err = run_tile<T, false, false, E_STATS, O>(f.tile, g, st))) return err;
-    if (a.n <= 64)
+    if (a.n <= FEW)
       join_stats_kernel<1><<<dim3((unsigned)a.n), 256, 0, st>>>(g.stats, g.at, a.label, g.tiles_m, (int)a.n, a.V, a.loss, a.lse);
     else
       join_stats_kernel<16><<<dim3((unsigned)((a.n + 15) / 16)), 256, 0, st>>>(g.stats, g.at, a.label, g.tiles_m, (int)a.n, a.V,
@@ -1039,13 +1082,16 @@ int backward(const LossArgs& a, dn_dtype dt, const BackPlan& b, char* work, floa
   int err;
   if ((err = lay_out(b.h, a.h, a.h_stride, a.C, dt, a.label, a.V, work, h, st))) return err;
   if ((err = lay_out(b.w, a.w, a.w_stride, a.C, dt, nullptr, 0, work, w, st))) return err;
-  if (b.two) {
+  lh = h, lw = w;
+  if (b.logits == TWO || b.logits == WIDE) {
     if ((err = lay_out(b.lh, a.h, a.h_stride, a.C, dt, a.label, a.V, work, lh, st))) return err;
     if ((err = lay_out(b.lw, a.w, a.w_stride, a.C, dt, nullptr, 0, work, lw, st))) return err;
   }
   float* coef = (float*)(work + b.coef_at);
   float* unscale = (float*)(work + b.unscale_at);
-  coef_kernel<<<1, 1024, 0, st>>>(a.label, a.dloss, a.n, a.V, a.scale, boost, coef, unscale);
+  weight_kernel<<<1, 1024, 0, st>>>(a.label, a.dloss, a.n, a.V, a.scale, boost, unscale + 1, unscale);
+  if ((err = (int)hipGetLastError())) return err;
+  coef_kernel<<<dim3((unsigned)((a.n + 255) / 256)), 256, 0, st>>>(a.label, a.dloss, a.n, a.V, unscale + 1, coef);
   if ((err = (int)hipGetLastError())) return err;
   Matrix gm{work + b.g_at, b.ldg, a.n * b.ldg, nullptr};
   for (int64_t v0 = 0; v0 < a.V; v0 += b.vc) {
@@ -1056,12 +1102,14 @@ int backward(const LossArgs& a, dn_dtype dt, const BackPlan& b, char* work, floa
       return m;
     };
     GemmArgs g{};  // the piece's logits, leaving as g
-    set_operands(g, piece(b.two ? lw : w), vc, b.two ? lh : h, (int)a.n);
-    g.M = vc, g.N = (int)a.n, g.K = (int)b.w.ld, g.products = b.two ? 3 : b.products, g.splits = 1;
+    set_operands(g, piece(lw), vc, lh, (int)a.n);
+    g.M = vc, g.N = (int)a.n, g.K = (int)(b.logits == TWO || b.logits == WIDE ? b.lw.ld : b.w.ld), g.products = logit_products(b), g.splits = 1;
     g.label = a.label, g.v0 = (int)v0, g.V = a.V, g.lse = a.lse_in, g.coef = coef;
     g.g = work + b.g_at, g.ldg = b.ldg, g.g_part = gm.part;
     if constexpr (std::is_same<O, float>::value)
-      err = b.two ? run_tile<_Float16, false, false, E_GRAD, O>(b.grad, g, st) : run_tile<T, false, false, E_GRAD, O>(b.grad, g, st);
+      err = b.logits == TWO    ? run_tile<_Float16, false, false, E_GRAD, O>(b.grad, g, st)
+            : b.logits == WIDE ? run_tile<float, false, false, E_GRAD, O>(b.grad, g, st)
+                               : run_tile<T, false, false, E_GRAD, O>(b.grad, g, st);
     else
       err = run_tile<T, false, false, E_GRAD, O>(b.grad, g, st);
     if (err) return err;

@@ -556,3 +556,15 @@ def test_loss_past_32_bit_offsets(D):
     ref = sum(p[:, i:i + 16384] @ w[i:i + 16384].double() for i in range(0, V, 16384))
     terms = sum(p[:, i:i + 16384].abs() @ w[i:i + 16384].double().abs() for i in range(0, V, 16384))
     within(dh, ref, UNIT["bf16"] * ref.abs() * 1.01 + (UNIT["bf16"] + 4 * err + sum_err(V)) * terms, "dh")
+
+
+FEW = [(3000, 264, 21, "bf16"), (700, 1000, 33, "f16"), (2500, 100, 64, "f32"), (300, 9216, 20, "f32"), (65, 130, 65, "f32"),
+       (200, 72, 32, "f32"), (64, 257, 3000, "f32"), (33, 1024, 40, "bf16"), (500, 300, 2048, "f32"), (450, 96, 1500, "f32")]
+
+
+@pytest.mark.parametrize("n,C,V,dt", FEW)
+def test_few_words_or_rows(D, n, C, V, dt):
+    """Shapes around those where the logits change tiles or the layout of fp32 operands: 32, 64 and 400 rows, 32 and 64 words."""
+    test_loss(D, n, C, V, dt, 0, 0)
+    test_loss_gradient(D, n, C, V, dt, 0, 0, True)
+    test_loss_gradient(D, n, C, V, dt, 1, 1, False)
