@@ -356,9 +356,9 @@ int densenet_rms_norm_backward(const void* d_dy, int64_t dy_stride, dn_dtype dy_
  * l_nv = h_n . w_v, lse_n = log sum_v exp l_nv, loss_n = lse_n - l_n,label.  d_label: int64 [n]; a row whose label lies
  * outside [0, V) is masked: its loss and lse are 0, and nothing in its h reaches another row's results.
  * d_loss, d_lse: fp32 [n].  d_workspace: NULL for a size query into *bytes_needed (which depends on the pointers' alignment
- * and the strides: pass the same).  fp32 rows are taken as two fp16 parts of a power of two times the row, more than 64 of
- * them (22 bits of every value down to 2^-17 of its row's largest, 2^-39 of that below), and as they are else; fp32 values
- * have to be finite, or their row's logits are NaN. */
+ * and the strides: pass the same).  fp32: of more than 64 rows and words, rows are taken as two fp16 parts of a power of two
+ * times the row (22 bits of every value down to 2^-17 of its row's largest, 2^-39 of that below) and have to be finite, or
+ * their logits are NaN. */
 int densenet_softmax_loss(const void* d_h, int64_t h_stride, const void* d_w, int64_t w_stride,
                           const int64_t* d_label, int64_t n, int32_t C, int32_t V, dn_dtype dtype,
                           float* d_loss, float* d_lse, void* d_workspace, size_t workspace_bytes,
@@ -368,8 +368,8 @@ int densenet_softmax_loss(const void* d_h, int64_t h_stride, const void* d_w, in
  * d_lse; the logits are computed again, a piece of the vocabulary at a time.  d_dloss: fp32 [n], or NULL for the mean over
  * the unmasked rows (1 / their number each); `scale` multiplies it.  Masked rows: dh = 0, and their h does not reach dw.
  * d_dh [n][C], d_dw [V][C]: `dtype`; dw is written, not added to.  g is rounded to `dtype` (16 bits: relative 2^-9 or 2^-12,
- * of the order of the rounding of dh and dw) between the products; fp32 values of h, w and g are taken as three bf16 parts
- * (24 bits; below 2^-110 fewer) and have to be finite. */
+ * of the order of the rounding of dh and dw) between the products; fp32: of more than 64 rows and words, values of h, w and g
+ * are taken as three bf16 parts (24 bits; below 2^-110 fewer) and have to be finite. */
 int densenet_softmax_loss_backward(const void* d_h, int64_t h_stride, const void* d_w, int64_t w_stride,
                                    const int64_t* d_label, const float* d_lse, const float* d_dloss,
                                    float scale, int64_t n, int32_t C, int32_t V, dn_dtype dtype, void* d_dh,

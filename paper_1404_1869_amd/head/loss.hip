@@ -8,9 +8,9 @@
 //  logits: rows as two fp16 parts, x 2^k = a + b with 2^k such that the row's largest value lies in [2^13, 2^14), and three
 //    products a a' + a b' + b a'.  a and b hold 22 bits of a value, down to 2^-39 of the row's largest; what is left out is at
 //    most 2^-22 of a product and of either sign, as an fp32 product's and sum's roundings.  The row factors are powers of two.
-//  logits of up to 64 rows: bound by reading w, which fp32 MFMAs keep up with, so w is read as it lies and not laid out first.
 //  dh, dw: the sums run across rows, which have no common factor: three bf16 parts of every value (h, w, g) and six products,
 //    as the library's fp32 convolutions.
+//  up to 64 rows, or 64 words: bound by reading w, or h, which fp32 MFMAs keep up with: all products on the values as they lie.
 // Rows whose label lies outside [0, V) are masked: loss and lse 0, g and dh 0, and what their h holds reaches nothing.
 #include <hip/hip_runtime.h>
 
@@ -49,6 +49,9 @@ struct GemmArgs {
   int32_t M, N, K;
   int32_t a_rows, b_rows;  // rows of the operand that may be read (turned: columns, a multiple of 8)
   const float *a_factor, *b_factor;  // of the operands' rows (both or none): D[m][n] is multiplied by both
+  const int32_t* alt;                // where *alt is not 0, A lies at a_alt
+  const void* a_alt;
+  int64_t lda_alt;
   int32_t tiles_m, tiles_n, products, splits;
   // E_STATS, E_GRAD: M runs over the vocabulary from v0 on, N over rows
   const int64_t* label;
@@ -84,14 +87,16 @@ __device__ inline void wave_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// One operand's tile of R rows x 64 k in LDS, loaded straight from memory in 16-byte slots (a wave instruction fills 1 KB).
-// Plain: rows of 8 slots, slot s of row r at place s ^ (r / 2) % 8, so that 16 consecutive rows' reads of one k meet 16
-// different 16-byte places modulo 256 bytes.  Turned: rows are k, R / 8 slots each, slot s of row k at place
-// s ^ 4 (k % 4): the transposing reads take 32 bytes from each of four k at a time.
+// One operand's tile of R rows x 64 k (fp32: 32) in LDS, loaded straight from memory in 16-byte slots (a wave instruction
+// fills 1 KB).  Plain: rows of 8 slots, slot s of row r at place s ^ (r / 2) % 8, so that 16 consecutive rows' reads of one k
+// meet 16 different 16-byte places modulo 256 bytes.  Turned: rows are k, R / 8 slots each (fp32: R / 4), slot s of row k at
+// place s ^ 4 (k % 4): the transposing reads take 32 bytes from each of four k at a time; fp32 at s ^ 8 (k / 4 % 2): the halves
+// of a wave read 128 bytes each, four k apart.
 template <typename T, bool TR, int R, int NW>
 struct Operand {
+  static constexpr int ES = TR && std::is_same<T, float>::value ? 2 : 1;  // 16-bit elements of a value (plain rows count those)
   static constexpr int BYTES = R * BK * 2, PIECES = BYTES / 1024, PER = PIECES / NW;
-  static constexpr int SLOTS = TR ? R / 8 : 8, LINES = 64 / SLOTS;  // slots of an LDS row, LDS rows of a piece
+  static constexpr int SLOTS = TR ? R * ES / 8 : 8, LINES = 64 / SLOTS;  // slots of an LDS row, LDS rows of a piece
   static_assert(PIECES % NW == 0 && (!TR || SLOTS >= 16), "whole pieces per wave");
   uint32_t voff[PER];
   const char* base;
@@ -100,14 +105,14 @@ struct Operand {
 
   __device__ inline void init(const void* p, int64_t ld_, int row0, int rows, int wave, int lane) {
     ld = ld_;
-    base = (const char*)p + (TR ? (int64_t)row0 : (int64_t)row0 * ld) * 2;
+    base = (const char*)p + (TR ? (int64_t)row0 * ES : (int64_t)row0 * ld) * 2;
     const int line = lane / SLOTS, slot = lane % SLOTS;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int row = (wave + i * NW) * LINES + line;
       if constexpr (TR) {
-        const int s = slot ^ ((row & 3) << 2);
-        voff[i] = row0 + s * 8 < rows ? (uint32_t)(row * ld * 2 + s * 16) : OOB;
+        const int s = slot ^ (ES == 2 ? (row & 4) << 1 : (row & 3) << 2);
+        voff[i] = row0 * ES + s * 8 < rows ? (uint32_t)(row * ld * 2 + s * 16) : OOB;
       } else {
         const int s = slot ^ ((row >> 1) & 7);
         voff[i] = row0 + row < rows ? (uint32_t)(row * ld * 2 + s * 16) : OOB;
@@ -117,7 +122,7 @@ struct Operand {
     if constexpr (TR) place = line;
   }
   __device__ inline void load(char* lds, int64_t part, int k0, int K, int wave) const {
-    const char* p = base + part * 2 + (TR ? (int64_t)k0 * ld * 2 : 0);
+    const char* p = base + part * 2 + (TR ? (int64_t)(k0 / ES) * ld * 2 : 0);
     const __amdgpu_buffer_rsrc_t rsrc = uniform_rsrc(p, 0x7fffffffu);
     const uint32_t soff = TR ? 0 : (uint32_t)k0 * 2;
     if (k0 + BK <= K) {
@@ -126,7 +131,7 @@ struct Operand {
     } else {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const int k = k0 + (TR ? (wave + i * NW) * LINES + place : place);
+        const int k = k0 + (TR ? ((wave + i * NW) * LINES + place) * ES : place);
         direct16(rsrc, lds + (wave + i * NW) * 1024, k < K ? voff[i] : OOB, soff);
       }
     }
@@ -139,7 +144,14 @@ struct Fragments {
   typedef typename Mfma<T>::frag frag;
   uint32_t off[TR ? NT : 4];
   __device__ inline void init(int r0, int lane) {
-    if constexpr (TR) {
+    if constexpr (TR && std::is_same<T, float>::value) {
+      const int half = lane >> 5;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int m = r0 + t * 32 + (lane & 31);
+        off[t] = 4 * half * (R * 4) + ((m / 4) ^ (half << 3)) * 16 + (m % 4) * 4;
+      }
+    } else if constexpr (TR) {
       const int q = (lane & 15) >> 2;  // k of the four that this lane's address is in
       const int k = 8 * (lane >> 5) + q;
 #pragma unroll
@@ -153,17 +165,24 @@ struct Fragments {
       for (int j = 0; j < 4; ++j) off[j] = row * 128 + (((2 * j + (lane >> 5)) ^ ((row >> 1) & 7)) * 16);
     }
   }
-  // Plain: the fragments of k-step J.
+  // Plain, or fp32: the fragments of k-step J.
   template <int J>
   __device__ inline void read_step(const char* lds, frag (&f)[NT]) const {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) f[t] = *(const frag*)(lds + off[J] + t * 32 * 128);
+    for (int t = 0; t < NT; ++t) {
+      if constexpr (TR) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[t][j] = *(const float*)(lds + off[t] + (8 * J + j) * (R * 4));
+      } else {
+        f[t] = *(const frag*)(lds + off[J] + t * 32 * 128);
+      }
+    }
   }
   // The fragments of k-steps 2 H and 2 H + 1.  Turned: in one block of assembly with its wait, because the compiler would
   // first wait for every load into LDS that is on its way (it takes the transposing read to depend on them).
   template <int H>
   __device__ inline void read(const char* lds, frag (&f)[2][NT]) const {
-    if constexpr (TR) {
+    if constexpr (TR && !std::is_same<T, float>::value) {
       constexpr int K0 = H * 32 * (R * 2), ROW4 = 4 * (R * 2);
       const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)lds;
       i16x4 v[2][NT][2];
@@ -232,7 +251,7 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
   constexpr int STAGE = OA::BYTES + OB::BYTES, PER = OA::PER + OB::PER;
   constexpr int WROWS = BN / WN, WCOLS = BM / WM;
   // A wave's 32 rows x WCOLS results on their way out, rows 16 bytes apart in banks
-  constexpr int OUT_SIZE = E == E_SLAB || (E == E_OUT && std::is_same<O, float>::value) ? 4 : 2;
+  constexpr int OUT_SIZE = E == E_SLAB || (E == E_OUT ? std::is_same<O, float>::value : std::is_same<T, float>::value) ? 4 : 2;
   constexpr int OUT_ROW = WCOLS * OUT_SIZE + 16, OUT_BYTES = E == E_STATS ? WM * BN * 8 : NW * 32 * OUT_ROW;
   constexpr int LDS = NST * STAGE > OUT_BYTES ? NST * STAGE : OUT_BYTES;
   __shared__ __align__(1024) char s_mem[LDS];
@@ -251,7 +270,8 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
 
   OA oa;
   OB ob;
-  oa.init(g.a, g.lda, m0, g.a_rows, wave, lane);
+  const bool alt = AT && BT && g.alt && *g.alt;
+  oa.init(alt ? g.a_alt : g.a, alt ? g.lda_alt : g.lda, m0, g.a_rows, wave, lane);
   ob.init(g.b, g.ldb, n0, g.b_rows, wave, lane);
   Fragments<T, AT, BM, TM> fa;
   Fragments<T, BT, BN, TN> fb;
@@ -468,7 +488,7 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
         g.stats[(int64_t)tile_m * g.N + n0 + c] = float2{top, sum};
       }
   } else if constexpr (E == E_GRAD) {
-    constexpr int PARTS = std::is_same<O, float>::value ? 3 : 1;
+    constexpr int PARTS = MULTI ? 3 : 1;
     using S = std::conditional_t<PARTS == 3, __bf16, T>;  // g as it is stored
     __syncthreads();
     char* stg = s_mem + wave * 32 * OUT_ROW;
@@ -505,13 +525,13 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
               o[e] = (S)acc[i][t][4 * q + e];
               if (PARTS > 1) acc[i][t][4 * q + e] -= (float)o[e];
             }
-            *(v4*)(stg + l32 * OUT_ROW + (32 * i + 8 * q + 4 * half) * 2) = o;
+            *(v4*)(stg + l32 * OUT_ROW + (32 * i + 8 * q + 4 * half) * OUT_SIZE) = o;
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        constexpr int LANES = WCOLS / 8, LINES = 64 / LANES;  // lanes of a row, rows of an instruction
-        typedef S v8 __attribute__((ext_vector_type(8)));
+        constexpr int EV = 16 / OUT_SIZE, LANES = WCOLS / EV, LINES = 64 / LANES;  // lanes of a row, rows of an instruction
+        typedef S v8 __attribute__((ext_vector_type(EV)));
         int nn = n0 + wn * WROWS + 32 * t + lane / LANES;
-        S* dst = (S*)g.g + part * g.g_part + m0 + wm * WCOLS + (lane % LANES) * 8 + nn * g.ldg;
+        S* dst = (S*)g.g + part * g.g_part + m0 + wm * WCOLS + (lane % LANES) * EV + nn * g.ldg;
 #pragma unroll
         for (int k = 0; k < 32 / LINES; ++k) {
           const v8 o = *(const v8*)(stg + (k * LINES + lane / LANES) * OUT_ROW + (lane % LANES) * 16);
@@ -652,8 +672,9 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void join_logits_kernel(const fl
 // finite |dloss| in [2^e, 2^(e + 1)).  boost: a power of two that moves fp16's g away from its smallest values.
 __global__ __launch_bounds__(1024) void weight_kernel(const int64_t* __restrict__ label, const float* __restrict__ dloss, int64_t n,
                                                       int V, float scale, float boost, float* __restrict__ mul,
-                                                      float* __restrict__ unscale) {
+                                                      float* __restrict__ unscale, int32_t* __restrict__ flag) {
   __shared__ float s_red[16];
+  if (threadIdx.x == 0) *flag = 0;
   float v = 0.f;
   for (int64_t i0 = threadIdx.x; i0 < n; i0 += 8 * 1024) {
     int64_t l[8];
@@ -699,7 +720,9 @@ __global__ __launch_bounds__(256) void coef_kernel(const int64_t* __restrict__ l
 // three; rows whose label is outside [0, V) become 0 (label may be null).
 template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(const T* __restrict__ in, int64_t ld, int64_t rows, int C, void* __restrict__ out,
-                                                   int64_t ldo, int64_t part, const int64_t* __restrict__ label, int V) {
+                                                   int64_t ldo, int64_t part, const int64_t* __restrict__ label, int V,
+                                                   const int32_t* __restrict__ only_if) {
+  if (only_if && !*only_if) return;
   const int64_t per = ldo / 8, total = rows * per;
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
     const int64_t row = u / per;
@@ -726,9 +749,28 @@ __global__ __launch_bounds__(256) void pack_kernel(const T* __restrict__ in, int
   }
 }
 
-// fp32 rows at any alignment as aligned ones of ldo elements, zeros past column C.
+// Sets *flag if a masked row (its label outside [0, V)) holds an infinity or a NaN: such a row alone can reach dw, as 0 times
+// that.  A wave per row.
+template <typename T>
+__global__ __launch_bounds__(256) void masked_rows_kernel(const T* __restrict__ in, int64_t ld, int64_t rows, int C,
+                                                          const int64_t* __restrict__ label, int V, int32_t* __restrict__ flag) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= rows || (label[row] >= 0 && label[row] < V)) return;
+  bool bad = false;
+  for (int c = (threadIdx.x & 63) * 8; c < C; c += 512) {
+    float v[8];
+    load8(in + row * ld, c, C, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) bad |= !(fabsf(v[j]) < INFINITY);
+  }
+  if (bad) *flag = 1;
+}
+
+// fp32 rows at any alignment as aligned ones of ldo elements, zeros past column C; masked rows become 0 (label may be null).
 __global__ __launch_bounds__(256) void copy_rows_kernel(const float* __restrict__ in, int64_t ld, int64_t rows, int C,
-                                                        float* __restrict__ out, int64_t ldo) {
+                                                        float* __restrict__ out, int64_t ldo, const int64_t* __restrict__ label, int V,
+                                                        const int32_t* __restrict__ only_if) {
+  if (only_if && !*only_if) return;
   const int64_t per = ldo / 4, total = rows * per;
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
     const int64_t row = u / per;
@@ -736,6 +778,7 @@ __global__ __launch_bounds__(256) void copy_rows_kernel(const float* __restrict_
     f32x4 v;
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = c + j < C ? in[row * ld + c + j] : 0.f;
+    if (label && !(label[row] >= 0 && label[row] < V)) v = f32x4{};
     *(f32x4*)(out + row * ldo + c) = v;
   }
 }
@@ -904,17 +947,18 @@ Pack plan_pack(const void* p, int64_t ld, int64_t rows, int32_t C, dn_dtype dt, 
 }
 
 template <typename T>
-int pack(const T* in, int64_t ld, int64_t rows, int C, void* out, int64_t ldo, const int64_t* label, int V, hipStream_t st) {
+int pack(const T* in, int64_t ld, int64_t rows, int C, void* out, int64_t ldo, const int64_t* label, int V, const int32_t* only_if,
+         hipStream_t st) {
   const int64_t total = rows * (ldo / 8);
   const unsigned grid = (unsigned)std::min<int64_t>((total + 255) / 256, 8192);
-  pack_kernel<T><<<grid, 256, 0, st>>>(in, ld, rows, C, out, ldo, rows * ldo, label, V);
+  pack_kernel<T><<<grid, 256, 0, st>>>(in, ld, rows, C, out, ldo, rows * ldo, label, V, only_if);
   return (int)hipGetLastError();
 }
 int pack_any(dn_dtype dt, const void* in, int64_t ld, int64_t rows, int C, void* out, int64_t ldo, const int64_t* label, int V,
-             hipStream_t st) {
-  if (dt == DN_F32) return pack((const float*)in, ld, rows, C, out, ldo, label, V, st);
-  if (dt == DN_F16) return pack((const _Float16*)in, ld, rows, C, out, ldo, label, V, st);
-  return pack((const __bf16*)in, ld, rows, C, out, ldo, label, V, st);
+             const int32_t* only_if, hipStream_t st) {
+  if (dt == DN_F32) return pack((const float*)in, ld, rows, C, out, ldo, label, V, only_if, st);
+  if (dt == DN_F16) return pack((const _Float16*)in, ld, rows, C, out, ldo, label, V, only_if, st);
+  return pack((const __bf16*)in, ld, rows, C, out, ldo, label, V, only_if, st);
 }
 
 template <typename T, bool AT, bool BT, Epilogue E, typename O, int BM, int BN, int WM, int WN, int NST>
@@ -926,18 +970,19 @@ int run_gemm(GemmArgs& g, hipStream_t st) {
 }
 template <typename T, bool AT, bool BT, Epilogue E, typename O>
 int run_tile(Tile t, GemmArgs& g, hipStream_t st) {
-  // fp32 as it lies: few rows only.  Its g, which leaves as three parts: T256's registers do not hold that (1001 rows over 10007
-  // words: 116 us, T128 99).
-  constexpr bool wide = std::is_same<T, float>::value, parts_out = E == E_GRAD && std::is_same<O, float>::value;
+  // fp32 as it lies: few rows or words.  fp32's g from parts leaves as three parts, which T256's registers do not hold (1001
+  // rows over 10007 words: 116 us, T128 99).
+  constexpr bool wide = std::is_same<T, float>::value, logits = !AT && !BT;
+  constexpr bool parts_out = E == E_GRAD && std::is_same<O, float>::value && !wide;
   if constexpr (!wide && !parts_out)
     if (t == T256) return run_gemm<T, AT, BT, E, O, 256, 256, 2, 4, 2>(g, st);
-  if constexpr (!wide) {
+  if constexpr (!wide || !logits)
     if (t == T128) return run_gemm<T, AT, BT, E, O, 128, 128, 2, 2, 2>(g, st);
-  }
-  // fp32's g comes from fp32 as it lies or from parts
-  if constexpr (!AT && !BT && !(parts_out && !wide)) {
+  if constexpr ((logits && !parts_out) || wide)
     if (t == T64) return run_gemm<T, AT, BT, E, O, 128, 64, 2, 2, 3>(g, st);
+  if constexpr ((logits && !parts_out) || (wide && !BT))
     if (t == T32) return run_gemm<T, AT, BT, E, O, 128, 32, 4, 1, 4>(g, st);
+  if constexpr (logits && !parts_out) {
     if (t == W64) return run_gemm<T, AT, BT, E, O, 64, 128, 1, 4, 3>(g, st);
     if (t == W32) return run_gemm<T, AT, BT, E, O, 32, 128, 1, 4, 4>(g, st);
   }
@@ -978,11 +1023,13 @@ FwdPlan plan_forward(const LossArgs& a, dn_dtype dt) {
 }
 
 struct BackPlan {
-  Pack h, w;    // for dh and dw, and for the logits but where these have
-  Pack lh, lw;  // fp32: for the logits, in two parts or as they lie
+  Layout how;    // of the operands of dh and dw
+  Pack h, w;
+  bool h_spare;  // h is read as it lies, and from its copy only where a masked row holds an infinity or a NaN
   Layout logits;
-  int parts, products;
-  int64_t vc, ldg;  // words of a piece (a multiple of 256)
+  Pack lh, lw;   // fp32 parts: the logits' own layout, in two parts
+  int parts, products, unit;  // unit: 16-bit elements of a value of g
+  int64_t vc, ldg;            // words of a piece (a multiple of 256)
   Tile grad, dh, dw;
   int dh_splits, dw_splits;
   bool dh_slab, dw_slab;
@@ -990,43 +1037,47 @@ struct BackPlan {
   size_t coef_at, unscale_at, g_at, dh_at, dw_at, total;
 };
 constexpr int64_t PIECE_BYTES = 1LL << 29;  // of one part of g
+constexpr int64_t SPARE_BYTES = 32 << 20;   // from here on h is looked through before it is copied (a launch against 13 us)
 int logit_products(const BackPlan& b) { return b.logits == THREE ? 6 : b.logits == TWO ? 3 : 1; }
 BackPlan plan_backward(const LossArgs& a, dn_dtype dt) {
   BackPlan b{};
   Work w;
-  const Layout how = dt == DN_F32 ? THREE : AS_IS;
-  b.parts = dt == DN_F32 ? 3 : 1, b.products = dt == DN_F32 ? 6 : 1;
-  b.h = plan_pack(a.h, a.h_stride, a.n, a.C, dt, how, true, w);  // always: masked rows become 0
-  b.w = plan_pack(a.w, a.w_stride, a.V, a.C, dt, how, false, w);
-  // fp32: with few rows or words the logits need no layout; from 400 rows on a second layout of w for them (12 bytes a value)
-  // costs less than three of the six products (1001 rows x 1024 over 10007 words: 16 us against 75).
-  b.logits = how;
-  if (dt == DN_F32 && (a.n <= FEW || a.V <= FEW)) b.logits = WIDE;
-  else if (dt == DN_F32 && a.n >= 400) b.logits = TWO;
-  if (b.logits != how) {
-    b.lh = plan_pack(a.h, a.h_stride, a.n, a.C, dt, b.logits, false, w);
-    b.lw = plan_pack(a.w, a.w_stride, a.V, a.C, dt, b.logits, false, w);
+  const bool few = a.n <= FEW || a.V <= FEW;
+  b.how = dt != DN_F32 ? AS_IS : few ? WIDE : THREE;
+  b.parts = b.how == THREE ? 3 : 1, b.products = b.how == THREE ? 6 : 1, b.unit = b.how == WIDE ? 2 : 1;
+  const Pack plain = plan_pack(a.h, a.h_stride, a.n, a.C, dt, b.how, false, w);
+  b.h_spare = !plain.copy && (int64_t)a.n * a.C * (int64_t)dtype_size(dt) >= SPARE_BYTES;
+  b.h = plain.copy ? plain : plan_pack(a.h, a.h_stride, a.n, a.C, dt, b.how, true, w);  // masked rows become 0
+  b.w = plan_pack(a.w, a.w_stride, a.V, a.C, dt, b.how, false, w);
+  // fp32: from 400 rows on a second layout of w for the logits (12 bytes a value) costs less than three of the six products
+  // (1001 rows x 1024 over 10007 words: 16 us against 75)
+  b.logits = b.how == THREE && a.n >= 400 ? TWO : b.how;
+  if (b.logits == TWO) {
+    b.lh = plan_pack(a.h, a.h_stride, a.n, a.C, dt, TWO, true, w);
+    b.lw = plan_pack(a.w, a.w_stride, a.V, a.C, dt, TWO, true, w);
   }
   const int64_t v256 = up(a.V, 256);
-  b.vc = std::min(v256, std::max<int64_t>(256, PIECE_BYTES / (2 * a.n) / 256 * 256));
+  b.vc = std::min(v256, std::max<int64_t>(256, PIECE_BYTES / (2 * b.unit * a.n) / 256 * 256));
   const int64_t pieces = (v256 + b.vc - 1) / b.vc;
   b.vc = up((v256 + pieces - 1) / pieces, 256);
   b.ldg = b.vc;
-  const Tile any[] = {T256, T128};
   const int64_t words = std::min<int64_t>(b.vc, a.V);
-  int one;
+  const int64_t k_c = b.logits == TWO ? b.lw.ld : b.w.ld, k_v = words * b.unit, k_n = a.n * b.unit;
   Tile of[2];
-  int tiles = logit_tiles(words, a.n, of);
-  if (dt == DN_F32 && tiles == 2) of[0] = T128, tiles = 1;  // see run_tile
-  choose(of, tiles, words, a.n, stages_of(b.logits != how ? b.lw.ld : b.w.ld, logit_products(b)), false, false, b.grad, one);
-  choose(any, 2, a.C, a.n, stages_of(words, b.products), true, true, b.dh, b.dh_splits);
-  choose(any, 2, a.C, words, stages_of(a.n, b.products), true, true, b.dw, b.dw_splits);
+  int one, tiles = logit_tiles(words, a.n, of);
+  if (b.how == THREE) of[0] = T128, tiles = 1;  // see run_tile
+  choose(of, tiles, words, a.n, stages_of(k_c, logit_products(b)), false, false, b.grad, one);
+  of[0] = T256, of[1] = T128, tiles = 2;
+  if (b.how == WIDE) of[0] = a.n > FEW ? T128 : a.n > 32 ? T64 : T32, tiles = 1;
+  choose(of, tiles, a.C, a.n, stages_of(k_v, b.products), true, true, b.dh, b.dh_splits);
+  if (b.how == WIDE) of[0] = a.n > FEW ? T64 : T128;
+  choose(of, tiles, a.C, words, stages_of(k_n, b.products), true, true, b.dw, b.dw_splits);
   b.dh_slab = pieces > 1 || b.dh_splits > 1;
   b.dw_slab = b.dw_splits > 1;
   b.slab_ld = up(a.C, 256);
   b.coef_at = w.take((size_t)a.n * 4);
-  b.unscale_at = w.take(8);
-  b.g_at = w.take((size_t)b.parts * a.n * b.ldg * 2);
+  b.unscale_at = w.take(12);
+  b.g_at = w.take((size_t)b.parts * b.unit * a.n * b.ldg * 2);
   if (b.dh_slab) b.dh_at = w.take((size_t)b.dh_splits * a.n * b.slab_ld * 4);
   if (b.dw_slab) b.dw_at = w.take((size_t)b.dw_splits * std::min<int64_t>(b.vc, a.V) * b.slab_ld * 4);
   b.total = w.total;
@@ -1034,8 +1085,9 @@ BackPlan plan_backward(const LossArgs& a, dn_dtype dt) {
 }
 
 // Lays an operand out as planned; label: rows whose label is outside [0, V) become 0.
+// only_if: nothing is done where *only_if is 0.
 int lay_out(const Pack& k, const void* p, int64_t ld, int32_t C, dn_dtype dt, const int64_t* label, int V, char* work, Matrix& m,
-            hipStream_t st) {
+            hipStream_t st, const int32_t* only_if = nullptr) {
   m = Matrix{p, k.how == WIDE ? 2 * ld : ld, 0, nullptr};
   if (!k.copy) return 0;
   m.p = work + k.at, m.ld = k.ld, m.part = k.rows * k.ld;
@@ -1047,10 +1099,10 @@ int lay_out(const Pack& k, const void* p, int64_t ld, int32_t C, dn_dtype dt, co
   }
   if (k.how == WIDE) {
     const unsigned grid = (unsigned)std::min<int64_t>((k.rows * (k.ld / 8) + 255) / 256, 8192);
-    copy_rows_kernel<<<grid, 256, 0, st>>>((const float*)p, ld, k.rows, C, (float*)m.p, k.ld / 2);
+    copy_rows_kernel<<<grid, 256, 0, st>>>((const float*)p, ld, k.rows, C, (float*)m.p, k.ld / 2, label, V, only_if);
     return (int)hipGetLastError();
   }
-  return pack_any(dt, p, ld, k.rows, C, (void*)m.p, k.ld, label, V, st);
+  return pack_any(dt, p, ld, k.rows, C, (void*)m.p, k.ld, label, V, only_if, st);
 }
 
 void set_operands(GemmArgs& g, const Matrix& a, int a_rows, const Matrix& b, int b_rows) {
@@ -1091,25 +1143,30 @@ int forward(const LossArgs& a, dn_dtype dt, const FwdPlan& f, char* work, hipStr
   return (int)hipGetLastError();
 }
 
-// T: type of the products' operands; O: of the results (float where T holds fp32's parts).
+// T: type of the products' operands; O: of h, w and the results.
 template <typename T, typename O>
 int backward(const LossArgs& a, dn_dtype dt, const BackPlan& b, char* work, float boost, hipStream_t st) {
-  Matrix h, w, lh, lw;
-  int err;
-  if ((err = lay_out(b.h, a.h, a.h_stride, a.C, dt, a.label, a.V, work, h, st))) return err;
-  if ((err = lay_out(b.w, a.w, a.w_stride, a.C, dt, nullptr, 0, work, w, st))) return err;
-  lh = h, lw = w;
-  if (b.logits == TWO || b.logits == WIDE) {
-    if ((err = lay_out(b.lh, a.h, a.h_stride, a.C, dt, a.label, a.V, work, lh, st))) return err;
-    if ((err = lay_out(b.lw, a.w, a.w_stride, a.C, dt, nullptr, 0, work, lw, st))) return err;
-  }
   float* coef = (float*)(work + b.coef_at);
   float* unscale = (float*)(work + b.unscale_at);
-  weight_kernel<<<1, 1024, 0, st>>>(a.label, a.dloss, a.n, a.V, a.scale, boost, unscale + 1, unscale);
+  int32_t* flag = (int32_t*)(unscale + 2);
+  int err;
+  weight_kernel<<<1, 1024, 0, st>>>(a.label, a.dloss, a.n, a.V, a.scale, boost, unscale + 1, unscale, flag);
   if ((err = (int)hipGetLastError())) return err;
   coef_kernel<<<dim3((unsigned)((a.n + 255) / 256)), 256, 0, st>>>(a.label, a.dloss, a.n, a.V, unscale + 1, coef);
   if ((err = (int)hipGetLastError())) return err;
-  Matrix gm{work + b.g_at, b.ldg, a.n * b.ldg, nullptr};
+  Matrix h, w, lh, lw;
+  if (b.h_spare) {
+    masked_rows_kernel<O><<<dim3((unsigned)((a.n + 3) / 4)), 256, 0, st>>>((const O*)a.h, a.h_stride, a.n, a.C, a.label, a.V, flag);
+    if ((err = (int)hipGetLastError())) return err;
+  }
+  if ((err = lay_out(b.h, a.h, a.h_stride, a.C, dt, a.label, a.V, work, h, st, b.h_spare ? flag : nullptr))) return err;
+  if ((err = lay_out(b.w, a.w, a.w_stride, a.C, dt, nullptr, 0, work, w, st))) return err;
+  lh = b.h_spare ? Matrix{a.h, a.h_stride * b.unit, 0, nullptr} : h, lw = w;  // (a masked row's logits reach nothing)
+  if (b.logits == TWO) {
+    if ((err = lay_out(b.lh, a.h, a.h_stride, a.C, dt, a.label, a.V, work, lh, st))) return err;
+    if ((err = lay_out(b.lw, a.w, a.w_stride, a.C, dt, nullptr, 0, work, lw, st))) return err;
+  }
+  const Matrix gm{work + b.g_at, b.ldg * b.unit, a.n * b.ldg, nullptr};
   for (int64_t v0 = 0; v0 < a.V; v0 += b.vc) {
     const int vc = (int)std::min<int64_t>(b.vc, a.V - v0);
     const auto piece = [&](Matrix m) {  // rows v0 on
@@ -1119,20 +1176,18 @@ int backward(const LossArgs& a, dn_dtype dt, const BackPlan& b, char* work, floa
     };
     GemmArgs g{};  // the piece's logits, leaving as g
     set_operands(g, piece(lw), vc, lh, (int)a.n);
-    g.M = vc, g.N = (int)a.n, g.K = (int)(b.logits == TWO || b.logits == WIDE ? b.lw.ld : b.w.ld), g.products = logit_products(b), g.splits = 1;
+    g.M = vc, g.N = (int)a.n, g.K = (int)(b.logits == TWO ? b.lw.ld : b.w.ld), g.products = logit_products(b), g.splits = 1;
     g.label = a.label, g.v0 = (int)v0, g.V = a.V, g.lse = a.lse_in, g.coef = coef;
     g.g = work + b.g_at, g.ldg = b.ldg, g.g_part = gm.part;
-    if constexpr (std::is_same<O, float>::value)
-      err = b.logits == TWO    ? run_tile<_Float16, false, false, E_GRAD, O>(b.grad, g, st)
-            : b.logits == WIDE ? run_tile<float, false, false, E_GRAD, O>(b.grad, g, st)
-                               : run_tile<T, false, false, E_GRAD, O>(b.grad, g, st);
+    if constexpr (std::is_same<T, __bf16>::value && std::is_same<O, float>::value)
+      err = b.logits == TWO ? run_tile<_Float16, false, false, E_GRAD, O>(b.grad, g, st) : run_tile<T, false, false, E_GRAD, O>(b.grad, g, st);
     else
       err = run_tile<T, false, false, E_GRAD, O>(b.grad, g, st);
     if (err) return err;
 
     GemmArgs d{};  // dh += g w
     set_operands(d, piece(w), (int)b.w.ld, gm, (int)a.n);
-    d.M = a.C, d.N = (int)a.n, d.K = vc, d.products = b.products, d.splits = b.dh_splits;
+    d.M = a.C, d.N = (int)a.n, d.K = vc * b.unit, d.products = b.products, d.splits = b.dh_splits;
     d.unscale = unscale;
     if (b.dh_slab) {
       d.slab = (float*)(work + b.dh_at), d.slab_ld = b.slab_ld, d.slab_stride = a.n * b.slab_ld, d.accumulate = v0 > 0;
@@ -1144,8 +1199,9 @@ int backward(const LossArgs& a, dn_dtype dt, const BackPlan& b, char* work, floa
     if (err) return err;
 
     GemmArgs e{};  // dw = g^T h
-    set_operands(e, h, (int)b.h.ld, gm, (int)up(vc, 8));
-    e.M = a.C, e.N = vc, e.K = (int)a.n, e.products = b.products, e.splits = b.dw_splits;
+    set_operands(e, b.h_spare ? lh : h, (int)b.h.ld, gm, (int)up(vc, 8) * b.unit);
+    if (b.h_spare) e.alt = flag, e.a_alt = h.p, e.lda_alt = h.ld;
+    e.M = a.C, e.N = vc, e.K = (int)a.n * b.unit, e.products = b.products, e.splits = b.dw_splits;
     e.unscale = unscale;
     O* dw = (O*)a.dw + v0 * a.dw_stride;
     if (b.dw_slab) {
@@ -1195,6 +1251,7 @@ int launch_softmax_loss_backward(const LossArgs& a, dn_dtype dt, void* d_work, v
   }
   const BackPlan b = plan_backward(a, dt);
   const hipStream_t st = (hipStream_t)stream;
+  if (b.how == WIDE) return backward<float, float>(a, dt, b, (char*)d_work, 1.f, st);
   if (dt == DN_F32) return backward<__bf16, float>(a, dt, b, (char*)d_work, 1.f, st);
   if (dt == DN_F16) return backward<_Float16, _Float16>(a, dt, b, (char*)d_work, 1024.f, st);
   return backward<__bf16, __bf16>(a, dt, b, (char*)d_work, 1.f, st);

@@ -568,3 +568,18 @@ def test_few_words_or_rows(D, n, C, V, dt):
     test_loss(D, n, C, V, dt, 0, 0)
     test_loss_gradient(D, n, C, V, dt, 0, 0, True)
     test_loss_gradient(D, n, C, V, dt, 1, 1, False)
+
+
+@pytest.mark.parametrize("n,C,V,dt", [(4200, 4096, 300, "bf16"), (2100, 4096, 40, "f32"), (40, 2048, 3000, "f32")])
+def test_masked_rows_of_a_large_batch(D, n, C, V, dt):
+    """As test_masked_rows_reach_nothing, where h is read as it lies unless a masked row holds an infinity or a NaN."""
+    h, w, labels = loss_case(n, C, V, dt)
+    has = (labels >= 0) & (labels < V)
+    _, lse = D.densenet_softmax_loss(h, w, labels)
+    dh, dw = D.densenet_softmax_loss_backward(h, w, labels, lse)
+    for value in (float("nan"), float("-inf"), 1e4):
+        h2 = h.clone()
+        h2[int((~has).nonzero()[-1]), C - 1] = value
+        dh2, dw2 = D.densenet_softmax_loss_backward(h2, w, labels, lse)
+        assert torch.equal(dh, dh2) and torch.equal(dw, dw2)
+    test_loss_gradient(D, n, C, V, dt, 0, 0, True)
