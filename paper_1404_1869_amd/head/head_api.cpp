@@ -44,7 +44,7 @@ constexpr int64_t MAX_ROWS = (1LL << 31) - 256;
 int check_loss(const LossArgs& a, dn_dtype dtype) {
   if (!valid_dtype(dtype)) return fail(DN_E_UNSUPPORTED, "unknown dtype");
   if (a.n < 0 || a.C <= 0 || a.V <= 0) return fail(DN_E_INVALID_ARG, "n must be >= 0, C and V positive");
-  if (a.n > MAX_ROWS || a.V > MAX_ROWS || a.C > (1 << 21)) return fail(DN_E_TOO_LARGE, "n, V or C");
+  if (a.n > MAX_ROWS || a.V > MAX_ROWS || a.C > (1 << 20)) return fail(DN_E_TOO_LARGE, "n, V or C");
   const int64_t tn = (a.n + 127) / 128, tv = (a.V + 127) / 128, tc = (a.C + 127) / 128;
   if (tn * tv > 0x7fffffffLL || tn * tc > 0x7fffffffLL || tv * tc > 0x7fffffffLL)
     return fail(DN_E_TOO_LARGE, "n times V, n times C or V times C");
