@@ -733,6 +733,20 @@ __global__ __launch_bounds__(256) void coef_kernel(const int64_t* __restrict__ l
   if (i < n) coef[i] = coef_of(label, dloss, i, V, *mul);
 }
 
+// Eight fp32 values as three bf16 parts, `part` elements apart.
+__device__ inline void store_split3(__bf16* out, int64_t part, const float (&v)[8]) {
+  float p[3][8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    __bf16 s[3];
+    split3(v[j], s);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) p[k][j] = (float)s[k];
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) store8(out + k * part, p[k]);
+}
+
 // Copies an operand into aligned rows of ldo elements (a multiple of 8), zeros past column C, as one 16-bit part or fp32's
 // three; rows whose label is outside [0, V) become 0 (label may be null).  Units first, first + step, ... of eight values.
 template <typename T>
@@ -748,16 +762,7 @@ __device__ inline void pack_rows(const T* __restrict__ in, int64_t ld, int64_t r
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = 0.f;
     if constexpr (std::is_same<T, float>::value) {
-      float p[3][8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        __bf16 s[3];
-        split3(v[j], s);
-#pragma unroll
-        for (int k = 0; k < 3; ++k) p[k][j] = (float)s[k];
-      }
-#pragma unroll
-      for (int k = 0; k < 3; ++k) store8((__bf16*)out + k * part + row * ldo + c, p[k]);
+      store_split3((__bf16*)out + row * ldo + c, part, v);
     } else {
       store8((T*)out + row * ldo + c, v);
     }
@@ -818,11 +823,12 @@ __global__ __launch_bounds__(256) void copy_rows_kernel(const float* __restrict_
   }
 }
 
-// fp32 rows as two fp16 parts [2][rows][ldo] of x 2^k and a factor 2^-k, one workgroup per row.  Rows whose label is outside
-// [0, V) become 0 (label may be null).  A row that is not finite keeps k = 0 and so its infinities and NaN.
+// fp32 rows as two fp16 parts [2][rows][ldo] of x 2^k and a factor 2^-k, one workgroup per row; with `three` also as three bf16
+// parts [3][rows][ldo].  Rows whose label is outside [0, V) become 0 (label may be null).  A row that is not finite keeps k = 0
+// and so its infinities and NaN.
 __global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict__ in, int64_t ld, int C, _Float16* __restrict__ out,
                                                          int64_t ldo, int64_t part, float* __restrict__ factor,
-                                                         const int64_t* __restrict__ label, int V) {
+                                                         __bf16* __restrict__ three, const int64_t* __restrict__ label, int V) {
   __shared__ float s_top[4];
   const int64_t row = blockIdx.x;
   const float* x = in + row * ld;
@@ -846,7 +852,7 @@ __global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict
   const float mul = ldexpf(1.f, k);
   if (threadIdx.x == 0) factor[row] = ldexpf(1.f, -k);
   for (int c = threadIdx.x * 8; c < ldo; c += 2048) {
-    float v[8], lo[8];
+    float v[8], w[8], lo[8];
     if (c == (int)threadIdx.x * 8) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = first[j];
@@ -855,11 +861,13 @@ __global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      v[j] = zero ? 0.f : v[j] * mul;
-      lo[j] = v[j] - (float)(_Float16)v[j];
+      v[j] = zero ? 0.f : v[j];
+      w[j] = v[j] * mul;
+      lo[j] = w[j] - (float)(_Float16)w[j];
     }
-    store8(out + row * ldo + c, v);
+    store8(out + row * ldo + c, w);
     store8(out + part + row * ldo + c, lo);
+    if (three) store_split3(three + row * ldo + c, part, v);
   }
 }
 
@@ -1120,16 +1128,16 @@ BackPlan plan_backward(const LossArgs& a, dn_dtype dt) {
 }
 
 // Lays an operand out as planned; label: rows whose label is outside [0, V) become 0.
-// only_if: nothing is done where *only_if is 0.
+// only_if: nothing is done where *only_if is 0.  three (two parts only): an operand's layout in three, done along with it.
 int lay_out(const Pack& k, const void* p, int64_t ld, int32_t C, dn_dtype dt, const int64_t* label, int V, char* work, Matrix& m,
-            hipStream_t st, const int32_t* only_if = nullptr) {
+            hipStream_t st, const int32_t* only_if = nullptr, const Pack* three = nullptr) {
   m = Matrix{p, k.how == WIDE ? 2 * ld : ld, 0, nullptr};
   if (!k.copy) return 0;
   m.p = work + k.at, m.ld = k.ld, m.part = k.rows * k.ld;
   if (k.how == TWO) {
     m.factor = (const float*)(work + k.factor_at);
     split_rows_kernel<<<dim3((unsigned)k.rows), 256, 0, st>>>((const float*)p, ld, C, (_Float16*)m.p, k.ld, m.part, (float*)m.factor,
-                                                             label, V);
+                                                             three ? (__bf16*)(work + three->at) : nullptr, label, V);
     return (int)hipGetLastError();
   }
   if (k.how == WIDE) {
@@ -1187,7 +1195,7 @@ int backward(const LossArgs& a, dn_dtype dt, const BackPlan& b, char* work, floa
   int err;
   // up to 8192 rows one workgroup weighs them in one go, and the copy of h goes along with it (64 x 512 over 1000 words: two
   // launches less, 37 -> 33 us)
-  const bool small = a.n <= 8192, along = small && b.how != WIDE && !b.h_spare;
+  const bool two = b.logits == TWO, small = a.n <= 8192, along = small && b.how != WIDE && !b.h_spare && !two;
   if (small) {
     const int64_t units = along ? a.n * (b.h.ld / 8) : 0;
     const unsigned grid = 1 + (unsigned)std::min<int64_t>((units + 1023) / 1024, 2048);
@@ -1201,19 +1209,22 @@ int backward(const LossArgs& a, dn_dtype dt, const BackPlan& b, char* work, floa
     if ((err = (int)hipGetLastError())) return err;
   }
   Matrix h, w, lh, lw;
-  if (b.h_spare) {
-    masked_rows_kernel<O><<<dim3((unsigned)((a.n + 3) / 4)), 256, 0, st>>>((const O*)a.h, a.h_stride, a.n, a.C, a.label, a.V, flag);
-    if ((err = (int)hipGetLastError())) return err;
-  }
-  if (along)
+  if (two) {
+    if ((err = lay_out(b.lh, a.h, a.h_stride, a.C, dt, a.label, a.V, work, lh, st, nullptr, &b.h))) return err;
+    if ((err = lay_out(b.lw, a.w, a.w_stride, a.C, dt, nullptr, 0, work, lw, st, nullptr, &b.w))) return err;
     h = Matrix{work + b.h.at, b.h.ld, b.h.rows * b.h.ld, nullptr};
-  else if ((err = lay_out(b.h, a.h, a.h_stride, a.C, dt, a.label, a.V, work, h, st, b.h_spare ? flag : nullptr)))
-    return err;
-  if ((err = lay_out(b.w, a.w, a.w_stride, a.C, dt, nullptr, 0, work, w, st))) return err;
-  lh = b.h_spare ? Matrix{a.h, a.h_stride * b.unit, 0, nullptr} : h, lw = w;  // (a masked row's logits reach nothing)
-  if (b.logits == TWO) {
-    if ((err = lay_out(b.lh, a.h, a.h_stride, a.C, dt, a.label, a.V, work, lh, st))) return err;
-    if ((err = lay_out(b.lw, a.w, a.w_stride, a.C, dt, nullptr, 0, work, lw, st))) return err;
+    w = Matrix{work + b.w.at, b.w.ld, b.w.rows * b.w.ld, nullptr};
+  } else {
+    if (b.h_spare) {
+      masked_rows_kernel<O><<<dim3((unsigned)((a.n + 3) / 4)), 256, 0, st>>>((const O*)a.h, a.h_stride, a.n, a.C, a.label, a.V, flag);
+      if ((err = (int)hipGetLastError())) return err;
+    }
+    if (along)
+      h = Matrix{work + b.h.at, b.h.ld, b.h.rows * b.h.ld, nullptr};
+    else if ((err = lay_out(b.h, a.h, a.h_stride, a.C, dt, a.label, a.V, work, h, st, b.h_spare ? flag : nullptr)))
+      return err;
+    if ((err = lay_out(b.w, a.w, a.w_stride, a.C, dt, nullptr, 0, work, w, st))) return err;
+    lh = b.h_spare ? Matrix{a.h, a.h_stride * b.unit, 0, nullptr} : h, lw = w;  // (a masked row's logits reach nothing)
   }
   const Matrix gm{work + b.g_at, b.ldg * b.unit, a.n * b.ldg, nullptr};
   for (int64_t v0 = 0; v0 < a.V; v0 += b.vc) {
