@@ -22,7 +22,7 @@
 // Bound by the matrix cores at the clock that the chip's power allows: the products of 16384 x 16384 x 2048 in bf16 take 976, 884
 // and 842 us (1.13, 1.24, 1.31 PFLOP/s; a library's large product 1.38), their MFMA pipes 58 to 69 % busy at 1.85 to 1.79 GHz.
 // Gradients of 16384 x 2048 over 65536 words 10.9 ms (1.21 PFLOP/s), 4096 x 2048 over 32000 1.37 ms (1.17), loss of 2000 x 2048
-// over 50257 words in fp16 391 us (1.05; 1576 tiles are 6.2 rounds of workgroups), of one row x 4096 over 32000 words 61 us
+// over 50257 words in fp16 395 us (1.04; 1576 tiles are 6.2 rounds of workgroups), of one row x 4096 over 32000 words 61 us
 // (bound by memory: 4.3 TB/s), of 32000 x 9216 over 21 words 109 us (5.4 TB/s).
 #include <hip/hip_runtime.h>
 
@@ -338,7 +338,8 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
     for (int s = s0; s < s1; ++s) {
       const int buf = (s - s0) & 1;
       const char* at = s_mem + buf * STAGE;
-      // (the turned operands' reads end in a wait, so the loads go out first)
+      // (the turned operands' reads end in a wait, so the loads go out first; plain ones' go after the reads: g of 16384 x 16384
+      // x 2048 992 us, the other way 1075)
       if ((AT || BT) && s + 1 < s1) load(s + 1, buf ^ 1);
       fb.template read<0>(at + OA::BYTES, b);
       fa.template read<0>(at, a);
@@ -604,7 +605,7 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
 }
 
 // Joins the tiles of a row: ROWS rows per workgroup, 256 / ROWS tiles at a time (16 rows share the lines that their
-// statistics lie in; of a few rows each takes a workgroup).
+// statistics lie in; of a few rows each takes a workgroup: one row of 250 tiles 3.9 us, of ROWS = 16 6.6).
 template <int ROWS>
 __global__ __launch_bounds__(256) void join_stats_kernel(const float2* __restrict__ stats, const float* __restrict__ at,
                                                          const int64_t* __restrict__ label, int tiles, int n, int V,
@@ -634,7 +635,8 @@ __global__ __launch_bounds__(256) void join_stats_kernel(const float2* __restric
   }
 }
 
-// The few-tiles forward pass: logits of a row as `splits` partial sums; a workgroup per row, or (WAVE) a wave.
+// The few-tiles forward pass: logits of a row as `splits` partial sums; a workgroup per row, or (WAVE) a wave
+// (32000 rows of 200 words: 21 us, a workgroup per row 140).
 template <bool WAVE>
 __global__ __launch_bounds__(WAVE ? 256 : 1024) void join_logits_kernel(const float* __restrict__ slab, int64_t ld, int64_t stride,
                                                                         int splits, const int64_t* __restrict__ label, int64_t n, int V,
@@ -927,7 +929,9 @@ bool lies_well(const void* p, int64_t ld, int32_t C, dn_dtype dt) {
 enum Tile { T256, T128, T64, T32, W64, W32 };
 int tile_m(Tile t) { return t == T256 ? 256 : t == W64 ? 64 : t == W32 ? 32 : 128; }
 int tile_n(Tile t) { return t == T256 ? 256 : t == T64 ? 64 : t == T32 ? 32 : 128; }
-constexpr int FEW = 64;  // rows or words that these are for
+// Rows or words that these are for (16 bits: 32000 rows x 9216 over 21 words 109 us, in T256 tiles 259; fp32, read as it lies:
+// 64 rows x 2048 over 32000 words 92 us, laid out in parts 265, and 100 rows in parts 187).
+constexpr int FEW = 64;
 
 // The time of a product [M][N] over `stages` of 64 k in us, by what launches of many shapes took: a stage of T256 takes 1.25
 // us on an idle chip and 1.75 on a full one, of T128 0.62 alone on a CU and 1.1 (turned operands: 1.2) for two, and a
@@ -1093,7 +1097,7 @@ BackPlan plan_backward(const LossArgs& a, dn_dtype dt) {
   b.h = plain.copy ? plain : plan_pack(a.h, a.h_stride, a.n, a.C, dt, b.how, true, w);  // masked rows become 0
   b.w = plan_pack(a.w, a.w_stride, a.V, a.C, dt, b.how, false, w);
   // fp32: from 400 rows on a second layout of w for the logits (12 bytes a value) costs less than three of the six products
-  // (1001 rows x 1024 over 10007 words: 16 us against 75)
+  // (1001 rows x 1024 over 10007 words: 16 us against 75; of 300 rows the whole call takes 213 us with it, 210 without)
   b.logits = b.how == THREE && a.n >= 400 ? TWO : b.how;
   if (b.logits == TWO) {
     b.lh = plan_pack(a.h, a.h_stride, a.n, a.C, dt, TWO, true, w);

@@ -583,3 +583,54 @@ def test_masked_rows_of_a_large_batch(D, n, C, V, dt):
         dh2, dw2 = D.densenet_softmax_loss_backward(h2, w, labels, lse)
         assert torch.equal(dh, dh2) and torch.equal(dw, dw2)
     test_loss_gradient(D, n, C, V, dt, 0, 0, True)
+
+
+def test_outputs_with_strides_leave_the_rest(D):
+    """Results written into columns of wider buffers: the columns beside them stay as they were."""
+    n, C, V = 70, 131, 300
+    g = gen(6)
+    x, r = rows(g, n, C, "bf16", 5), rows(g, n, C, "bf16", 2)
+    wide = lambda rows_, dt: torch.full((rows_ + 1, C + 3), 7.0, device="cuda").to(dt)  # noqa: E731
+    y, s, q, dx, dh, dw = (wide(k, torch.bfloat16) for k in (n, n, n, n, n, V))
+    q = wide(n, torch.float8_e4m3fn)
+    cut = lambda t, k=n: t[:k, 1:1 + C]  # noqa: E731
+    D.densenet_rms_norm(x, residual=r, out=cut(y), sum_out=cut(s))
+    D.densenet_rms_norm(x, residual=r, out=cut(q), out_dtype=D.DN_F8, block=32)
+    D.densenet_rms_norm_backward(r, x, dx=cut(dx))
+    w, labels = rows(g, V, C, "bf16", 4, 0.1), torch.randint(-1, V, (n,), generator=g, device="cuda")
+    _, lse = D.densenet_softmax_loss(x, w, labels)
+    D.densenet_softmax_loss_backward(x, w, labels, lse, dh=cut(dh), dw=cut(dw, V))
+    a, b, _ = D.densenet_rms_norm(x, residual=r)
+    c, _, _ = D.densenet_rms_norm(x, residual=r, out_dtype=D.DN_F8, block=32)
+    e, _ = D.densenet_rms_norm_backward(r, x)
+    h, v = D.densenet_softmax_loss_backward(x, w, labels, lse)
+    for t, want in ((y, a), (s, b), (q, c), (dx, e), (dh, h), (dw, v)):
+        k = want.shape[0]
+        assert torch.equal(t[:k, 1:1 + C].float(), want.float())
+        rest = t.float().clone()
+        rest[:k, 1:1 + C] = 7
+        assert bool((rest == 7).all())
+
+
+@pytest.mark.parametrize("n,C,V,dt", [(1, 4096, 2000, "bf16"), (64, 1024, 30000, "f16"), (300, 96, 777, "bf16"), (1001, 300, 5003, "f32"),
+                                      (200, 264, 3000, "f32"), (20, 512, 4000, "f32"), (3000, 264, 21, "f32"), (9000, 130, 500, "bf16"),
+                                      (4200, 4096, 300, "bf16")])
+def test_workspace_is_enough(D, n, C, V, dt):
+    """The calls stay within the workspace that their size queries ask for."""
+    import ctypes
+    h, w, labels = loss_case(n, C, V, dt)
+    L, code, st = D.lib(), D.DTYPES[dt], D._on(h.device)
+    need = ctypes.c_size_t()
+    out = [torch.empty(n, device="cuda") for _ in range(2)]
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    ops = (h.data_ptr(), C, w.data_ptr(), C, labels.data_ptr())
+    dims = (n, C, V, code)
+    calls = ((L.densenet_softmax_loss, (*ops, *dims, out[0].data_ptr(), out[1].data_ptr())),
+             (L.densenet_softmax_loss_backward, (*ops, out[1].data_ptr(), None, 1.0, *dims, dh.data_ptr(), C, dw.data_ptr(), C)))
+    for call, args in calls:
+        D.check(call(*args, None, 0, ctypes.byref(need), st))
+        work = torch.full((need.value + 4096,), 165, dtype=torch.uint8, device="cuda")
+        D.check(call(*args, work.data_ptr(), need.value, ctypes.byref(need), st))
+        assert bool((work[need.value:] == 165).all())
+        assert call(*args, work.data_ptr(), need.value - 1, ctypes.byref(need), st) == D.DN_E_BUFFER_TOO_SMALL
+    assert all(bool(t.isfinite().all()) for t in (*out, dh, dw))
