@@ -479,10 +479,12 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
       // the maximum in base 2, rounded: what is subtracted here is added again by the join, to the bit
       top = fmaxf(top, __shfl_xor(top, 32)) * LOG2E;
       const float ref = top == -INFINITY ? 0.f : top;
+      float part[4] = {0.f, 0.f, 0.f, 0.f};  // small exponentials meet the largest, 1, in a fourth of the sums
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum += exp2_of(__builtin_fmaf(acc[i][t][r], LOG2E, -ref));
+        for (int r = 0; r < 16; ++r) part[r % 4] += exp2_of(__builtin_fmaf(acc[i][t][r], LOG2E, -ref));
+      sum = (part[0] + part[1]) + (part[2] + part[3]);
       sum += __shfl_xor(sum, 32);
       if (half == 0) red[wm * BN + wn * WROWS + 32 * t + l32] = float2{top, sum};
     }
@@ -629,9 +631,11 @@ __global__ __launch_bounds__(256) void join_stats_kernel(const float2* __restric
     for (int w = 1; w < 4; ++w) add(s_red[w][threadIdx.x]);
     const int64_t l = label[row];
     const bool has = l >= 0 && l < V;
-    const float z = (log2f(sum) + top) * LN2;
-    lse[row] = has ? z : 0.f;
-    loss[row] = has ? z - at[row] : 0.f;
+    // the loss from the logits' difference, not from lse, whose rounding grows with the logits: of a row that is sure of its
+    // label, little is left of lse - l
+    const float lg = logf(sum);
+    lse[row] = has ? __builtin_fmaf(top, LN2, lg) : 0.f;
+    loss[row] = has ? __builtin_fmaf(__builtin_fmaf(at[row], -LOG2E, top), LN2, lg) : 0.f;
   }
 }
 
@@ -675,9 +679,9 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void join_logits_kernel(const fl
       for (int w = 0; w < 16; ++w) z += s_top[w] == -INFINITY ? s_sum[w] : s_sum[w] * exp2_of((s_top[w] - mr) * LOG2E);
     }
     const bool has = l >= 0 && l < V;
-    z = logf(z) + m;
-    lse[row] = has ? z : 0.f;
-    loss[row] = has ? z - s_at[sub] : 0.f;
+    z = logf(z);
+    lse[row] = has ? z + m : 0.f;
+    loss[row] = has ? z + (m - s_at[sub]) : 0.f;  // as above
   }
 }
 

@@ -634,3 +634,22 @@ def test_workspace_is_enough(D, n, C, V, dt):
         assert bool((work[need.value:] == 165).all())
         assert call(*args, work.data_ptr(), need.value - 1, ctypes.byref(need), st) == D.DN_E_BUFFER_TOO_SMALL
     assert all(bool(t.isfinite().all()) for t in (*out, dh, dw))
+
+
+@pytest.mark.parametrize("n,C,V", [(4, 64, 300), (4, 4096, 300), (200, 4096, 40), (300, 64, 5000), (300, 4096, 300)])
+def test_loss_of_rows_that_are_sure(D, n, C, V):
+    """Labels whose logits lead by 8 among logits of a hundred: the loss (about V e^-8) keeps its digits, in all paths of the
+    join.  The logits are exact (one value of a row, integers and eighths), so the bound is the softmax's own: a few units of
+    fp32 of the loss and of the exponentials, not of the logits."""
+    h = torch.zeros(n, C, device="cuda", dtype=torch.bfloat16)
+    w = torch.zeros(V, C, device="cuda", dtype=torch.bfloat16)
+    h[:, 0] = 8
+    w[:, 0] = torch.randint(90, 97, (V,), generator=gen(1), device="cuda").bfloat16() / 8
+    labels = torch.randint(0, V, (n,), generator=gen(2), device="cuda")
+    labels[:] = labels[0]
+    w[labels[0], 0] = 13  # 104, at least 8 above the others
+    loss, _ = D.densenet_softmax_loss(h, w, labels)
+    logits = h.double() @ w.double().T
+    want = torch.logsumexp(logits, 1) - logits.gather(1, labels[:, None])[:, 0]
+    assert 0 < float(want.min()) < 1
+    within(loss, want, 2.0 ** -20 * (want + 0.1), "loss")
