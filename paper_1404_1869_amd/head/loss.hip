@@ -21,8 +21,8 @@
 // same bits every time.
 // Bound by the matrix cores at the clock that the chip's power allows: the products of 16384 x 16384 x 2048 in bf16 take 976, 884
 // and 842 us (1.13, 1.24, 1.31 PFLOP/s; a library's large product 1.38), their MFMA pipes 58 to 69 % busy at 1.85 to 1.79 GHz.
-// Gradients of 16384 x 2048 over 65536 words 10.9 ms (1.21 PFLOP/s), 4096 x 2048 over 32000 1.37 ms (1.17), loss of 2000 x 2048
-// over 50257 words in fp16 395 us (1.04; 1576 tiles are 6.2 rounds of workgroups), of one row x 4096 over 32000 words 61 us
+// Gradients of 16384 x 2048 over 65536 words 10.9 ms (1.21 PFLOP/s), 4096 x 2048 over 32000 1.35 ms (1.19), loss of 2000 x 2048
+// over 50257 words in fp16 386 us (1.07; 1576 tiles are 6.2 rounds of workgroups), of one row x 4096 over 32000 words 61 us
 // (bound by memory: 4.3 TB/s), of 32000 x 9216 over 21 words 109 us (5.4 TB/s).
 #include <hip/hip_runtime.h>
 
