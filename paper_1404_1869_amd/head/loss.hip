@@ -6,8 +6,9 @@
 // 16 bits, and two more products take dh and dw from it: 6 n V C operations, the least without the logits.
 // 16-bit types: products on the matrix cores, 32-bit sums.  fp32, by what the product can take:
 //  logits: rows as two fp16 parts, x 2^k = a + b with 2^k such that the row's largest value lies in [2^13, 2^14), and three
-//    products a a' + a b' + b a'.  a and b hold 22 bits of a value, down to 2^-39 of the row's largest; what is left out is at
-//    most 2^-22 of a product and of either sign, as an fp32 product's and sum's roundings.  The row factors are powers of two.
+//    products a a' + a b' + b a'.  a and b hold 22 bits of a value down to 2^-16 of the row's largest (half of b's smallest
+//    step is 2^-25, 2^-38 of the largest); what is left out is at most 2^-22 of a product and of either sign, as an fp32
+//    product's and sum's roundings.  The row factors are powers of two.
 //  dh, dw: the sums run across rows, which have no common factor: three bf16 parts of every value (h, w, g) and six products,
 //    as the library's fp32 convolutions.
 //  up to 64 rows, or 64 words: bound by reading w, or h, which fp32 MFMAs keep up with: all products on the values as they lie.

@@ -653,3 +653,22 @@ def test_loss_of_rows_that_are_sure(D, n, C, V):
     want = torch.logsumexp(logits, 1) - logits.gather(1, labels[:, None])[:, 0]
     assert 0 < float(want.min()) < 1
     within(loss, want, 2.0 ** -20 * (want + 0.1), "loss")
+
+
+@pytest.mark.parametrize("drop", [0, 10, 16, 24])
+def test_fp32_values_far_below_their_rows_largest(D, drop):
+    """fp32 logits from two fp16 parts: a value of 2^-drop to 2^-(drop + 1) of its row's largest, which meets a zero weight,
+    keeps 22 bits, or is off by half of fp16's smallest step, 2^-25, where the largest is scaled to 2^13 at least: 2^-38 of
+    it.  Each product is off by that of either factor (w's one value is its row's largest)."""
+    rel = max(2.0 ** -22, 2.0 ** (drop + 1 - 38))
+    n, C, V = 100, 16, 200
+    g = gen(drop)
+    h, w = torch.zeros(n, C, device="cuda"), torch.zeros(V, C, device="cuda")
+    h[:, 0] = 1 + torch.rand(n, generator=g, device="cuda")
+    h[:, 5] = h[:, 0] * 2.0 ** -drop * (1 + torch.rand(n, generator=g, device="cuda")) / 2
+    w[:, 5] = 2.0 ** drop * (20 + 40 * torch.rand(V, generator=g, device="cuda"))
+    labels = torch.randint(0, V, (n,), generator=g, device="cuda")
+    _, lse = D.densenet_softmax_loss(h, w, labels)
+    logits = h.double() @ w.double().T
+    want = torch.logsumexp(logits, 1)
+    within(lse, want, (rel + 2.0 ** -22 + 2.0 ** -23) * 1.01 * logits.amax(1) + 2.0 ** -22 * want, "lse")
