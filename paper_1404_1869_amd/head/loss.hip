@@ -245,9 +245,11 @@ struct Fragments {
 constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
 __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// x as three bf16 parts, each the nearest of what the ones before leave.
+// x as three bf16 parts, each the nearest of what the ones before leave.  Finite values past bf16's largest (fp32's lowest, as
+// a mask, among them) start from that: rounded to an infinity, they would make a NaN of their product with a g of 0.
 __device__ inline void split3(float x, __bf16 (&p)[3]) {
-  p[0] = (__bf16)x;
+  constexpr float BF16_MAX = 3.38953139e38f;
+  p[0] = (__bf16)(fabsf(x) < INFINITY ? fminf(fmaxf(x, -BF16_MAX), BF16_MAX) : x);
   const float r = x - (float)p[0];
   p[1] = (__bf16)r;
   p[2] = (__bf16)(r - (float)p[1]);
@@ -421,6 +423,9 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
   const int mw = m0 + wm * WCOLS + 4 * half, nw = n0 + wn * WROWS + l32;
   // fp32's logits from two fp16 parts: the rows' factors
   if constexpr ((E == E_STATS || E == E_GRAD || E == E_SLAB) && !AT && std::is_same<T, _Float16>::value && std::is_same<O, float>::value) {
+    float fb[TN];
+#pragma unroll
+    for (int t = 0; t < TN; ++t) fb[t] = nw + 32 * t < g.N ? g.b_factor[nw + 32 * t] : 0.f;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
 #pragma unroll
@@ -433,20 +438,14 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) f[e] = m + e < g.M ? g.a_factor[m + e] : 0.f;
         }
+        // (one factor at a time a sum could pass fp32's range on its way to a logit within it; an infinite factor would make
+        // a NaN of a sum of 0)
 #pragma unroll
         for (int t = 0; t < TN; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][t][4 * q + e] *= f[e];
+          for (int e = 0; e < 4; ++e) acc[i][t][4 * q + e] *= fminf(f[e] * fb[t], 3.4e38f);
       }
       __builtin_amdgcn_sched_barrier(0);  // 16 factors at a time: the registers are full of sums
-    }
-#pragma unroll
-    for (int t = 0; t < TN; ++t) {
-      const float f = nw + 32 * t < g.N ? g.b_factor[nw + 32 * t] : 0.f;
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][t][r] *= f;
     }
   }
   if constexpr (E == E_STATS) {

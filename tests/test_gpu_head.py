@@ -672,3 +672,27 @@ def test_fp32_values_far_below_their_rows_largest(D, drop):
     logits = h.double() @ w.double().T
     want = torch.logsumexp(logits, 1)
     within(lse, want, (rel + 2.0 ** -22 + 2.0 ** -23) * 1.01 * logits.amax(1) + 2.0 ** -22 * want, "lse")
+
+
+@pytest.mark.parametrize("n", [3, 100, 500])
+def test_fp32_words_of_the_lowest_value(D, n):
+    """A word masked by fp32's lowest value, in each layout of fp32 operands (as they lie, three parts, two and three): no row
+    reaches it, and the gradients of the others are what they are without it."""
+    C, V = 72, 200
+    h, w, labels = loss_case(n, C, V, "f32", masked=0.0)
+    h[:, 0] = 0.5
+    labels[labels == 7] = 8
+    keep = [v for v in range(V) if v != 7]
+    w[7] = 0
+    w[7, 0] = torch.finfo(torch.float32).min
+    loss, lse = D.densenet_softmax_loss(h, w, labels)
+    dh, dw = D.densenet_softmax_loss_backward(h, w, labels, lse)
+    assert not bool(dw[7].any())
+    want, wl, _, _, err = plain_loss(h, w[keep], labels - (labels > 7).long(), "f32")
+    within(lse, wl, 2 * err + 2.0 ** -21 * (wl.abs() + 16), "lse")
+    p = torch.exp(h.double() @ w.double().T - wl[:, None])
+    p.scatter_add_(1, labels[:, None], -torch.ones_like(p[:, :1]))
+    p /= n
+    tol = 2 * err.max() + 2.0 ** -20
+    within(dh, p @ w.double(), (tol + 6 * sum_err(V)) * (p[:, keep].abs() @ w[keep].double().abs()) + 1e-30, "dh")
+    within(dw, p.T @ h.double(), (tol + 6 * sum_err(n)) * (p.abs().T @ h.double().abs()) + 1e-30, "dw")
