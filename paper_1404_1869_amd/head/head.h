@@ -7,6 +7,9 @@
 namespace dn {
 namespace head {
 
+// HIP counts a launch's threads in 32 bits: of 2^32 and more it runs fewer workgroups than were asked for, and says nothing.
+constexpr int64_t MAX_LAUNCH_THREADS = (1LL << 32) - 1;
+
 // ---------------------------------------------------------------------------------------------
 // Launchers.  Every launcher enqueues on `stream` and returns hipGetLastError() as an int (0 = success).
 // ---------------------------------------------------------------------------------------------

@@ -251,22 +251,35 @@ int with_type(dn_dtype dt, F&& f) {
 }  // namespace
 
 // A wave per row where its lanes can hold it in up to four times eight values each, else a workgroup (8191 unaligned rows of
-// 2047 fp16 values: 27 us, a workgroup per row 35).
+// 2047 fp16 values: 27 us, a workgroup per row 35).  More rows than a launch can have threads for (2^26 by waves) go in several.
 int launch_rms_norm(const NormArgs& a, dn_dtype dt, dn_dtype y_dt, void* stream) {
   const auto with = [&](auto shape) {
     using S = decltype(shape);
     return with_type(dt, [&](auto x) {
       using T = decltype(x);
-      const dim3 grid((unsigned)(S::wave ? (a.n + 3) / 4 : a.n));
       const int threads = S::threads(a.C);
-      if (y_dt == DN_F8)
-        rms_norm_kernel<T, F8, S::wave, S::nv, S::most><<<grid, threads, 0, (hipStream_t)stream>>>(a);
-      else
-        with_type(y_dt, [&](auto y) {
-          rms_norm_kernel<T, decltype(y), S::wave, S::nv, S::most><<<grid, threads, 0, (hipStream_t)stream>>>(a);
-          return 0;
-        });
-      return (int)hipGetLastError();
+      const int64_t per = S::wave ? 4 : 1, most = MAX_LAUNCH_THREADS / threads * per;  // rows of a workgroup, of a launch
+      const int64_t y_size = y_dt == DN_F8 ? 1 : (int64_t)dtype_size(y_dt);
+      const int64_t scales = a.block ? (a.C + a.block - 1) / a.block : 1;
+      for (int64_t at = 0; at < a.n; at += most) {
+        NormArgs b = a;
+        b.n = std::min(a.n - at, most);
+        b.x = (const T*)a.x + at * a.x_stride;
+        if (a.res) b.res = (const T*)a.res + at * a.res_stride;
+        if (a.sum) b.sum = (T*)a.sum + at * a.sum_stride;
+        b.y = (char*)a.y + at * a.y_stride * y_size;
+        if (a.scale) b.scale = a.scale + at * scales;
+        const dim3 grid((unsigned)((b.n + per - 1) / per));
+        if (y_dt == DN_F8)
+          rms_norm_kernel<T, F8, S::wave, S::nv, S::most><<<grid, threads, 0, (hipStream_t)stream>>>(b);
+        else
+          with_type(y_dt, [&](auto y) {
+            rms_norm_kernel<T, decltype(y), S::wave, S::nv, S::most><<<grid, threads, 0, (hipStream_t)stream>>>(b);
+            return 0;
+          });
+        if (const int err = (int)hipGetLastError()) return err;
+      }
+      return 0;
     });
   };
   if (a.C <= 512) return with(Shape<true, 1, 512>{});
