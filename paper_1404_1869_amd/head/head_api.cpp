@@ -40,14 +40,19 @@ int check_work(const void* work, size_t bytes, size_t need, size_t* needed) {
 }
 
 constexpr int64_t MAX_ROWS = (1LL << 31) - 256;
+constexpr int64_t MAX_BACK_ROWS = (1LL << 30) - 256;  // twice their number is a product's k in fp32
+constexpr int64_t MAX_TILES = MAX_LAUNCH_THREADS / 256;
 
-int check_loss(const LossArgs& a, dn_dtype dtype) {
+int check_loss(const LossArgs& a, dn_dtype dtype, bool backward) {
   if (!valid_dtype(dtype)) return fail(DN_E_UNSUPPORTED, "unknown dtype");
   if (a.n < 0 || a.C <= 0 || a.V <= 0) return fail(DN_E_INVALID_ARG, "n must be >= 0, C and V positive");
   if (a.n > MAX_ROWS || a.V > MAX_ROWS || a.C > (1 << 20)) return fail(DN_E_TOO_LARGE, "n, V or C");
   const int64_t tn = (a.n + 127) / 128, tv = (a.V + 127) / 128, tc = (a.C + 127) / 128;
   if (tn * tv > 0x7fffffffLL || tn * tc > 0x7fffffffLL || tv * tc > 0x7fffffffLL)
     return fail(DN_E_TOO_LARGE, "n times V, n times C or V times C");
+  // (the forward pass goes over n in pieces, the gradient over V)
+  if (backward && (a.n > MAX_BACK_ROWS || tn * tc > MAX_TILES || tv * tc > MAX_TILES))
+    return fail(DN_E_TOO_LARGE, "n, n times C or V times C");
   const size_t e = dtype_size(dtype);
   int st;
   if ((st = check_rows("h", a.h, a.h_stride, a.n, a.C, e))) return st;
@@ -134,7 +139,7 @@ int densenet_softmax_loss(const void* d_h, int64_t h_stride, const void* d_w, in
     a.h = d_h, a.w = d_w, a.label = d_label, a.h_stride = h_stride, a.w_stride = w_stride;
     a.n = n, a.C = C, a.V = V, a.loss = d_loss, a.lse = d_lse;
     int st;
-    if ((st = check_loss(a, dtype))) return st;
+    if ((st = check_loss(a, dtype, false))) return st;
     const size_t need = n ? softmax_loss_bytes(a, dtype) : 0;
     if ((st = check_work(d_workspace, workspace_bytes, need, bytes_needed)) || !d_workspace) return st;
     if (n == 0) return DN_OK;
@@ -155,7 +160,7 @@ int densenet_softmax_loss_backward(const void* d_h, int64_t h_stride, const void
     a.n = n, a.C = C, a.V = V, a.lse_in = d_lse, a.dloss = d_dloss, a.scale = scale;
     a.dh = d_dh, a.dw = d_dw, a.dh_stride = dh_stride, a.dw_stride = dw_stride;
     int st;
-    if ((st = check_loss(a, dtype))) return st;
+    if ((st = check_loss(a, dtype, true))) return st;
     const size_t need = softmax_loss_backward_bytes(a, dtype);
     if ((st = check_work(d_workspace, workspace_bytes, need, bytes_needed)) || !d_workspace) return st;
     const size_t e = dtype_size(dtype);

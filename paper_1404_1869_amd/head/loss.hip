@@ -964,13 +964,19 @@ int logit_tiles(int64_t V, int64_t n, Tile (&of)[2]) {
   of[0] = V <= 32 && n > 32 ? W32 : n <= 32 ? T32 : n <= FEW ? T64 : W64;
   return 1;
 }
-// The tile and the splits with the least time (splits of at least 4 stages; one split unless `split`).
+// Whether a launch can have the product's workgroups.
+bool fits_launch(Tile t, int64_t M, int64_t N, int splits) {
+  const int64_t groups = ((M + tile_m(t) - 1) / tile_m(t)) * ((N + tile_n(t) - 1) / tile_n(t)) * splits;
+  return groups <= MAX_LAUNCH_THREADS / (t == T256 ? 512 : 256);
+}
+// The tile and the splits with the least time (splits of at least 4 stages; one split unless `split`).  One of the tiles in one
+// split fits a launch: the checks of the arguments, and forward_rows, see to it.
 void choose(const Tile* of, int n_tiles, int64_t M, int64_t N, int64_t stages, bool split, bool turned, Tile& tile, int& splits) {
   double best = 1e300;
   for (int i = 0; i < n_tiles; ++i)
     for (int s = 1; s <= 64 && (s == 1 || (split && stages / s >= 4)); ++s) {
       const double us = product_us(of[i], M, N, stages, s, turned);
-      if (us < best * 0.999) best = us, tile = of[i], splits = s;
+      if (fits_launch(of[i], M, N, s) && us < best * 0.999) best = us, tile = of[i], splits = s;
     }
 }
 int64_t stages_of(int64_t k, int products) { return (k + BK - 1) / BK * products; }
@@ -1149,9 +1155,14 @@ int lay_out(const Pack& k, const void* p, int64_t ld, int32_t C, dn_dtype dt, co
   m.p = work + k.at, m.ld = k.ld, m.part = k.rows * k.ld;
   if (k.how == TWO) {
     m.factor = (const float*)(work + k.factor_at);
-    split_rows_kernel<<<dim3((unsigned)k.rows), 256, 0, st>>>((const float*)p, ld, C, (_Float16*)m.p, k.ld, m.part, (float*)m.factor,
-                                                             three ? (__bf16*)(work + three->at) : nullptr, label, V);
-    return (int)hipGetLastError();
+    constexpr int64_t most = MAX_LAUNCH_THREADS / 256;  // rows of a launch
+    for (int64_t at = 0; at < k.rows; at += most) {
+      split_rows_kernel<<<dim3((unsigned)std::min(k.rows - at, most)), 256, 0, st>>>(
+          (const float*)p + at * ld, ld, C, (_Float16*)m.p + at * k.ld, k.ld, m.part, (float*)m.factor + at,
+          three ? (__bf16*)(work + three->at) + at * k.ld : nullptr, label ? label + at : nullptr, V);
+      if (const int err = (int)hipGetLastError()) return err;
+    }
+    return 0;
   }
   if (k.how == WIDE) {
     const unsigned grid = (unsigned)std::min<int64_t>((k.rows * (k.ld / 8) + 255) / 256, 8192);
@@ -1229,8 +1240,13 @@ int backward(const LossArgs& a, dn_dtype dt, const BackPlan& b, char* work, floa
     w = Matrix{work + b.w.at, b.w.ld, b.w.rows * b.w.ld, nullptr};
   } else {
     if (b.h_spare) {
-      masked_rows_kernel<O><<<dim3((unsigned)((a.n + 3) / 4)), 256, 0, st>>>((const O*)a.h, a.h_stride, a.n, a.C, a.label, a.V, flag);
-      if ((err = (int)hipGetLastError())) return err;
+      constexpr int64_t most = MAX_LAUNCH_THREADS / 256 * 4;  // rows of a launch
+      for (int64_t at = 0; at < a.n; at += most) {
+        const int64_t rows = std::min(a.n - at, most);
+        masked_rows_kernel<O><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>((const O*)a.h + at * a.h_stride, a.h_stride, rows, a.C,
+                                                                                a.label + at, a.V, flag);
+        if ((err = (int)hipGetLastError())) return err;
+      }
     }
     if (along)
       h = Matrix{work + b.h.at, b.h.ld, b.h.rows * b.h.ld, nullptr};
@@ -1301,16 +1317,41 @@ int backward(const LossArgs& a, dn_dtype dt, const BackPlan& b, char* work, floa
 
 }  // namespace
 
-size_t softmax_loss_bytes(const LossArgs& a, dn_dtype dt) { return plan_forward(a, dt).total; }
+// The forward pass goes over more rows than its launches have threads for in pieces: of 2^22 rows less a tile (1024 threads each
+// in the join), and of 2^24 - 1 tiles of 128 x 128.
+int64_t forward_rows(const LossArgs& a) {
+  const int64_t most = std::min<int64_t>((1 << 22) - 128, ((1 << 24) - 1) / (((int64_t)a.V + 127) / 128) * 128);
+  const int64_t pieces = (a.n + most - 1) / most;
+  return std::min(most, up((a.n + pieces - 1) / pieces, 128));
+}
+LossArgs forward_piece(const LossArgs& a, dn_dtype dt, int64_t at, int64_t rows) {
+  LossArgs p = a;
+  p.h = (const char*)a.h + at * a.h_stride * (int64_t)dtype_size(dt);
+  p.label = a.label + at, p.n = std::min(rows, a.n - at);
+  if (a.loss) p.loss = a.loss + at;
+  if (a.lse) p.lse = a.lse + at;
+  return p;
+}
+
+size_t softmax_loss_bytes(const LossArgs& a, dn_dtype dt) {
+  const int64_t rows = forward_rows(a), last = (a.n - 1) / rows * rows;  // all pieces but the last are alike
+  return std::max(plan_forward(forward_piece(a, dt, 0, rows), dt).total, plan_forward(forward_piece(a, dt, last, rows), dt).total);
+}
 size_t softmax_loss_backward_bytes(const LossArgs& a, dn_dtype dt) { return a.n ? plan_backward(a, dt).total : 0; }
 
 int launch_softmax_loss(const LossArgs& a, dn_dtype dt, void* d_work, void* stream) {
-  const FwdPlan f = plan_forward(a, dt);
   const hipStream_t st = (hipStream_t)stream;
-  if (f.how == WIDE) return forward<float, float>(a, dt, f, (char*)d_work, st);
-  if (f.how == TWO) return forward<_Float16, float>(a, dt, f, (char*)d_work, st);
-  if (dt == DN_F16) return forward<_Float16, _Float16>(a, dt, f, (char*)d_work, st);
-  return forward<__bf16, __bf16>(a, dt, f, (char*)d_work, st);
+  const int64_t rows = forward_rows(a);
+  for (int64_t at = 0; at < a.n; at += rows) {
+    const LossArgs p = forward_piece(a, dt, at, rows);
+    const FwdPlan f = plan_forward(p, dt);
+    const int err = f.how == WIDE  ? forward<float, float>(p, dt, f, (char*)d_work, st)
+                    : f.how == TWO ? forward<_Float16, float>(p, dt, f, (char*)d_work, st)
+                    : dt == DN_F16 ? forward<_Float16, _Float16>(p, dt, f, (char*)d_work, st)
+                                   : forward<__bf16, __bf16>(p, dt, f, (char*)d_work, st);
+    if (err) return err;
+  }
+  return 0;
 }
 
 int launch_softmax_loss_backward(const LossArgs& a, dn_dtype dt, void* d_work, void* stream) {
