@@ -221,7 +221,7 @@ int densenet_adamw(const dn_adamw_tensor* tensors, int32_t count, dn_dtype p_dty
     for (int32_t i = 0; i < count; ++i) {
       const dn_adamw_tensor& t = tensors[i];
       // a tensor of more workgroups than a launch can have goes in several parts, at whole tiles
-      constexpr int64_t most = 1LL << 30;
+      constexpr int64_t most = MAX_LAUNCH_THREADS / 256;
       for (int64_t at = 0; at < t.n;) {
         const int64_t n = std::min<int64_t>(t.n - at, most * ADAMW_TILE), own = (n + ADAMW_TILE - 1) / ADAMW_TILE;
         if (a.count == ADAMW_TENSORS || groups + own > most) {

@@ -142,3 +142,25 @@ def test_loss_over_many_words(D):
         off = (part.double() - ref.repeat(-(-len(part) // PERIOD), 1)[:len(part)]).abs()
         good = off <= bound.repeat(-(-len(part) // PERIOD), 1)[:len(part)]
         assert bool((good.all(1) | ~kept[i:i + len(part)]).all()), f"dw of words {i} on"
+
+
+def test_adamw_of_a_tensor_past_a_launch(D):
+    """2^24 workgroups of 2048 values end a launch: a tensor of 2^35 + 5000 16-bit values, states in 8 bits (194 GB).  All
+    values are alike, so all parameters and all codes have to be."""
+    n = (1 << 35) + 5000
+    if torch.cuda.mem_get_info()[0] < 205 << 30:
+        pytest.skip("needs 205 GiB")
+    make = lambda k: ([torch.full((k,), 1.0, dtype=torch.bfloat16, device="cuda")], [torch.full((k,), 0.5, dtype=torch.bfloat16, device="cuda")])  # noqa: E731
+    small, large = (D.AdamWPlan(*make(k), state_bits=8) for k in (256, n))
+    for plan in (small, large):
+        D.densenet_adamw(plan, lr=0.125, step=1, seed=3)
+    step = 1 << 30
+    for what in ("p", "m", "v", "m_scale", "v_scale"):
+        got, want = (plan.params[0] if what == "p" else getattr(plan, what) for plan in (large, small))
+        got, want = (t.view(torch.uint8) if t.element_size() == 1 else t for t in (got, want))
+        value, off = float(want[0]), int((want != want[0]).sum())
+        assert off == 0 and value not in (0, 1)
+        got = got[:n] if what in "pmv" else got
+        for i in range(0, len(got), step):
+            off = int((got[i:i + step] != want[0]).sum())  # (not in the assertion, whose report would go through the values)
+            assert off == 0, f"{what}: {off} values of {i} on"
