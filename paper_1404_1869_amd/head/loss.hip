@@ -721,7 +721,8 @@ __device__ inline float weigh(const int64_t* __restrict__ label, const float* __
     for (int w = 1; w < 16; ++w) v = dloss ? fmaxf(v, s_red[w]) : v + s_red[w];
     int e = dloss && v > 0.f ? ilogbf(v) : 0;
     e = e < -100 ? -100 : e > 100 ? 100 : e;
-    const float by = !dloss || v == 0.f ? 1.f : by_largest ? fminf(fmaxf(v, 1e-37f), 1e37f) : ldexpf(1.f, e);
+    // (a factor in fp32's normal range: an infinite one would make NaN of all of dh and dw)
+    const float by = !dloss || v == 0.f ? 1.f : by_largest ? fminf(fmaxf(v, boost * 0x1p-126f), boost * 0x1p126f) : ldexpf(1.f, e);
     *mul = s_mul = boost / by;
     *unscale = dloss ? scale * (by / boost) : v > 0.f ? scale / (v * boost) : 0.f;
     *flag = 0;

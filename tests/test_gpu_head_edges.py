@@ -1,0 +1,69 @@
+"""The head's operators where their numbers run out of range: weights of rows far apart or next to nothing, infinities among
+words, batches that the gradient takes in pieces.  Against plain forms in 64 bits; tolerances as in test_gpu_head.py."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+UNIT = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f32": 1e-37, "f16": 2.0 ** -25, "bf16": 1e-37}
+
+
+@pytest.fixture(scope="module")
+def D():
+    from paper_1404_1869_amd import densenet
+    assert torch.cuda.is_available()
+    densenet.lib()
+    return densenet
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def normal(g, *shape, dt="f32", scale=1.0):
+    return (torch.randn(*shape, generator=g, device="cuda") * scale).to(DT[dt])
+
+
+def sum_err(k):
+    return (k / 8 + 16) * 2.0 ** -24
+
+
+def within(got, want, bound, what):
+    got, want = got.double(), want.double()
+    off = (got - want).abs()
+    bad = int((~(off <= bound)).sum())
+    assert bad == 0, f"{what}: {bad} of {off.numel()} off, by up to {float((off / bound).max()):.2f} bounds"
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("weight", [1e-45, 1e-38, 2.9e-36, 1e-30, 1.0, 1e30, 3e38])
+def test_weights_of_any_size(D, dt, weight):
+    """Rows' weights (dloss) from fp32's smallest to its largest value: gradients are finite, and those of weight 1 times it.
+    `scale` brings them back where it can.  g: its rounding (fp16: 2^-25 of values 2^10 times the weights over the largest, or
+    2^126 times the weights where that is less), and the exponent's error."""
+    n, C, V = 70, 64, 100
+    g = gen(1)
+    h, w = normal(g, n, C, dt=dt), normal(g, V, C, dt=dt, scale=0.5)
+    labels = torch.randint(0, V, (n,), generator=g, device="cuda")
+    _, lse = D.densenet_softmax_loss(h, w, labels)
+    part = torch.rand(n, generator=g, device="cuda") * 0.5 + 0.5
+    part[3] = 1
+    dloss = part * weight
+    scale = max(1.2e-38, min(1e38, 1 / weight))
+    c = dloss.double() * scale  # (as fp32 holds the weights: the smallest are 0 or one step)
+    dh, dw = D.densenet_softmax_loss_backward(h, w, labels, lse, dloss=dloss, scale=scale)
+    assert bool(dh.isfinite().all()) and bool(dw.isfinite().all())
+    p = torch.exp(h.double() @ w.double().T - lse.double()[:, None]) * c[:, None]
+    d = p.clone()
+    d[torch.arange(n, device="cuda"), labels] -= c
+    err = (6 if dt == "f32" else 1) * sum_err(C) * (h.double().abs() @ w.double().abs().T).amax(1)
+    off = (2.0 ** -22 if dt == "f32" else UNIT[dt]) * d.abs() + p * (2 * err + 2.0 ** -22 * (lse.double().abs() + 40))[:, None]
+    off = off + (2.0 ** -25 * max(2.0 ** -126 * scale, 2.0 ** -10 * float(c.max())) if dt == "f16" else 0)
+    many = 6 if dt == "f32" else 1
+    for got, a, b, e, k, what in ((dh, d, w.double(), off, V, "dh"), (dw, d.T, h.double(), off.T, n, "dw")):
+        want = a @ b
+        within(got, want, UNIT[dt] * want.abs() * 1.01 + e @ b.abs() + many * sum_err(k) * (a.abs() @ b.abs()) + TINY[dt], what)
