@@ -368,8 +368,8 @@ int densenet_softmax_loss(const void* d_h, int64_t h_stride, const void* d_w, in
 /* Gradient of the loss: g_nv = dloss_n (exp(l_nv - lse_n) - [v = label_n]), dh = g w, dw = g^T h, from the forward pass's
  * d_lse; the logits are computed again, a piece of the vocabulary at a time.  d_dloss: fp32 [n], or NULL for the mean over
  * the unmasked rows (1 / their number each); `scale` multiplies it.  Masked rows: dh = 0, and their h does not reach dw.
- * d_dh [n][C], d_dw [V][C]: `dtype`; dw is written, not added to.  g is rounded to `dtype` (16 bits: relative 2^-9 or 2^-12,
- * of the order of the rounding of dh and dw) between the products; fp32: of more than 64 rows and words, values of h, w and g
+ * d_dh [n][C], d_dw [V][C]: `dtype`; dw is written, not added to.  g is rounded to `dtype` between the products (16 bits: relative
+ * 2^-9 or 2^-12, of the order of the rounding of dh and dw; in fp16 2^-39 of the largest |dloss| where that is more); fp32: of more than 64 rows and words, values of h, w and g
  * are taken as three bf16 parts (24 bits; below 2^-110 fewer) and have to be finite.  Limits (DN_E_TOO_LARGE): those of the
  * loss, n <= 2^30 - 256, and n C and V C in tiles of 128 x 128 below 2^24 (of 2^38 values). */
 int densenet_softmax_loss_backward(const void* d_h, int64_t h_stride, const void* d_w, int64_t w_stride,

@@ -685,12 +685,17 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void join_logits_kernel(const fl
   }
 }
 
+// |g| <= FP16_BOOST: the coefficients are over the largest and |p - 1| <= 1; 65504 leaves room for p of up to 4, from an lse that
+// is off.  fp16's smallest step, 2^-24, is 2^-38 of the largest weight then: a row whose weight is 1e-6 of the largest keeps
+// probabilities of 5e-5 to 4 % (with 2^10 it lost them).
+constexpr float FP16_BOOST = 0x1p14f;
+
 // A row's part in the gradient, coef[n], and the factor that is left for the end, *unscale.  Without dloss every unmasked
 // row counts 1 and unscale is scale / (their number).  With it the rows keep dloss / 2^e in (-2, 2) for the largest
 // finite |dloss| in [2^e, 2^(e + 1)), or (by_largest, 16 bits) dloss over the largest: the heaviest row's g is then p - 1 at
 // its label, nearly exact in 16 bits, where 1.02 (p - 1) would carry one rounding of up to 2^-8 into all of dh (one row of
 // 5234 values over 12405 words: off by 2.9e-3 in all, 1.7e-3 now).  boost: a power of two that moves fp16's g away from its
-// smallest values.
+// smallest values, FP16_BOOST.
 // A workgroup of 1024 threads; returns the factor of the coefficients to all of them.
 __device__ inline float weigh(const int64_t* __restrict__ label, const float* __restrict__ dloss, int64_t n, int V, float scale,
                               float boost, bool by_largest, float* __restrict__ mul, float* __restrict__ unscale,
@@ -1368,7 +1373,7 @@ int launch_softmax_loss_backward(const LossArgs& a, dn_dtype dt, void* d_work, v
   const hipStream_t st = (hipStream_t)stream;
   if (b.how == WIDE) return backward<float, float>(a, dt, b, (char*)d_work, 1.f, st);
   if (dt == DN_F32) return backward<__bf16, float>(a, dt, b, (char*)d_work, 1.f, st);
-  if (dt == DN_F16) return backward<_Float16, _Float16>(a, dt, b, (char*)d_work, 1024.f, st);
+  if (dt == DN_F16) return backward<_Float16, _Float16>(a, dt, b, (char*)d_work, FP16_BOOST, st);
   return backward<__bf16, __bf16>(a, dt, b, (char*)d_work, 1.f, st);
 }
 

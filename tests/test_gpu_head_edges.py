@@ -67,3 +67,30 @@ def test_weights_of_any_size(D, dt, weight):
     for got, a, b, e, k, what in ((dh, d, w.double(), off, V, "dh"), (dw, d.T, h.double(), off.T, n, "dw")):
         want = a @ b
         within(got, want, UNIT[dt] * want.abs() * 1.01 + e @ b.abs() + many * sum_err(k) * (a.abs() @ b.abs()) + TINY[dt], what)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+def test_rows_of_light_weight_keep_their_gradient(D, dt):
+    """Weights from 1 to 1e-7 in one call, a vocabulary of 20000 words with a common mean, so that what g's small values add
+    up to is most of a row of dh.  Each row to its own size: half a unit of g, or half of fp16's smallest step of g times 2^14 over
+    the largest weight.  A call for each decade, whose `scale` brings its rows into fp16's range."""
+    n, C, V = 64, 64, 20000
+    g = gen(5)
+    w = (normal(g, V, C, scale=0.1) + normal(g, C)).to(DT[dt])
+    h, labels = normal(g, n, C, dt=dt, scale=0.1), torch.randint(0, V, (n,), generator=g, device="cuda")
+    dloss = torch.logspace(0, -7, n, device="cuda")
+    _, lse = D.densenet_softmax_loss(h, w, labels)
+    p = torch.exp(h.double() @ w.double().T - lse.double()[:, None]) * dloss.double()[:, None]
+    d = p.clone()
+    d[torch.arange(n, device="cuda"), labels] -= dloss.double()
+    err = sum_err(C) * (h.double().abs() @ w.double().abs().T).amax(1)
+    off = UNIT[dt] * d.abs() + p * (2 * err + 2.0 ** -22 * (lse.double().abs() + 40))[:, None]
+    if dt == "f16":
+        off = off + 2.0 ** -25 * 2.0 ** -14
+    for decade in range(8):
+        scale = 10.0 ** decade
+        dh, _ = D.densenet_softmax_loss_backward(h, w, labels, lse, dloss=dloss, scale=scale)
+        rows = (dloss * scale > 0.3) & (dloss * scale <= 3.001)
+        want = d[rows] @ w.double() * scale
+        bound = UNIT[dt] * want.abs() * 1.01 + scale * (off[rows] @ w.double().abs() + sum_err(V) * (d[rows].abs() @ w.double().abs())) + TINY[dt]
+        within(dh[rows], want, bound, f"dh of weights around 1e-{decade}")
