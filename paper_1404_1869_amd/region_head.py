@@ -13,12 +13,13 @@ trains a head to tell the regions of a synthetic image apart and prints its loss
 from __future__ import annotations
 
 import argparse
+import math
 
 from . import densenet as D
 
 
 class RegionHead:
-    """The head's parameters, gradients' buffers and optimiser states on one GPU."""
+    """The head's parameters, gradients' buffers (times ``scale``) and optimiser states on one GPU."""
 
     def __init__(self, words: int, length: int = 9216, dtype: int = D.DN_BF16, state_bits: int = 8, eps: float = 1e-6, seed: int = 0,
                  device="cuda"):
@@ -29,6 +30,9 @@ class RegionHead:
         self.w = torch.randn(words, length, generator=g, device=device) * (0.1 / length ** 0.5)
         low = D._tdtype(dtype)
         self.products = self.w if dtype == D.DN_F32 else self.w.to(low)  # what the products read
+        # fp16's gradients of a mean over many rows are next to nothing: they are taken times a power of two, and the optimiser
+        # divides by it.  A row of y is at most sqrt(length) |gamma|, and so dw at most half of fp16's range times |gamma|.
+        self.scale = 2.0 ** math.floor(math.log2(32768 / length ** 0.5)) if dtype == D.DN_F16 else 1.0
         self.dgamma, self.dw = torch.zeros_like(self.gamma), torch.zeros(words, length, dtype=low, device=device)
         copies = None if dtype == D.DN_F32 else [self.products]
         self.plans = (D.AdamWPlan([self.w], [self.dw], copies=copies, state_bits=state_bits),
@@ -43,11 +47,11 @@ class RegionHead:
         """One training step on the mean loss of the rows that have a label.  Returns the rows' losses before it."""
         y, _, _ = D.densenet_rms_norm(descriptors, self.gamma, eps=self.eps, out_dtype=self.dtype)
         loss, lse = D.densenet_softmax_loss(y, self.products, labels)
-        dy, _ = D.densenet_softmax_loss_backward(y, self.products, labels, lse, dw=self.dw)
+        dy, _ = D.densenet_softmax_loss_backward(y, self.products, labels, lse, scale=self.scale, dw=self.dw)
         D.densenet_rms_norm_backward(dy, descriptors, self.gamma, eps=self.eps, dgamma=self.dgamma)
         self.steps += 1
         for plan in self.plans:
-            D.densenet_adamw(plan, lr=lr, step=self.steps, weight_decay=weight_decay, seed=self.steps)
+            D.densenet_adamw(plan, lr=lr, step=self.steps, weight_decay=weight_decay, grad_scale=1 / self.scale, seed=self.steps)
         return loss
 
     def store(self, descriptors):

@@ -94,3 +94,32 @@ def test_rows_of_light_weight_keep_their_gradient(D, dt):
         want = d[rows] @ w.double() * scale
         bound = UNIT[dt] * want.abs() * 1.01 + scale * (off[rows] @ w.double().abs() + sum_err(V) * (d[rows].abs() @ w.double().abs())) + TINY[dt]
         within(dh[rows], want, bound, f"dh of weights around 1e-{decade}")
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16", "f32"])
+def test_region_head_gradients(D, dt):
+    """The first step's gradients of 2000 rows of 9216 over 20000 words, whose mean leaves values below fp16's smallest.  Off, as
+    a whole, by some roundings of terms of either sign: eight of `dt`'s (fp32: of 2^-20)."""
+    from paper_1404_1869_amd.region_head import RegionHead
+    n, C, V = 2000, 9216, 20000
+    desc = torch.relu(normal(gen(1), n, C, scale=2.0))
+    labels = torch.randint(-1, V, (n,), generator=gen(2), device="cuda")
+    head = RegionHead(V, C, dtype=D.DTYPES[dt], state_bits=32)
+    y, _, _ = D.densenet_rms_norm(desc, head.gamma, eps=head.eps, out_dtype=D.DTYPES[dt])
+    w, start = head.products.clone(), head.w.clone()
+    head.step(desc, labels)
+    has = labels >= 0
+    p = torch.softmax(y.double() @ w.double().T, 1)
+    p.scatter_add_(1, labels.clamp(min=0)[:, None], torch.full_like(p[:, :1], -1.0))
+    p *= (has.double() / int(has.sum()))[:, None]
+    dw = p.T @ y.double()
+    s = desc.double()
+    dgamma = ((p @ w.double()) * s / (s.square().mean(1, keepdim=True) + head.eps).sqrt()).sum(0)
+    scale = getattr(head, "scale", 1.0)
+    for got, want, what in ((head.dw, dw, "dw"), (head.dgamma, dgamma, "dgamma")):
+        off = float((got.double() / scale - want).norm() / want.norm())
+        assert off < 8 * max(UNIT[dt], 2.0 ** -20), f"{what} off by {off:.1e}"
+    # and the optimiser takes the scale back: m = (1 - beta1) gradient
+    m = head.plans[0].m[:V * C].view(V, C)
+    assert float((m.double() / 0.1 - dw).norm() / dw.norm()) < 8 * max(UNIT[dt], 2.0 ** -20)
+    assert not torch.equal(head.w, start)
