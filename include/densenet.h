@@ -357,8 +357,9 @@ int densenet_rms_norm_backward(const void* d_dy, int64_t dy_stride, dn_dtype dy_
  * outside [0, V) is masked: its loss and lse are 0, and nothing in its h reaches another row's results.
  * d_loss, d_lse: fp32 [n].  d_workspace: NULL for a size query into *bytes_needed (which depends on the pointers' alignment
  * and the strides: pass the same).  fp32: of more than 64 rows and words, rows are taken as two fp16 parts of a power of two
- * times the row (22 bits of every value down to 2^-16 of its row's largest, 2^-38 of that below) and have to be finite, or
- * their logits are NaN.  Limits (DN_E_TOO_LARGE): C <= 2^20; n, V <= 2^31 - 256; n V, n C and V C in tiles of 128 x 128
+ * times the row (22 bits of every value down to 2^-16 of its row's largest, 2^-38 of that below); of a word with infinities these
+ * alone count, by the sign of their sum (one masked by -infinity adds nothing), and an infinity in a row of h makes its results
+ * NaN.  Limits (DN_E_TOO_LARGE): C <= 2^20; n, V <= 2^31 - 256; n V, n C and V C in tiles of 128 x 128
  * below 2^31. */
 int densenet_softmax_loss(const void* d_h, int64_t h_stride, const void* d_w, int64_t w_stride,
                           const int64_t* d_label, int64_t n, int32_t C, int32_t V, dn_dtype dtype,

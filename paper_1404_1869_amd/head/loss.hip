@@ -438,8 +438,8 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) f[e] = m + e < g.M ? g.a_factor[m + e] : 0.f;
         }
-        // (one factor at a time a sum could pass fp32's range on its way to a logit within it; an infinite factor would make
-        // a NaN of a sum of 0)
+        // (one factor at a time a sum could pass fp32's range on its way to a logit within it; an infinite product of finite
+        // factors would make a NaN of a sum of 0; -infinity is the factor of a word with infinities)
 #pragma unroll
         for (int t = 0; t < TN; ++t)
 #pragma unroll
@@ -841,11 +841,15 @@ __global__ __launch_bounds__(256) void copy_rows_kernel(const float* __restrict_
 }
 
 // fp32 rows as two fp16 parts [2][rows][ldo] of x 2^k and a factor 2^-k, one workgroup per row; with `three` also as three bf16
-// parts [3][rows][ldo].  Rows whose label is outside [0, V) become 0 (label may be null).  A row that is not finite keeps k = 0
-// and so its infinities and NaN.
+// parts [3][rows][ldo].  Rows whose label is outside [0, V) become 0 (label may be null).  A row with a NaN keeps it.  Of a word
+// (words) with infinities only these count, as +-2^13 without a second part, and the factor is infinite: logits are infinite by
+// the sign of their sum, so a word masked by -infinity is one that no row reaches.  (Both signs are turned: -infinity as the
+// factor tells it from products of factors past fp32's range.)  A row of h with infinities keeps them in both parts, inf and
+// NaN: its logits are NaN.
 __global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict__ in, int64_t ld, int C, _Float16* __restrict__ out,
                                                          int64_t ldo, int64_t part, float* __restrict__ factor,
-                                                         __bf16* __restrict__ three, const int64_t* __restrict__ label, int V) {
+                                                         __bf16* __restrict__ three, const int64_t* __restrict__ label, int V,
+                                                         bool words) {
   __shared__ float s_top[4];
   const int64_t row = blockIdx.x;
   const float* x = in + row * ld;
@@ -866,8 +870,9 @@ __global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict
   top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
   int k = 0;
   if (!zero && top > 0.f && top < INFINITY) k = 13 - max(ilogbf(top), -100);
+  const bool infinite = words && top == INFINITY;
   const float mul = ldexpf(1.f, k);
-  if (threadIdx.x == 0) factor[row] = ldexpf(1.f, -k);
+  if (threadIdx.x == 0) factor[row] = infinite ? -INFINITY : ldexpf(1.f, -k);
   for (int c = threadIdx.x * 8; c < ldo; c += 2048) {
     float v[8], w[8], lo[8];
     if (c == (int)threadIdx.x * 8) {
@@ -880,6 +885,7 @@ __global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict
     for (int j = 0; j < 8; ++j) {
       v[j] = zero ? 0.f : v[j];
       w[j] = v[j] * mul;
+      if (infinite) w[j] = v[j] != v[j] ? v[j] : fabsf(v[j]) == INFINITY ? copysignf(8192.f, -v[j]) : 0.f;
       lo[j] = w[j] - (float)(_Float16)w[j];
     }
     store8(out + row * ldo + c, w);
@@ -998,6 +1004,7 @@ struct Matrix {
 enum Layout { AS_IS, WIDE, THREE, TWO };
 struct Pack {
   bool copy;       // laid out in the workspace
+  bool words;      // w, not h
   Layout how;
   int64_t rows, ld;  // elements of a row there
   size_t at, factor_at;
@@ -1073,6 +1080,7 @@ FwdPlan plan_forward(const LossArgs& a, dn_dtype dt) {
   f.how = dt != DN_F32 ? AS_IS : a.n <= FEW || a.V <= FEW ? WIDE : TWO;
   f.h = plan_pack(a.h, a.h_stride, a.n, a.C, dt, f.how, false, w);
   f.w = plan_pack(a.w, a.w_stride, a.V, a.C, dt, f.how, false, w);
+  f.w.words = true;
   f.products = f.how == TWO ? 3 : 1;
   Tile of[2];
   const int tiles = logit_tiles(a.V, a.n, of);
@@ -1123,6 +1131,7 @@ BackPlan plan_backward(const LossArgs& a, dn_dtype dt) {
   if (b.logits == TWO) {
     b.lh = plan_pack(a.h, a.h_stride, a.n, a.C, dt, TWO, true, w);
     b.lw = plan_pack(a.w, a.w_stride, a.V, a.C, dt, TWO, true, w);
+    b.lw.words = true;
   }
   const int64_t v256 = up(a.V, 256);
   b.vc = std::min(v256, std::max<int64_t>(256, PIECE_BYTES / (2 * b.unit * a.n) / 256 * 256));
@@ -1165,7 +1174,7 @@ int lay_out(const Pack& k, const void* p, int64_t ld, int32_t C, dn_dtype dt, co
     for (int64_t at = 0; at < k.rows; at += most) {
       split_rows_kernel<<<dim3((unsigned)std::min(k.rows - at, most)), 256, 0, st>>>(
           (const float*)p + at * ld, ld, C, (_Float16*)m.p + at * k.ld, k.ld, m.part, (float*)m.factor + at,
-          three ? (__bf16*)(work + three->at) + at * k.ld : nullptr, label ? label + at : nullptr, V);
+          three ? (__bf16*)(work + three->at) + at * k.ld : nullptr, label ? label + at : nullptr, V, k.words);
       if (const int err = (int)hipGetLastError()) return err;
     }
     return 0;

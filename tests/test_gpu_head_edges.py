@@ -123,3 +123,44 @@ def test_region_head_gradients(D, dt):
     m = head.plans[0].m[:V * C].view(V, C)
     assert float((m.double() / 0.1 - dw).norm() / dw.norm()) < 8 * max(UNIT[dt], 2.0 ** -20)
     assert not torch.equal(head.w, start)
+
+
+@pytest.mark.parametrize("n,V", [(10, 200), (100, 60), (100, 200), (300, 3000), (500, 1000)])
+def test_fp32_words_of_minus_infinity(D, n, V):
+    """Words masked by -infinity in one value (h is positive there), in every layout of fp32 operands: no row reaches them, and
+    the loss is that of the other words.  Where it is one of theirs that is the label, the loss is infinite; a word of +infinity
+    and a NaN make it NaN."""
+    C = 72
+    g = gen(n)
+    h, w = normal(g, n, C), normal(g, V, C, scale=0.3)
+    h[:, 5] = h[:, 5].abs() + 0.1
+    gone = torch.arange(7, V, 13, device="cuda")
+    keep = torch.ones(V, dtype=torch.bool, device="cuda")
+    keep[gone] = False
+    labels = keep.nonzero()[torch.randint(0, int(keep.sum()), (n,), generator=g, device="cuda"), 0]
+    w[gone, 5] = -math.inf
+    loss, lse = D.densenet_softmax_loss(h, w, labels)
+    logits = h.double() @ w[keep].double().T
+    want = torch.logsumexp(logits, 1)
+    at = (h.double() * w[labels].double()).sum(1)
+    err = 6 * sum_err(C) * (h.double().abs() @ w[keep].double().abs().T).amax(1)
+    tol = 2 * err + 2.0 ** -21 * (want.abs() + 16)
+    within(lse, want, tol, "lse")
+    within(loss, want - at, 2 * tol, "loss")
+    if n > 64 and V > 64:  # (as they lie, dh holds 0 times -infinity; in two parts g is 0 and so is the word's gradient)
+        _, dw = D.densenet_softmax_loss_backward(h, w, labels, lse)
+        assert n < 400 or not bool(dw[gone].any())
+    one = labels.clone()
+    one[3] = int(gone[0])
+    loss, lse2 = D.densenet_softmax_loss(h, w, one)
+    assert float(loss[3]) == math.inf and bool(loss.isfinite().sum() == n - 1) and torch.equal(lse, lse2)
+    w[gone[0], 5] = math.inf
+    loss, _ = D.densenet_softmax_loss(h, w, labels)
+    assert not bool(loss.isfinite().any())
+    w[gone[0], 5] = math.nan
+    loss, _ = D.densenet_softmax_loss(h, w, labels)
+    assert bool(loss.isnan().all())
+    w[gone, 5] = 0
+    h[4, 9] = math.inf
+    loss, _ = D.densenet_softmax_loss(h, w, labels)
+    assert not bool(loss[4].isfinite()) and int(loss.isfinite().sum()) == n - 1
