@@ -2,6 +2,7 @@
 // host before any device work is enqueued.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "head.h"
@@ -112,7 +113,8 @@ int densenet_rms_norm_backward(const void* d_dy, int64_t dy_stride, dn_dtype dy_
     if (n > MAX_ROWS) return fail(DN_E_TOO_LARGE, "too many rows");
     if (!(eps >= 0) || std::isinf(eps)) return fail(DN_E_INVALID_ARG, "eps must be finite and >= 0");
     const int32_t groups = norm_back_groups(n, C);
-    const size_t need = 4 * (size_t)groups * C;
+    // (never 0, so that a caller's workspace is never the null pointer of a size query: without rows, dgamma is still to be written)
+    const size_t need = 4 * (size_t)std::max(groups, 1) * C;
     int st;
     if ((st = check_work(d_workspace, workspace_bytes, need, bytes_needed)) || !d_workspace) return st;
     const size_t e = dtype_size(dtype);

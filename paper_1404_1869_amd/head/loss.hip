@@ -1352,7 +1352,8 @@ size_t softmax_loss_bytes(const LossArgs& a, dn_dtype dt) {
   const int64_t rows = forward_rows(a), last = (a.n - 1) / rows * rows;  // all pieces but the last are alike
   return std::max(plan_forward(forward_piece(a, dt, 0, rows), dt).total, plan_forward(forward_piece(a, dt, last, rows), dt).total);
 }
-size_t softmax_loss_backward_bytes(const LossArgs& a, dn_dtype dt) { return a.n ? plan_backward(a, dt).total : 0; }
+// (never 0, so that a caller's workspace is never the null pointer of a size query: without rows, dw is still to be written)
+size_t softmax_loss_backward_bytes(const LossArgs& a, dn_dtype dt) { return a.n ? plan_backward(a, dt).total : 256; }
 
 int launch_softmax_loss(const LossArgs& a, dn_dtype dt, void* d_work, void* stream) {
   const hipStream_t st = (hipStream_t)stream;

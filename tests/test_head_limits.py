@@ -46,3 +46,12 @@ def test_a_piece_of_few_rows_has_its_own_workspace():
         assert loss(n, 8, 3000, D.DN_F32, need) == D.DN_OK
         sizes.append(need.value)
     assert sizes[1] <= sizes[0] * 1.01 and sizes[1] >= sizes[2] * 0.99
+
+
+def test_gradients_of_no_rows_ask_for_a_workspace():
+    """A null workspace is a size query, so a call that has dw or dgamma to write must not be told that it needs none."""
+    need = ctypes.c_size_t(0)
+    assert loss_back(0, 8, 10, D.DN_BF16, need) == D.DN_OK and need.value > 0
+    need.value = 0
+    assert D.lib().densenet_rms_norm_backward(P, 8, D.DN_F32, P, 8, None, 0, None, 0, 8, D.DN_F32, 1e-6, P, 8, P, None, 0,
+                                              ctypes.byref(need), None) == D.DN_OK and need.value > 0
