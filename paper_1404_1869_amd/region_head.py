@@ -80,6 +80,8 @@ def main(argv=None):
     ap.add_argument("--boxes", type=int, default=2000)
     ap.add_argument("--steps", type=int, default=20)
     args = ap.parse_args(argv)
+    if min(args.words, args.boxes, args.steps) < 1:
+        ap.error("--words, --boxes and --steps must be at least 1")
     desc = image_descriptors(args.boxes)
     labels = torch.arange(args.boxes, device="cuda") % args.words
     head = RegionHead(args.words, desc.shape[1])

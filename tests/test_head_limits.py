@@ -55,3 +55,12 @@ def test_gradients_of_no_rows_ask_for_a_workspace():
     need.value = 0
     assert D.lib().densenet_rms_norm_backward(P, 8, D.DN_F32, P, 8, None, 0, None, 0, 8, D.DN_F32, 1e-6, P, 8, P, None, 0,
                                               ctypes.byref(need), None) == D.DN_OK and need.value > 0
+
+
+@pytest.mark.parametrize("option", ["--words", "--boxes", "--steps"])
+def test_example_refuses_nothing_to_do(option, capsys):
+    pytest.importorskip("torch")
+    from paper_1404_1869_amd import region_head
+    with pytest.raises(SystemExit) as e:
+        region_head.main([option, "0"])
+    assert e.value.code == 2 and "at least 1" in capsys.readouterr().err
