@@ -5,6 +5,8 @@ import math
 import pytest
 
 torch = pytest.importorskip("torch")
+import test_gpu_head as base  # noqa: E402
+
 pytestmark = pytest.mark.gpu
 
 DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
@@ -164,3 +166,36 @@ def test_fp32_words_of_minus_infinity(D, n, V):
     h[4, 9] = math.inf
     loss, _ = D.densenet_softmax_loss(h, w, labels)
     assert not bool(loss[4].isfinite()) and int(loss.isfinite().sum()) == n - 1
+
+
+@pytest.mark.parametrize("n,C,V,dt,per_row", [(20000, 40, 30000, "bf16", False), (17000, 72, 20011, "f16", True), (20000, 24, 15013, "f32", True),
+                                              (64, 24, 2100000, "f32", False), (100, 16, 2700000, "f32", True), (40, 16, 7000003, "bf16", True)])
+def test_gradient_in_pieces_of_the_vocabulary(D, n, C, V, dt, per_row):
+    """More words than one piece of g holds (2^28 values in 16 bits; fp32 of few rows 2^27), in each layout: labels, factors and
+    sums go on from piece to piece."""
+    torch.cuda.empty_cache()
+    assert n * V > 1 << (27 if dt == "f32" and n <= 64 else 28)
+    base.test_loss_gradient(D, n, C, V, dt, 0, 0, per_row)
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n", [100, 450])
+def test_fp32_gradient_holds_fp32(D, n):
+    """dh and dw of fp32 to 2^-21 of their terms, which takes all six products of the bf16 parts (of each of the three smaller
+    ones some terms hold over 2^-20).  Row i's softmax is all on word i (logits 256 and 0), its label is word i + 1, so g is
+    +-dloss in two places; words and rows meet in columns of their own.  What is left out is below 2^-24; the sums of a result's two
+    terms, and its factor, round six times to 2^-24."""
+    K = 64
+    g = gen(n)
+    h, w = torch.zeros(n, n + 2 * K, device="cuda"), torch.zeros(n, n + 2 * K, device="cuda")
+    at = torch.arange(n, device="cuda")
+    h[at, at] = w[at, at] = 16
+    w[:, n:n + K], h[:, n + K:] = normal(g, n, K), normal(g, n, K)
+    labels, dloss = (at + 1) % n, normal(g, n)
+    dh, dw = D.densenet_softmax_loss_backward(h, w, labels, torch.full((n,), 256.0, device="cuda"), dloss=dloss)
+    c, W, H = dloss.double()[:, None], w.double(), h.double()
+    want, terms = c * (W - W[labels]), c.abs() * (W.abs() + W[labels].abs())
+    within(dh, want, 2.0 ** -21 * terms, "dh")
+    want, terms = c * H, (c * H).abs()
+    back = (at - 1) % n  # the row whose label the word is
+    within(dw, want - want[back], 2.0 ** -21 * (terms + terms[back]), "dw")
