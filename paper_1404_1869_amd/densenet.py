@@ -652,6 +652,8 @@ def _rows(t, what, shape=None, dtype=None, device=None):
                    f"{tuple(size)}")
     if dtype is not None and t.dtype != dtype:
         raise _bad(f"{what}: {dtype} expected, not {t.dtype}")
+    if size[1] >= 1 << 31:  # (a C int would take the low 32 bits)
+        raise DenseNetError(DN_E_TOO_LARGE, f"{what}: rows of {size[1]} values")
     if (t.device != device) if device is not None else not t.is_cuda:
         raise _bad(f"{what}: not on the operands' GPU")
     row, col = t.stride()
@@ -759,6 +761,8 @@ def _loss_operands(h, w, labels):
     if w.dim() != 2:
         raise _bad("w: a matrix expected")
     V = w.shape[0]
+    if V >= 1 << 31:
+        raise DenseNetError(DN_E_TOO_LARGE, f"w: {V} words")
     wp, ws = _rows(w, "w", (V, C), h.dtype, dev)
     return (hp, hs, wp, ws, _vector(labels, "labels", n, torch.int64, dev)), n, C, V, dt, dev
 

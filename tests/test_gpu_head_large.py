@@ -164,3 +164,17 @@ def test_adamw_of_a_tensor_past_a_launch(D):
         for i in range(0, len(got), step):
             off = int((got[i:i + step] != want[0]).sum())  # (not in the assertion, whose report would go through the values)
             assert off == 0, f"{what}: {off} values of {i} on"
+
+
+def test_binding_refuses_sizes_past_32_bits(D):
+    """C and V are 32-bit arguments: sizes of 2^32 and some must not pass as the some."""
+    words = torch.empty((1 << 32) + 5, 1, dtype=torch.bfloat16, device="cuda")
+    h, labels = torch.zeros(3, 1, dtype=torch.bfloat16, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    lse = torch.zeros(3, device="cuda")
+    row = words[:(1 << 32) + 3].view(1, -1)
+    for call in (lambda: D.densenet_softmax_loss(h, words, labels), lambda: D.densenet_softmax_loss_backward(h, words, labels, lse, dw=words),
+                 lambda: D.densenet_rms_norm(row, out=row), lambda: D.densenet_rms_norm_backward(row, row, dx=row),
+                 lambda: D.densenet_softmax_loss(row, row, labels[:1])):
+        with pytest.raises(D.DenseNetError) as e:
+            call()
+        assert e.value.status == D.DN_E_TOO_LARGE
