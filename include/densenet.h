@@ -387,9 +387,10 @@ int densenet_softmax_loss_backward(const void* d_h, int64_t h_stride, const void
  * n in the last one unused; ranges of different tensors must not meet.  n_blocks: blocks that d_m and d_v hold; both are
  * aligned to 16 bytes.
  * state_bits 32: fp32 m and v.  state_bits 8: DN_F8 codes of m and of sqrt(v), with a scale a block in d_m_scale and
- * d_v_scale (fp32 [n_blocks]); value = code * scale, scale = the block's largest magnitude / 448.  A value between two codes
- * takes the upper one with the chance of its place between them, by a hash of its place in the states and of `seed`
- * (use another seed every step); a sqrt(v) above 0 is stored as at least the smallest code.  All zeros: a fresh state. */
+ * d_v_scale (fp32 [n_blocks]); value = code * scale, scale = the block's largest finite magnitude / 448 (an infinity becomes a
+ * NaN code).  A value between two codes takes the upper one with the chance of its place between them, by a hash of its place
+ * in the states and of `seed` (use another seed every step); a sqrt(v) above 0 is stored as at least the smallest code.  All
+ * zeros: a fresh state. */
 typedef struct {
   void* p;
   const void* g;

@@ -90,8 +90,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamWArgs a) {
     const float root = sqrtf(v);
     r[j] = BITS8 ? root : v;
     p[j] = p[j] * a.decay - a.rate * m[j] / (root * a.root + a.eps);
-    m_top = fmaxf(m_top, fabsf(m[j]));
-    r_top = fmaxf(r_top, r[j]);
+    if constexpr (BITS8) {  // an infinity is stored as NaN, and counts for no scale: it would take its whole block along
+      m[j] = fabsf(m[j]) < INFINITY ? m[j] : NAN;
+      r[j] = r[j] < INFINITY ? r[j] : NAN;
+      m_top = fmaxf(m_top, fabsf(m[j]));
+      r_top = fmaxf(r_top, r[j]);
+    }
   }
   store8(p_at, i, left, p);
   if (t.copy) store8((Q*)t.copy + base, i, left, p);

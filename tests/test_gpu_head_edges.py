@@ -199,3 +199,29 @@ def test_fp32_gradient_holds_fp32(D, n):
     want, terms = c * H, (c * H).abs()
     back = (at - 1) % n  # the row whose label the word is
     within(dw, want - want[back], 2.0 ** -21 * (terms + terms[back]), "dw")
+
+
+def test_infinite_gradient_spoils_its_own_value_only(D):
+    """8-bit states share a scale: an infinite (and a NaN) gradient must not reach its block's other values, in the step itself or
+    in those that follow from the states."""
+    n = 700
+    g = gen(3)
+    p, grads = normal(g, n), [normal(g, n, scale=0.01) for _ in range(3)]
+    grads[0][[5, 300, 699]] = 0
+    runs = []
+    for values in ((0.0, 0.0, 0.0), (math.inf, math.nan, -math.inf)):
+        plan = D.AdamWPlan([p.clone()], [grads[0].clone()], state_bits=8)
+        for i, x in zip((5, 300, 699), values):
+            plan.grads[0][i] = x
+        for step in (1, 2, 3):
+            if step > 1:
+                plan.grads[0].copy_(grads[step - 1])
+                plan.grads[0][[5, 300, 699]] = 0
+            D.densenet_adamw(plan, lr=1e-2, step=step, seed=step)
+        runs.append((plan.params[0], plan.m.view(torch.uint8)[:n], plan.v.view(torch.uint8)[:n], plan.m_scale, plan.v_scale))
+    kept = torch.ones(n, dtype=torch.bool, device="cuda")
+    kept[[5, 300, 699]] = False
+    for a, b in zip(*runs):
+        kept_of = kept if len(a) == n else slice(None)
+        assert torch.equal(a[kept_of], b[kept_of])
+    assert bool(runs[1][0][~kept].isnan().all()) and bool(runs[0][0].isfinite().all())
