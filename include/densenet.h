@@ -354,7 +354,8 @@ int densenet_rms_norm_backward(const void* d_dy, int64_t dy_stride, dn_dtype dy_
 
 /* Softmax cross entropy of n rows h [n][C] over the products with w [V][C] (both `dtype`), the logits not kept:
  * l_nv = h_n . w_v, lse_n = log sum_v exp l_nv, loss_n = lse_n - l_n,label.  d_label: int64 [n]; a row whose label lies
- * outside [0, V) is masked: its loss and lse are 0, and nothing in its h reaches another row's results.
+ * outside [0, V) is masked: its loss and lse are 0, and nothing in its h reaches another row's results.  Logits of 2^127 and
+ * more in magnitude may count as infinite.
  * d_loss, d_lse: fp32 [n].  d_workspace: NULL for a size query into *bytes_needed (which depends on the pointers' alignment
  * and the strides: pass the same).  fp32: of more than 64 rows and words, rows are taken as two fp16 parts of a power of two
  * times the row (22 bits of every value down to 2^-16 of its row's largest, 2^-38 of that below); of a word with infinities these
@@ -369,10 +370,11 @@ int densenet_softmax_loss(const void* d_h, int64_t h_stride, const void* d_w, in
 /* Gradient of the loss: g_nv = dloss_n (exp(l_nv - lse_n) - [v = label_n]), dh = g w, dw = g^T h, from the forward pass's
  * d_lse; the logits are computed again, a piece of the vocabulary at a time.  d_dloss: fp32 [n], or NULL for the mean over
  * the unmasked rows (1 / their number each); `scale` multiplies it.  Masked rows: dh = 0, and their h does not reach dw.
- * d_dh [n][C], d_dw [V][C]: `dtype`; dw is written, not added to.  g is rounded to `dtype` between the products (16 bits: relative
- * 2^-9 or 2^-12, of the order of the rounding of dh and dw; in fp16 2^-39 of the largest |dloss| where that is more); fp32: of more than 64 rows and words, values of h, w and g
- * are taken as three bf16 parts (24 bits; below 2^-110 fewer) and have to be finite.  Limits (DN_E_TOO_LARGE): those of the
- * loss, n <= 2^30 - 256, and n C and V C in tiles of 128 x 128 below 2^24 (of 2^38 values). */
+ * d_dh [n][C], d_dw [V][C]: `dtype`; dw is written, not added to.  g is rounded to `dtype` between the products (16 bits:
+ * relative 2^-9 or 2^-12, of the order of the rounding of dh and dw; in fp16 2^-39 of the largest |dloss| where that is more);
+ * fp32: of more than 64 rows and words, values of h, w and g are taken as three bf16 parts (24 bits; below 2^-110 fewer) and
+ * have to be finite.  Limits (DN_E_TOO_LARGE): those of the loss, n <= 2^30 - 256, and n C and V C in tiles of 128 x 128 below
+ * 2^24 (of 2^38 values). */
 int densenet_softmax_loss_backward(const void* d_h, int64_t h_stride, const void* d_w, int64_t w_stride,
                                    const int64_t* d_label, const float* d_lse, const float* d_dloss,
                                    float scale, int64_t n, int32_t C, int32_t V, dn_dtype dtype, void* d_dh,

@@ -8,7 +8,7 @@
 //  logits: rows as two fp16 parts, x 2^k = a + b with 2^k such that the row's largest value lies in [2^13, 2^14), and three
 //    products a a' + a b' + b a'.  a and b hold 22 bits of a value down to 2^-16 of the row's largest (half of b's smallest
 //    step is 2^-25, 2^-38 of the largest); what is left out is at most 2^-22 of a product and of either sign, as an fp32
-//    product's and sum's roundings.  The row factors are powers of two.
+//    product's and sum's roundings.  The row factors are powers of two (a word with infinities: see split_rows_kernel).
 //  dh, dw: the sums run across rows, which have no common factor: three bf16 parts of every value (h, w, g) and six products,
 //    as the library's fp32 convolutions.
 //  up to 64 rows, or 64 words: bound by reading w, or h, which fp32 MFMAs keep up with: all products on the values as they lie.
@@ -20,10 +20,10 @@
 // over different axes; pieces of 2^29 bytes of it (of 2^27, 28, 29, 30 bytes, 16384 rows over 65536 words took 13.0, 12.5,
 // 12.4, 12.3 ms in one version).  Partial sums of splits and pieces have slabs of their own, added in order: no atomics, the
 // same bits every time.
-// Bound by the matrix cores at the clock that the chip's power allows: the products of 16384 x 16384 x 2048 in bf16 take 976, 884
-// and 842 us (1.13, 1.24, 1.31 PFLOP/s; a library's large product 1.38), their MFMA pipes 58 to 69 % busy at 1.85 to 1.79 GHz.
-// Gradients of 16384 x 2048 over 65536 words 10.9 ms (1.21 PFLOP/s), 4096 x 2048 over 32000 1.35 ms (1.19), loss of 2000 x 2048
-// over 50257 words in fp16 386 us (1.07; 1576 tiles are 6.2 rounds of workgroups), of one row x 4096 over 32000 words 61 us
+// Bound by the matrix cores at the clock that the chip's power allows: the products of 16384 x 16384 x 2048 in bf16 take 998, 898
+// and 849 us (1.10, 1.22, 1.29 PFLOP/s; a library's large product 1.38), their MFMA pipes 58 to 68 % busy at 1.89 to 1.84 GHz.
+// Gradients of 16384 x 2048 over 65536 words 11.0 ms (1.20 PFLOP/s), 4096 x 2048 over 32000 1.38 ms (1.17), loss of 2000 x 2048
+// over 50257 words in fp16 390 us (1.06; 1576 tiles are 6.2 rounds of workgroups), of one row x 4096 over 32000 words 61 us
 // (bound by memory: 4.3 TB/s), of 32000 x 9216 over 21 words 109 us (5.4 TB/s).
 #include <hip/hip_runtime.h>
 

@@ -5,8 +5,9 @@
 // All of it is computed in 32 bits from the unrounded sum s and rounded once, when a result is stored.
 // Bound by memory: a row is read once, kept in registers over its reductions, and written once; the gradient sums dgamma in
 // registers over a workgroup's rows and then over the workgroups in a fixed order.  A large copy moves 5.08 TB/s on this card;
-// measured: 2000 rows of 9216 fp32 values to 8 bits 18.5 us (5.0 TB/s), 8191 unaligned rows of 2047 fp16 values with residual
-// 28.2 us (4.8), the gradient of 32000 rows of 4096 bf16 values with dsum 207 us (5.1).
+// measured: 2000 rows of 9216 fp32 values to 8 bits 18.4 us (5.0 TB/s; a scale for every 32, 64 or 128 values: the same), 8191
+// unaligned rows of 2047 fp16 values with residual 28.1 us (4.8), the gradient of 32000 rows of 4096 bf16 values with dsum 207 us
+// (5.1).
 #include <hip/hip_runtime.h>
 
 #include "head.h"
