@@ -87,9 +87,7 @@ template <typename T, bool AT, bool BT, int BM, int BN, int WM, int WN, int NST,
 __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
   constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
   constexpr bool MULTI = std::is_same<O, float>::value && !std::is_same<T, float>::value;  // parts of fp32 values
-  using OA = Operand<T, AT, BM, NW>;
-  using OB = Operand<T, BT, BN, NW>;
-  constexpr int STAGE = OA::BYTES + OB::BYTES, PER = OA::PER + OB::PER;
+  constexpr int STAGE = Operand<T, AT, BM, NW>::BYTES + Operand<T, BT, BN, NW>::BYTES;
   constexpr int WROWS = BN / WN, WCOLS = BM / WM;
   // A wave's 32 rows x WCOLS results on their way out, rows 16 bytes apart in banks
   constexpr int OUT_SIZE = E == E_SLAB || (E == E_OUT ? std::is_same<O, float>::value : std::is_same<T, float>::value) ? 4 : 2;
@@ -109,141 +107,11 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(GemmArgs g) {
   const int tile_m = in / width, tile_n = col * COL + in % width;
   const int m0 = tile_m * BM, n0 = tile_n * BN;
 
-  OA oa;
-  OB ob;
   const bool alt = AT && BT && g.alt && *g.alt;
-  oa.init(alt ? g.a_alt : g.a, alt ? g.lda_alt : g.lda, m0, g.a_rows, wave, lane);
-  ob.init(g.b, g.ldb, n0, g.b_rows, wave, lane);
-  Fragments<T, AT, BM, TM> fa;
-  Fragments<T, BT, BN, TN> fb;
-  fa.init(wm * WCOLS, lane);
-  fb.init(wn * WROWS, lane);
-
-  const int kt = (g.K + BK - 1) / BK, total = MULTI ? kt * g.products : kt;
-  const int s0 = (int)((int64_t)total * split / g.splits), s1 = (int)((int64_t)total * (split + 1) / g.splits);
-  auto load = [&](int s, int buf) {
-    // products of parts from the smallest to the largest, the last `products` of (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
-    const int turn = MULTI ? s / kt : 0, pr = MULTI ? 6 - g.products + turn : 5, k0 = (s - turn * kt) * BK;
-    const int pa = pr == 0 ? 2 : pr == 1 || pr == 3 ? 1 : 0, pb = pr == 2 ? 2 : pr == 1 || pr == 4 ? 1 : 0;
-    char* at = s_mem + buf * STAGE;
-    oa.load(at, pa * g.a_part, k0, g.K, wave);
-    ob.load(at + OA::BYTES, pb * g.b_part, k0, g.K, wave);
-  };
-
   f32x16 acc[TM][TN];
-#pragma unroll
-  for (int a = 0; a < TM; ++a)
-#pragma unroll
-    for (int t = 0; t < TN; ++t) acc[a][t] = f32x16{};
-
-  typename Mfma<T>::frag a[2][TM], b[2][TN];
-  auto mma = [&](int h) {
-#pragma unroll
-    for (int t = 0; t < TN; ++t)
-#pragma unroll
-      for (int i = 0; i < TM; ++i) acc[i][t] = Mfma<T>::mma(a[h][i], b[h][t], acc[i][t]);
-  };
-  if constexpr (NW == 8) {
-    // Two waves per SIMD, in turns: while waves 0..3 run the MFMAs of half a stage, waves 4..7 read their next half's
-    // fragments and send off loads, and the other way round, a barrier between the turns (waves 4..7 are one turn late).
-    // Turn 4 s: waves 0..3 read the first half of stage s and load stage s + 1 into the other buffer, which the last turn
-    // of stage s - 1 has left; 4 s + 1: waves 4..7 do; 4 s + 3: the last reads of stage s, and the loads have come.
-    const bool late = wave >= 4;
-    auto turn = [&]() {
-      __builtin_amdgcn_sched_barrier(0);
-      wave_barrier();
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    auto compute = [&]() {
-      __builtin_amdgcn_s_setprio(1);
-      mma(0);
-      mma(1);
-      __builtin_amdgcn_s_setprio(0);
-    };
-    if (s1 > s0) load(s0, 0);
-    wait_loads<0>();
-    turn();
-    if (late) turn();
-    for (int s = s0; s < s1; ++s) {
-      const int buf = (s - s0) & 1;
-      const char* at = s_mem + buf * STAGE;
-      // (the turned operands' reads end in a wait, so the loads go out first; plain ones' go after the reads: g of 16384 x 16384
-      // x 2048 992 us, the other way 1075)
-      if ((AT || BT) && s + 1 < s1) load(s + 1, buf ^ 1);
-      fb.template read<0>(at + OA::BYTES, b);
-      fa.template read<0>(at, a);
-      if (!(AT || BT) && s + 1 < s1) load(s + 1, buf ^ 1);
-      wait_lds();
-      turn();
-      compute();
-      turn();
-      fb.template read<1>(at + OA::BYTES, b);
-      fa.template read<1>(at, a);
-      if (late) wait_loads<0>();
-      else wait_lds();
-      turn();
-      compute();
-      if (!late) wait_loads<0>();
-      turn();
-    }
-    if (!late) turn();
-  } else if (s1 > s0) {
-    // Stage s computes from buffer (s - s0) % NST while the next NST - 1 stages' loads are on their way.  Once every wave
-    // holds the rest of the stage in registers, its buffer takes the loads of stage s + NST.  The workgroups of a CU cover
-    // each other's waits.
-#pragma unroll
-    for (int i = 0; i < NST; ++i)
-      if (s0 + i < s1) load(s0 + i, i);
-    if (s1 - s0 >= NST) wait_loads<PER * (NST - 1)>();
-    else wait_loads<0>();
-    wave_barrier();
-    auto next_stage = [&](int s, int buf) {
-      if (NST > 2 && s + NST <= s1) wait_loads<PER * (NST > 2 ? NST - 2 : 0)>();
-      else wait_loads<0>();
-      wave_barrier();
-      if (s + NST < s1) load(s + NST, buf);
-    };
-    int buf = 0;
-    if constexpr (AT || BT) {
-      for (int s = s0; s < s1; ++s) {
-        const char* at = s_mem + buf * STAGE;
-        fb.template read<0>(at + OA::BYTES, b);
-        fa.template read<0>(at, a);
-        mma(0);
-        mma(1);
-        fb.template read<1>(at + OA::BYTES, b);
-        fa.template read<1>(at, a);
-        if (s + 1 < s1) next_stage(s, buf);
-        mma(0);
-        mma(1);
-        buf = buf + 1 == NST ? 0 : buf + 1;
-      }
-    } else {
-      // plain operands: a wave reads the fragments of k-step j + 1 while the MFMAs of k-step j run, across stages too
-      auto step = [&](auto j, const char* at) {
-        constexpr int J = decltype(j)::value;
-        fa.template read_step<J>(at, a[J & 1]);
-        fb.template read_step<J>(at + OA::BYTES, b[J & 1]);
-      };
-      step(std::integral_constant<int, 0>{}, s_mem);
-      for (int s = s0; s < s1; ++s) {
-        const char* at = s_mem + buf * STAGE;
-        const int next = buf + 1 == NST ? 0 : buf + 1;
-        step(std::integral_constant<int, 1>{}, at);
-        mma(0);
-        step(std::integral_constant<int, 2>{}, at);
-        mma(1);
-        step(std::integral_constant<int, 3>{}, at);
-        mma(0);
-        if (s + 1 < s1) {
-          next_stage(s, buf);
-          step(std::integral_constant<int, 0>{}, s_mem + next * STAGE);
-        }
-        mma(1);
-        buf = next;
-      }
-    }
-  }
+  multiply<T, AT, BT, BM, BN, WM, WN, NST, MULTI>(
+      s_mem, Multiplied{alt ? g.a_alt : g.a, g.b, alt ? g.lda_alt : g.lda, g.ldb, g.a_part, g.b_part, g.a_rows, g.b_rows, g.K, g.products},
+      m0, n0, split, g.splits, wave, lane, acc);
 
   // Element r of acc[i][t]: m = m0 + wm WCOLS + 32 i + 8 (r / 4) + 4 half + r % 4, n = n0 + wn WROWS + 32 t + l32.
   const int mw = m0 + wm * WCOLS + 4 * half, nw = n0 + wn * WROWS + l32;
