@@ -410,6 +410,91 @@ int densenet_adamw(const dn_adamw_tensor* tensors, int32_t count, dn_dtype p_dty
                    dn_dtype copy_dtype, const dn_adamw_params* params, void* d_m, void* d_v,
                    float* d_m_scale, float* d_v_scale, int64_t n_blocks, void* stream);
 
+/* Operators of a head that learns and answers in 8 bits: rows and weights as DN_F8 codes with a scale for every block of
+ * DN_SCALE_BLOCK, products of such operands, scores of the logits that they give, and Muon's step. */
+#define DN_SCALE_BLOCK 128
+
+/* Rows x [n][C] as codes with scales: x = code * scale.  rows 1: a scale for every DN_SCALE_BLOCK values of a row,
+ * d_scale[n][ceil(C / 128)]; rows DN_SCALE_BLOCK: for every square of 128 rows x 128 values, d_scale[ceil(n / 128)][ceil(C / 128)];
+ * blocks at the ends are cut short.  scale = max |x| / 448 over the block's finite values (a NaN or an infinity is a NaN code and
+ * counts for no maximum; of a block below 1.4e-36 all codes are 0).
+ * d_codes [n][C] (NULL: not wanted, and d_scale NULL too).  d_turned [C][n] (NULL likewise): the same of the turned matrix, from
+ * the same reading: rows 1: a scale for every 128 rows of a column, d_turned_scale[C][ceil(n / 128)]; rows 128: the same codes,
+ * d_turned_scale[ceil(C / 128)][ceil(n / 128)].
+ * Limit (DN_E_TOO_LARGE): n C in tiles of 128 x 128 below 2^24. */
+int densenet_quantize_blocks(const void* d_x, int64_t x_stride, int64_t n, int32_t C, dn_dtype dtype,
+                             int32_t rows, void* d_codes, int64_t codes_stride, float* d_scale,
+                             void* d_turned, int64_t turned_stride, float* d_turned_scale, void* stream);
+
+/* y_nv = sum_c a_nc w_vc of codes a [n][C] and w [V][C] (DN_F8) with scales: of a for every 128 values of a row
+ * (d_a_scale[n][ceil(C / 128)], as densenet_quantize_blocks with rows 1 and densenet_rms_norm with block 128 give them), of w for
+ * every square (d_w_scale[ceil(V / 128)][ceil(C / 128)], rows 128).  A layer's forward pass takes w's codes; its gradients are
+ * products too: dx from the codes of dy (rows 1) and w's turned ones (rows 128), dw [V][C] from dy's turned codes (rows 1) and x's
+ * turned ones (rows 128).
+ * A block's products are summed in 32 bits and multiplied by the product of its two scales (which has to be in fp32's range).
+ * d_y [n][V]: `y_dtype`, any of DN_F32, DN_F16, DN_BF16.  d_workspace: NULL for a size query into *bytes_needed (which depends on
+ * the codes' alignment and strides: pass the same).  Codes whose rows start on 16 bytes are read as they lie, others are copied to
+ * such rows first.  Limits (DN_E_TOO_LARGE): C <= 2^20; n, V <= 2^31 - 256; n V in tiles of 128 x 32 below 2^24. */
+int densenet_block_product(const void* d_a, int64_t a_stride, const float* d_a_scale, const void* d_w,
+                           int64_t w_stride, const float* d_w_scale, int64_t n, int32_t C, int32_t V,
+                           void* d_y, int64_t y_stride, dn_dtype y_dtype, void* d_workspace,
+                           size_t workspace_bytes, size_t* bytes_needed, void* stream);
+
+/* Scores of rows of logits l [n][V] (`dtype`): with x = scale l (scale > 0, the inverse temperature),
+ *   lse = log sum_v exp x_v;  logp = x_token - lse;  entropy = -sum_v p_v log p_v, p = exp(x - lse);
+ *   the `top` (0 .. DN_MAX_TOP) largest logits, of equal ones the lower index first: their indices and log probabilities.
+ * d_token: int64 [n], or NULL; of a row whose token lies outside [0, V), logp is 0.  d_logp, d_entropy (NULL: not wanted), d_lse:
+ * fp32 [n].  d_top_id: int64 [n][top]; d_top_logp: fp32 [n][top].  A logit of -infinity has no probability and is no alternative:
+ * where fewer than `top` others are left, the rest are id -1 with -infinity.  A row of -infinity alone: lse -infinity, logp and
+ * entropy 0.  A row with a NaN or +infinity: NaN and ids -1 (logp without a token: 0).
+ * d_workspace: NULL for a size query into *bytes_needed.  n <= 2^31 - 256, V < 2^31 - 256. */
+#define DN_MAX_TOP 64
+int densenet_token_scores(const void* d_logits, int64_t stride, const int64_t* d_token, int64_t n, int32_t V,
+                          dn_dtype dtype, float scale, int32_t top, float* d_logp, float* d_entropy,
+                          float* d_lse, int64_t* d_top_id, float* d_top_logp, void* d_workspace,
+                          size_t workspace_bytes, size_t* bytes_needed, void* stream);
+
+/* Gradient of the scores, from the forward pass's lse (and entropy and ids):
+ *   dl_v = scale (p_v (dlse - dlogp - sum_j dtop_j - dentropy (log p_v + entropy)) + dlogp [v = token] + sum_j dtop_j [v = id_j])
+ * d_dlogp, d_dentropy, d_dlse: fp32 [n], d_dtop: fp32 [n][top], each NULL for 0; d_entropy is needed with d_dentropy, d_top_id with
+ * d_dtop, d_token with d_dlogp.  A token or id outside [0, V) has no gradient; an id may be there more than once, or be the token.
+ * A row of which nothing is asked (all its gradients 0) gets zeros, whatever it holds, and so does a row of -infinity alone.  d_dlogits: `dtype`; it may be the logits'
+ * own memory (same stride). */
+int densenet_token_scores_backward(const void* d_logits, int64_t stride, const int64_t* d_token,
+                                   const float* d_lse, const float* d_entropy, const float* d_dlogp,
+                                   const float* d_dentropy, const float* d_dlse, const int64_t* d_top_id,
+                                   const float* d_dtop, int64_t n, int32_t V, dn_dtype dtype, float scale,
+                                   int32_t top, void* d_dlogits, int64_t dlogits_stride, void* stream);
+
+/* One Muon step over `count` matrices (host table), in place:
+ *   g' = g grad_scale;  m = momentum m + g';  u = g' + momentum m (nesterov), or m;  X = u / (|u| + eps) (Frobenius norm)
+ *   X = a X + (b A + c A^2) X with A = X X' (of more rows than columns: X (b A + c A^2) with A = X' X), `steps` times
+ *   p = p (1 - lr weight_decay) - lr rate X
+ * p, g: contiguous [rows][cols] of p_dtype and g_dtype; copy (or NULL): the new p in copy_dtype (DN_F16 or DN_BF16); m: fp32
+ * [rows][cols], or NULL with momentum 0.  No two tensors of a call may meet in memory.  |u| is taken in fp32: squares have to be in
+ * its range.
+ * steps: 1 .. DN_MAX_NS_STEPS; step s takes coefficients[s] = (a, b, c), which have to keep the singular values of X below 4 and
+ * those of b A + c A^2 below 2 (1.5 |b| + 2.25 |c|), as the usual ones (3.4445, -4.775, 2.0315) do.
+ * parts: fp16 parts of a value in the products, 1 (11 bits) or 2 (22 bits); 0: 1 for DN_BF16 weights, 2 for others.
+ * d_workspace: NULL for a size query into *bytes_needed.  Limits (DN_E_TOO_LARGE): rows, cols <= 2^22, the smaller <= 2^15. */
+#define DN_MAX_NS_STEPS 16
+typedef struct {
+  void* p;
+  const void* g;
+  void* copy;
+  float* m;
+  int64_t rows, cols;
+  double rate;
+} dn_muon_tensor;
+typedef struct {
+  double lr, momentum, weight_decay, grad_scale, eps;
+  double coefficients[DN_MAX_NS_STEPS][3];
+  int32_t steps, nesterov, parts, reserved;
+} dn_muon_params;
+int densenet_muon(const dn_muon_tensor* tensors, int32_t count, dn_dtype p_dtype, dn_dtype g_dtype,
+                  dn_dtype copy_dtype, const dn_muon_params* params, void* d_workspace,
+                  size_t workspace_bytes, size_t* bytes_needed, void* stream);
+
 /* Launch tracing.  While tracing is on, every kernel launch whose name matches `filter` (a
  * comma-separated list of names; NULL or "" = all) is bracketed by two hipEvents recorded on the
  * launch's own stream.  densenet_profile_stop() waits for the recorded events, writes per-name
@@ -417,7 +502,7 @@ int densenet_adamw(const dn_adamw_tensor* tensors, int32_t count, dn_dtype p_dty
  * tracing off.  Kernel names: build_planes, conv1..conv5, lrn_pool1, lrn_pool2, pool5, warp_regions,
  * region_windows, region_pool, pack_weights (a cross-image packed batch traces as build_planes,
  * region_windows, region_pool), rms_norm, rms_norm_backward, softmax_loss, softmax_loss_backward (all launches of a call
- * as one) and adamw.  Events come from a pool owned by the library (no device memory). */
+ * as one), adamw, quantize_blocks, block_product, token_scores, token_scores_backward and muon (likewise).  Events come from a pool owned by the library (no device memory). */
 typedef struct {
   char name[32];
   int32_t launches;

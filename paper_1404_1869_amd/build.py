@@ -19,7 +19,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libdensenet.so")
 HEAD = os.path.join(PKG, "head")   # the head's operators: sources of their own beside the descriptor path's
 SOURCES = ("plan.cpp", "api.cpp", "trace.cpp", "pyramid.hip", "conv.hip", "lrn_pool.hip", "regions.hip", "windows.hip",
-           *(os.path.join(HEAD, f) for f in ("head_api.cpp", "norm.hip", "loss.hip", "adamw.hip")))
+           *(os.path.join(HEAD, f) for f in ("head_api.cpp", "norm.hip", "loss.hip", "adamw.hip", "blocks.hip", "scores.hip", "muon.hip")))
 PROBE_SRC = os.path.join(PKG, "probe", "probe_mfma.hip")
 PROBE_LIB = os.path.join(PKG, "libprobe.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -27,6 +27,7 @@ DN_MAX_SCALES, DN_MAX_PLANES_PER_IMAGE, DN_MAX_WARP_SIDE, DN_MAX_ASPECTS = 64, 6
 DN_MAX_BATCH_ITEMS = 65536
 DN_STATIC_SCRATCH_BYTES = 64 << 20
 DN_MAX_NORM_C = 32768
+DN_SCALE_BLOCK, DN_MAX_TOP, DN_MAX_NS_STEPS = 128, 64, 16
 ADAMW_BLOCK = 256
 DTYPES = {"f32": DN_F32, "f16": DN_F16, "bf16": DN_BF16}
 
@@ -36,7 +37,8 @@ EXPORTS = ("densenet_plan_pyramid", "densenet_build_pyramid", "densenet_pack_wei
            "densenet_region_pool", "densenet_plan_batch", "densenet_build_batch",
            "densenet_region_windows_batch", "densenet_build_pyramid_noalloc", "densenet_rms_norm",
            "densenet_rms_norm_backward", "densenet_softmax_loss", "densenet_softmax_loss_backward",
-           "densenet_adamw", "densenet_profile_start", "densenet_profile_stop", "densenet_last_error")
+           "densenet_adamw", "densenet_quantize_blocks", "densenet_block_product", "densenet_token_scores",
+           "densenet_token_scores_backward", "densenet_muon", "densenet_profile_start", "densenet_profile_stop", "densenet_last_error")
 
 
 class dn_pyramid_params(ctypes.Structure):
@@ -76,6 +78,17 @@ class dn_adamw_tensor(ctypes.Structure):
 class dn_adamw_params(ctypes.Structure):
     _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")] + \
                [("step", ctypes.c_int64), ("seed", ctypes.c_uint32), ("state_bits", ctypes.c_int32)]
+
+
+class dn_muon_tensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("p", "g", "copy", "m")] + [("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                                                                         ("rate", ctypes.c_double)]
+
+
+class dn_muon_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "momentum", "weight_decay", "grad_scale", "eps")] + \
+               [("coefficients", ctypes.c_double * 3 * DN_MAX_NS_STEPS)] + \
+               [(n, ctypes.c_int32) for n in ("steps", "nesterov", "parts", "reserved")]
 
 
 class DenseNetError(RuntimeError):
@@ -128,6 +141,11 @@ def lib():
                                                i64, P, sz, psz, P],
             "densenet_adamw": [ctypes.POINTER(dn_adamw_tensor), i32, i32, i32, i32,
                                ctypes.POINTER(dn_adamw_params), P, P, P, P, i64, P],
+            "densenet_quantize_blocks": [P, i64, i64, i32, i32, i32, P, i64, P, P, i64, P, P],
+            "densenet_block_product": [P, i64, P, P, i64, P, i64, i32, i32, P, i64, i32, P, sz, psz, P],
+            "densenet_token_scores": [P, i64, P, i64, i32, i32, f32, i32, P, P, P, P, P, P, sz, psz, P],
+            "densenet_token_scores_backward": [P, i64, P, P, P, P, P, P, P, P, i64, i32, i32, f32, i32, P, i64, P],
+            "densenet_muon": [ctypes.POINTER(dn_muon_tensor), i32, i32, i32, i32, ctypes.POINTER(dn_muon_params), P, sz, psz, P],
             "densenet_profile_start": [ctypes.c_char_p],
             "densenet_profile_stop": [ctypes.POINTER(dn_profile_entry), i32, pi32],
         }
@@ -879,3 +897,238 @@ def densenet_adamw(plan: AdamWPlan, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, 
     check(lib().densenet_adamw(plan.table, len(plan.table), plan.p_dtype, plan.g_dtype, plan.copy_dtype, ctypes.byref(k),
                                ptr(plan.m), ptr(plan.v), ptr(plan.m_scale), ptr(plan.v_scale), plan.n_blocks,
                                _on(plan.device)))
+
+
+# ------------------------------------------------------------------------------------------------
+# A head in 8 bits
+# ------------------------------------------------------------------------------------------------
+def _codes(shape, device):
+    """Codes in rows that start on 16 bytes, which products read as they lie."""
+    torch = _torch()
+    n, C = shape
+    return torch.empty((n, -(-C // 16) * 16), dtype=torch.float8_e4m3fn, device=device)[:, :C]
+
+
+def _scales(t, what, shape, device):
+    torch = _torch()
+    if t is None:
+        return torch.empty(shape, dtype=torch.float32, device=device)
+    if tuple(t.shape) != shape or t.dtype != torch.float32 or t.device != device or not t.is_contiguous():
+        raise _bad(f"{what}: contiguous fp32 {list(shape)} on the operands' GPU expected")
+    return t
+
+
+def densenet_quantize_blocks(x, rows=1, codes=True, turned=False, out=None, scale=None, turned_out=None, turned_scale=None):
+    """Rows of x [n][C] as e4m3 codes, x = code * scale, with a scale for every 128 values of a row (rows=1) or every square of
+    128 x 128 (rows=128).  Returns (codes [n][C], scale, turned [C][n], turned_scale): with codes=False or turned=False None in
+    place of those; turned is the same of x's transpose, from one reading.  New codes lie in rows that start on 16 bytes."""
+    torch = _torch()
+    dt = _code(x, "x")
+    xp, xs = _rows(x, "x")
+    n, C = x.shape
+    dev = x.device
+    if rows not in (1, DN_SCALE_BLOCK):
+        raise DenseNetError(DN_E_UNSUPPORTED, f"rows: 1 or {DN_SCALE_BLOCK}")
+    codes, turned = codes or out is not None, turned or turned_out is not None
+    if not codes and not turned:
+        raise _bad("codes, turned or both")
+    if (not codes and scale is not None) or (not turned and turned_scale is not None):
+        raise _bad("scales belong to codes that are asked for")
+    if n >= 1 << 31:
+        raise DenseNetError(DN_E_TOO_LARGE, f"x: {n} rows")
+    up = lambda v: -(-v // DN_SCALE_BLOCK)  # noqa: E731
+    cp, cs, kp, tp, ts, tkp = None, 0, None, None, 0, None
+    f8 = torch.float8_e4m3fn
+    if codes:
+        out = _codes((n, C), dev) if out is None else out
+        cp, cs = _rows(out, "out", (n, C), f8, dev)
+        scale = _scales(scale, "scale", (n if rows == 1 else up(n), up(C)), dev)
+        kp = scale.data_ptr()
+    if turned:
+        turned_out = _codes((C, n), dev) if turned_out is None else turned_out
+        tp, ts = _rows(turned_out, "turned_out", (C, n), f8, dev)
+        turned_scale = _scales(turned_scale, "turned_scale", (C if rows == 1 else up(C), up(n)), dev)
+        tkp = turned_scale.data_ptr()
+    if n:
+        check(lib().densenet_quantize_blocks(xp, xs, n, C, dt, rows, cp, cs, kp, tp, ts, tkp, _on(dev)))
+    return out, scale, turned_out, turned_scale
+
+
+def densenet_block_product(a, a_scale, w, w_scale, out_dtype=DN_BF16, out=None):
+    """y [n][V] = a w^T of e4m3 codes a [n][C] and w [V][C]: a_scale [n][ceil(C / 128)], a scale for every 128 values of a row;
+    w_scale [ceil(V / 128)][ceil(C / 128)], one for every square of 128 x 128 (densenet_quantize_blocks with rows 1 and 128).
+    out_dtype: DN_F32, DN_F16 or DN_BF16."""
+    torch = _torch()
+    f8 = torch.float8_e4m3fn
+    ap, as_ = _rows(a, "a", None, f8)
+    n, C = a.shape
+    dev = a.device
+    if w.dim() != 2:
+        raise _bad("w: a matrix expected")
+    V = w.shape[0]
+    if V >= 1 << 31:
+        raise DenseNetError(DN_E_TOO_LARGE, f"w: {V} rows")
+    wp, ws_ = _rows(w, "w", (V, C), f8, dev)
+    up = lambda v: -(-v // DN_SCALE_BLOCK)  # noqa: E731
+    if a_scale is None or w_scale is None:
+        raise _bad("codes need their scales")
+    a_scale, w_scale = _scales(a_scale, "a_scale", (n, up(C)), dev), _scales(w_scale, "w_scale", (up(V), up(C)), dev)
+    yt = _types()[1].get(out_dtype)
+    if yt is None or out_dtype == DN_F8:
+        raise DenseNetError(DN_E_UNSUPPORTED, f"out_dtype {out_dtype}")
+    out = torch.empty((n, V), dtype=yt, device=dev) if out is None else out
+    yp, ys = _rows(out, "out", (n, V), yt, dev)
+    # (the size depends on the codes' alignment: addresses of the same one in place of their own)
+    need = _work_bytes("densenet_block_product", 4096 + ap % 16 if ap else None, as_, None, 4096 + wp % 16, ws_, None, n, C, V, None, 0,
+                       out_dtype)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    check(lib().densenet_block_product(ap, as_, a_scale.data_ptr(), wp, ws_, w_scale.data_ptr(), n, C, V, yp, ys, out_dtype,
+                                       ws.data_ptr(), need, None, _on(dev)))
+    return out
+
+
+def _top_buffers(ids, logp, n, top, dev, make):
+    torch = _torch()
+    if top == 0:
+        if ids is not None or logp is not None:
+            raise _bad("ids and their values belong to top > 0")
+        return None, None
+    for t, what, dtype in ((ids, "ids", torch.int64), (logp, "their values", torch.float32)):
+        if t is not None and (tuple(t.shape) != (n, top) or t.dtype != dtype or t.device != dev or not t.is_contiguous()):
+            raise _bad(f"{what}: contiguous {dtype} [{n}][{top}] on the operands' GPU expected")
+    if make:
+        ids = torch.empty((n, top), dtype=torch.int64, device=dev) if ids is None else ids
+        logp = torch.empty((n, top), dtype=torch.float32, device=dev) if logp is None else logp
+    return ids, logp
+
+
+def densenet_token_scores(logits, tokens=None, top=0, scale=1.0, logp=None, entropy=None, lse=None, top_id=None, top_logp=None):
+    """Log probability of each row's token, entropy, log of the sum of exponentials, and the `top` (up to 64) best alternatives of
+    logits [n][V] times scale.  tokens: int64 [n], or None (then logp is 0 where given, else None); a token outside [0, V): logp 0.
+    Of equal logits the lower index comes first; -infinity is no alternative (id -1).  Returns (logp, entropy, lse, top_id,
+    top_logp), the last two None with top=0."""
+    torch = _torch()
+    dt = _code(logits, "logits")
+    xp, xs = _rows(logits, "logits")
+    n, V = logits.shape
+    dev = logits.device
+    if not 0 <= top <= DN_MAX_TOP:
+        raise DenseNetError(DN_E_UNSUPPORTED, f"top: 0 .. {DN_MAX_TOP}")
+    new = lambda t: torch.empty(n, dtype=torch.float32, device=dev) if t is None else t  # noqa: E731
+    entropy, lse = new(entropy), new(lse)
+    if tokens is not None:
+        logp = new(logp)
+    top_id, top_logp = _top_buffers(top_id, top_logp, n, top, dev, True)
+    vec = lambda t, what: _vector(t, what, n, torch.float32, dev)  # noqa: E731
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    need = _work_bytes("densenet_token_scores", 4096, V, None, n, V, dt, 1.0, top, None, None, None, None, None)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    check(lib().densenet_token_scores(xp, xs, _vector(tokens, "tokens", n, torch.int64, dev), n, V, dt, scale, top, vec(logp, "logp"),
+                                      vec(entropy, "entropy"), vec(lse, "lse"), ptr(top_id), ptr(top_logp), ws.data_ptr(), need, None,
+                                      _on(dev)))
+    return logp, entropy, lse, top_id, top_logp
+
+
+def densenet_token_scores_backward(logits, tokens, lse, entropy=None, dlogp=None, dentropy=None, dlse=None, top_id=None, dtop=None,
+                                   scale=1.0, out=None):
+    """Gradient of densenet_token_scores by the logits, from its results and from the gradients of each of them (None: 0; dtop
+    [n][top] belongs to top_id's log probabilities).  Returns dlogits in the logits' type; out may be the logits themselves."""
+    torch = _torch()
+    dt = _code(logits, "logits")
+    xp, xs = _rows(logits, "logits")
+    n, V = logits.shape
+    dev = logits.device
+    top = 0 if dtop is None else dtop.shape[1] if dtop.dim() == 2 else -1
+    if not 0 <= top <= DN_MAX_TOP:
+        raise DenseNetError(DN_E_UNSUPPORTED, f"dtop: up to {DN_MAX_TOP} alternatives of each row")
+    if top and top_id is None:
+        raise _bad("dtop needs top_id")
+    ids, vals = _top_buffers(top_id if top else None, dtop if top else None, n, top, dev, False)
+    out = torch.empty((n, V), dtype=logits.dtype, device=dev) if out is None else out
+    op, os_ = _rows(out, "out", (n, V), logits.dtype, dev)
+    vec = lambda t, what: _vector(t, what, n, torch.float32, dev)  # noqa: E731
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    check(lib().densenet_token_scores_backward(
+        xp, xs, _vector(tokens, "tokens", n, torch.int64, dev), vec(lse, "lse"), vec(entropy, "entropy"), vec(dlogp, "dlogp"),
+        vec(dentropy, "dentropy"), vec(dlse, "dlse"), ptr(ids), ptr(vals), n, V, dt, scale, top, op, os_, _on(dev)))
+    return out
+
+
+class MuonPlan:
+    """Matrices that step together by Muon: parameters (one type, updated in place), their gradients' buffers (one type), momentum
+    (fp32, made as zeros if not given), 16-bit copies of the parameters (optional; None entries allowed), and a rate for each that
+    multiplies the learning rate (by default 0.2 sqrt(max(rows, cols)), which gives updates of AdamW's size).  parts: fp16 parts of a value in the products (0: 1 for bf16 parameters, else 2)."""
+
+    def __init__(self, params, grads, momentum=None, copies=None, rates=None, parts=0):
+        torch = _torch()
+        self.params, self.parts = list(params), parts
+        self.copies = list(copies) if copies is not None else [None] * len(self.params)
+        if not self.params or len(self.copies) != len(self.params):
+            raise _bad("as many copies as parameters expected, one at least")
+        if parts not in (0, 1, 2):
+            raise DenseNetError(DN_E_UNSUPPORTED, "parts: 0, 1 or 2")
+        self.device = self.params[0].device
+        self.p_dtype = _code(self.params[0], "params")
+        given = [c for c in self.copies if c is not None]
+        self.copy_dtype = _code(given[0], "copies") if given else DN_BF16
+        if momentum is None:
+            momentum = [torch.zeros(p.shape, dtype=torch.float32, device=self.device) for p in self.params]
+        self.momentum = list(momentum)
+        rates = [0.2 * max(p.shape) ** 0.5 if p.dim() == 2 else 0.0 for p in self.params] if rates is None else list(rates)
+        if len(self.momentum) != len(self.params) or len(rates) != len(self.params):
+            raise _bad("as much momentum and as many rates as parameters expected")
+        self.table = (dn_muon_tensor * len(self.params))()
+        for e, p, c, m, rate in zip(self.table, self.params, self.copies, self.momentum, rates):
+            if p.dim() != 2 or p.numel() == 0:
+                raise _bad("params: matrices expected")
+            self._fits(p, "params", p, self.params[0].dtype)
+            self._fits(m, "momentum", p, torch.float32)
+            if c is not None:
+                self._fits(c, "copies", p, given[0].dtype)
+            e.p, e.copy, e.m = p.data_ptr(), None if c is None else c.data_ptr(), m.data_ptr()
+            e.rows, e.cols, e.rate = p.shape[0], p.shape[1], rate
+        held = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in self.params + self.momentum + given)
+        if any(a + size > b for (a, size), (b, _) in zip(held, held[1:])):
+            raise _bad("two of the tensors that are stepped meet in memory")
+        self.set_grads(grads)
+
+    def _fits(self, t, what, p, dtype):
+        if t.dtype != dtype or t.shape != p.shape or t.device != self.device or not t.is_cuda or not t.is_contiguous():
+            raise _bad(f"{what}: contiguous tensors of one type on one GPU, of their parameters' shapes, expected")
+
+    def set_grads(self, grads):
+        """Takes the gradients of the following steps from other tensors."""
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise _bad("as many gradients as parameters expected")
+        for g, p in zip(grads, self.params):
+            self._fits(g, "grads", p, grads[0].dtype)
+        self.grads, self.g_dtype = grads, _code(grads[0], "grads")
+        for e, g in zip(self.table, grads):
+            e.g = g.data_ptr()
+
+
+#: The usual coefficients of a Newton-Schulz step, which bring singular values to between 0.7 and 1.2 in five of them.
+NS_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+
+def densenet_muon(plan: MuonPlan, lr, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5, coefficients=NS_COEFFICIENTS, eps=1e-7,
+                  grad_scale=1.0):
+    """One Muon step over a plan's matrices: p = p (1 - lr weight_decay) - lr rate X, X the update orthogonalised by `steps`
+    Newton-Schulz steps.  coefficients: (a, b, c) of all steps, or one such triple for each."""
+    if not 1 <= steps <= DN_MAX_NS_STEPS:
+        raise DenseNetError(DN_E_UNSUPPORTED, f"steps: 1 .. {DN_MAX_NS_STEPS}")
+    each = [tuple(c) for c in coefficients] if hasattr(coefficients[0], "__len__") else [tuple(coefficients)] * steps
+    if len(each) != steps or any(len(c) != 3 for c in each):
+        raise _bad("coefficients: (a, b, c), or as many of these as steps, expected")
+    k = dn_muon_params(lr, momentum, weight_decay, grad_scale, eps)
+    for i, c in enumerate(each):
+        k.coefficients[i][:] = c
+    k.steps, k.nesterov, k.parts = steps, int(nesterov), plan.parts
+    on = _on(plan.device)
+    torch = _torch()
+    args = (plan.table, len(plan.table), plan.p_dtype, plan.g_dtype, plan.copy_dtype, ctypes.byref(k))
+    need = ctypes.c_size_t()
+    check(lib().densenet_muon(*args, None, 0, ctypes.byref(need), None))
+    ws = torch.empty(need.value, dtype=torch.uint8, device=plan.device)
+    check(lib().densenet_muon(*args, ws.data_ptr(), need.value, None, on))

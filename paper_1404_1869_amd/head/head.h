@@ -79,6 +79,59 @@ int launch_softmax_loss(const LossArgs& a, dn_dtype dt, void* d_work, void* stre
 size_t softmax_loss_backward_bytes(const LossArgs& a, dn_dtype dt);
 int launch_softmax_loss_backward(const LossArgs& a, dn_dtype dt, void* d_work, void* stream);
 
+// Scores of rows of logits [n][V].  Strides in elements.
+struct ScoresArgs {
+  const void* x;
+  const int64_t* token;
+  int64_t x_stride, n;
+  int32_t V, top, parts;  // parts: workgroups of a row
+  float scale;
+  float *logp, *entropy, *lse;
+  int64_t* top_id;
+  float* top_logp;
+  void* work;
+};
+int32_t scores_parts(int64_t n, int32_t V);
+size_t scores_bytes(int64_t n, int32_t V, int32_t top);
+int launch_token_scores(const ScoresArgs& a, dn_dtype dt, void* stream);
+struct ScoresBackArgs {
+  const void* x;
+  const int64_t *token, *top_id;
+  const float *lse, *entropy, *dlogp, *dentropy, *dlse, *dtop;
+  void* dx;
+  int64_t x_stride, dx_stride, n;
+  int32_t V, top, segments;
+  float scale;
+};
+int launch_token_scores_backward(const ScoresBackArgs& a, dn_dtype dt, void* stream);
+
+// Rows [n][C] to codes and scales, as they lie and turned.
+struct QuantArgs {
+  const void* x;
+  int64_t x_stride, n;
+  int32_t C, rows;
+  uint8_t *codes, *turned;
+  int64_t codes_stride, turned_stride;
+  float *scale, *turned_scale;
+};
+int launch_quantize_blocks(const QuantArgs& a, dn_dtype dt, void* stream);
+
+// Product of rows a [n][C] with w [V][C], codes with scales.
+struct ProductArgs {
+  const uint8_t *a, *w;
+  const float *a_scale, *w_scale;
+  int64_t a_stride, w_stride, n;
+  int32_t C, V;
+  void* y;
+  int64_t y_stride;
+};
+size_t block_product_bytes(const ProductArgs& a);
+int launch_block_product(const ProductArgs& a, dn_dtype dt, void* d_work, void* stream);
+
+size_t muon_bytes(const dn_muon_tensor* tensors, int32_t count, dn_dtype p_dt, const dn_muon_params& k);
+int launch_muon(const dn_muon_tensor* tensors, int32_t count, dn_dtype p_dt, dn_dtype g_dt, dn_dtype copy_dt, const dn_muon_params& k,
+                void* d_work, void* stream);
+
 }  // namespace head
 }  // namespace dn
 

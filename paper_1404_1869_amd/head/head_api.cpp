@@ -62,6 +62,18 @@ int check_loss(const LossArgs& a, dn_dtype dtype, bool backward) {
   return DN_OK;
 }
 
+int64_t blocks_of(int64_t x) { return (x + DN_SCALE_BLOCK - 1) / DN_SCALE_BLOCK; }
+
+int check_scores(const void* logits, int64_t stride, const int64_t* token, int64_t n, int32_t V, dn_dtype dtype, float scale, int32_t top) {
+  if (!valid_dtype(dtype)) return fail(DN_E_UNSUPPORTED, "unknown dtype");
+  if (n < 0 || V <= 0) return fail(DN_E_INVALID_ARG, "n must be >= 0 and V positive");
+  if (n > MAX_ROWS || V >= MAX_ROWS) return fail(DN_E_TOO_LARGE, "n or V");
+  if (!(scale > 0) || std::isinf(scale)) return fail(DN_E_INVALID_ARG, "scale must be positive and finite");
+  if (top < 0 || top > DN_MAX_TOP) return fail(DN_E_UNSUPPORTED, "top must be 0 .. DN_MAX_TOP");
+  if ((uintptr_t)token % 8) return fail(DN_E_INVALID_ARG, "tokens: not aligned");
+  return check_rows("logits", logits, stride, n, V, dtype_size(dtype));
+}
+
 }  // namespace
 }  // namespace head
 }  // namespace dn
@@ -237,6 +249,153 @@ int densenet_adamw(const dn_adamw_tensor* tensors, int32_t count, dn_dtype p_dty
       }
     }
     return flush();
+  } catch (...) {
+    return fail(DN_E_INTERNAL, "unexpected exception");
+  }
+}
+
+int densenet_quantize_blocks(const void* d_x, int64_t x_stride, int64_t n, int32_t C, dn_dtype dtype, int32_t rows, void* d_codes,
+                             int64_t codes_stride, float* d_scale, void* d_turned, int64_t turned_stride, float* d_turned_scale,
+                             void* stream) {
+  try {
+    if (!valid_dtype(dtype)) return fail(DN_E_UNSUPPORTED, "unknown dtype");
+    if (rows != 1 && rows != DN_SCALE_BLOCK) return fail(DN_E_UNSUPPORTED, "rows must be 1 or DN_SCALE_BLOCK");
+    if (n < 0 || C <= 0) return fail(DN_E_INVALID_ARG, "n must be >= 0 and C positive");
+    if (n > MAX_ROWS) return fail(DN_E_TOO_LARGE, "too many rows");
+    const int64_t tiles = blocks_of(n) * blocks_of(C);
+    if (tiles > MAX_TILES) return fail(DN_E_TOO_LARGE, "n times C");
+    if (!d_codes && !d_turned) return n ? fail(DN_E_INVALID_ARG, "no output asked for") : DN_OK;
+    if (!d_codes != !d_scale || !d_turned != !d_turned_scale) return fail(DN_E_INVALID_ARG, "codes and their scales belong together");
+    int st;
+    if ((st = check_rows("x", d_x, x_stride, n, C, dtype_size(dtype)))) return st;
+    if (d_codes && (st = check_rows("codes", d_codes, codes_stride, n, C, 1))) return st;
+    // (turned rows are n long, which is within 31 bits)
+    if (d_turned && (st = check_rows("turned", d_turned, turned_stride, C, (int32_t)n, 1))) return st;
+    if ((uintptr_t)d_scale % 4 || (uintptr_t)d_turned_scale % 4) return fail(DN_E_INVALID_ARG, "scale: not aligned");
+    if (n == 0) return DN_OK;
+    QuantArgs a{d_x,      x_stride, n, C, rows, (uint8_t*)d_codes, (uint8_t*)d_turned, codes_stride, turned_stride, d_scale,
+                d_turned_scale};
+    return run_step("quantize_blocks", stream, [&] { return launch_quantize_blocks(a, dtype, stream); });
+  } catch (...) {
+    return fail(DN_E_INTERNAL, "unexpected exception");
+  }
+}
+
+int densenet_block_product(const void* d_a, int64_t a_stride, const float* d_a_scale, const void* d_w, int64_t w_stride,
+                           const float* d_w_scale, int64_t n, int32_t C, int32_t V, void* d_y, int64_t y_stride, dn_dtype y_dtype,
+                           void* d_workspace, size_t workspace_bytes, size_t* bytes_needed, void* stream) {
+  try {
+    if (!valid_dtype(y_dtype)) return fail(DN_E_UNSUPPORTED, "unknown dtype");
+    if (n < 0 || C <= 0 || V <= 0) return fail(DN_E_INVALID_ARG, "n must be >= 0, C and V positive");
+    if (n > MAX_ROWS || V > MAX_ROWS || C > (1 << 20)) return fail(DN_E_TOO_LARGE, "n, V or C");
+    if (((n + 31) / 32) * blocks_of(V) > MAX_TILES) return fail(DN_E_TOO_LARGE, "n times V");
+    ProductArgs a{(const uint8_t*)d_a, (const uint8_t*)d_w, d_a_scale, d_w_scale, a_stride, w_stride, n, C, V, d_y, y_stride};
+    int st;
+    if ((st = check_rows("a", d_a, a_stride, n, C, 1))) return st;
+    if ((st = check_rows("w", d_w, w_stride, V, C, 1))) return st;
+    // (never 0, so that a caller's workspace is never the null pointer of a size query)
+    const size_t need = std::max<size_t>(n ? block_product_bytes(a) : 0, 256);
+    if ((st = check_work(d_workspace, workspace_bytes, need, bytes_needed)) || !d_workspace) return st;
+    if (n == 0) return DN_OK;
+    if (!d_a_scale || !d_w_scale) return fail(DN_E_INVALID_ARG, "null scale pointer");
+    if ((uintptr_t)d_a_scale % 4 || (uintptr_t)d_w_scale % 4) return fail(DN_E_INVALID_ARG, "scale: not aligned");
+    if ((st = check_rows("y", d_y, y_stride, n, V, dtype_size(y_dtype)))) return st;
+    return run_step("block_product", stream, [&] { return launch_block_product(a, y_dtype, d_workspace, stream); });
+  } catch (...) {
+    return fail(DN_E_INTERNAL, "unexpected exception");
+  }
+}
+
+int densenet_token_scores(const void* d_logits, int64_t stride, const int64_t* d_token, int64_t n, int32_t V, dn_dtype dtype,
+                          float scale, int32_t top, float* d_logp, float* d_entropy, float* d_lse, int64_t* d_top_id,
+                          float* d_top_logp, void* d_workspace, size_t workspace_bytes, size_t* bytes_needed, void* stream) {
+  try {
+    int st;
+    if ((st = check_scores(d_logits, stride, d_token, n, V, dtype, scale, top))) return st;
+    const size_t need = std::max<size_t>(scores_bytes(n, V, top), 256);
+    if ((st = check_work(d_workspace, workspace_bytes, need, bytes_needed)) || !d_workspace) return st;
+    if (n == 0) return DN_OK;
+    if (!d_lse) return fail(DN_E_INVALID_ARG, "null lse pointer");
+    if (top > 0 && (!d_top_id || !d_top_logp)) return fail(DN_E_INVALID_ARG, "alternatives need d_top_id and d_top_logp");
+    if ((uintptr_t)d_logp % 4 || (uintptr_t)d_entropy % 4 || (uintptr_t)d_lse % 4 || (uintptr_t)d_top_logp % 4 ||
+        (uintptr_t)d_top_id % 8)
+      return fail(DN_E_INVALID_ARG, "an output is not aligned to its elements");
+    ScoresArgs a{d_logits, d_token, stride,    n,     V,        top,        scores_parts(n, V), scale,
+                 d_logp,   d_entropy, d_lse, d_top_id, d_top_logp, d_workspace};
+    return run_step("token_scores", stream, [&] { return launch_token_scores(a, dtype, stream); });
+  } catch (...) {
+    return fail(DN_E_INTERNAL, "unexpected exception");
+  }
+}
+
+int densenet_token_scores_backward(const void* d_logits, int64_t stride, const int64_t* d_token, const float* d_lse,
+                                   const float* d_entropy, const float* d_dlogp, const float* d_dentropy, const float* d_dlse,
+                                   const int64_t* d_top_id, const float* d_dtop, int64_t n, int32_t V, dn_dtype dtype, float scale,
+                                   int32_t top, void* d_dlogits, int64_t dlogits_stride, void* stream) {
+  try {
+    int st;
+    if ((st = check_scores(d_logits, stride, d_token, n, V, dtype, scale, top))) return st;
+    if ((st = check_rows("dlogits", d_dlogits, dlogits_stride, n, V, dtype_size(dtype)))) return st;
+    if (d_dlogits == d_logits && n > 1 && dlogits_stride != stride)
+      return fail(DN_E_INVALID_ARG, "dlogits in the logits' own memory: with their stride");
+    if (n == 0) return DN_OK;
+    if (!d_lse) return fail(DN_E_INVALID_ARG, "null lse pointer");
+    if (d_dentropy && !d_entropy) return fail(DN_E_INVALID_ARG, "dentropy needs the entropy");
+    if (d_dlogp && !d_token) return fail(DN_E_INVALID_ARG, "dlogp needs the tokens");
+    if (top > 0 && d_dtop && !d_top_id) return fail(DN_E_INVALID_ARG, "dtop needs the ids");
+    for (const void* p : {(const void*)d_lse, (const void*)d_entropy, (const void*)d_dlogp, (const void*)d_dentropy,
+                          (const void*)d_dlse, (const void*)d_dtop})
+      if ((uintptr_t)p % 4) return fail(DN_E_INVALID_ARG, "a vector is not aligned to its elements");
+    if ((uintptr_t)d_top_id % 8) return fail(DN_E_INVALID_ARG, "ids: not aligned");
+    ScoresBackArgs a{d_logits, d_token,   d_top_id, d_lse, d_entropy, d_dlogp, d_dentropy, d_dlse, top > 0 ? d_dtop : nullptr,
+                     d_dlogits, stride, dlogits_stride, n, V, top, 1, scale};
+    return run_step("token_scores_backward", stream, [&] { return launch_token_scores_backward(a, dtype, stream); });
+  } catch (...) {
+    return fail(DN_E_INTERNAL, "unexpected exception");
+  }
+}
+
+int densenet_muon(const dn_muon_tensor* tensors, int32_t count, dn_dtype p_dtype, dn_dtype g_dtype, dn_dtype copy_dtype,
+                  const dn_muon_params* params, void* d_workspace, size_t workspace_bytes, size_t* bytes_needed, void* stream) {
+  try {
+    if (!params || count < 0 || (count > 0 && !tensors)) return fail(DN_E_INVALID_ARG, "null table or parameters");
+    const dn_muon_params& k = *params;
+    if (!valid_dtype(p_dtype) || !valid_dtype(g_dtype)) return fail(DN_E_UNSUPPORTED, "unknown dtype");
+    if (copy_dtype != DN_F16 && copy_dtype != DN_BF16) return fail(DN_E_UNSUPPORTED, "copies are DN_F16 or DN_BF16");
+    if (k.steps < 1 || k.steps > DN_MAX_NS_STEPS) return fail(DN_E_UNSUPPORTED, "steps must be 1 .. DN_MAX_NS_STEPS");
+    if (k.parts < 0 || k.parts > 2) return fail(DN_E_UNSUPPORTED, "parts must be 0, 1 or 2");
+    if (!(k.momentum >= 0 && k.momentum < 1)) return fail(DN_E_INVALID_ARG, "momentum must be in [0, 1)");
+    if (!((float)k.eps > 0) || !std::isfinite(k.eps)) return fail(DN_E_INVALID_ARG, "eps must be positive in fp32");
+    if (!std::isfinite(k.lr) || !std::isfinite(k.weight_decay) || !std::isfinite(k.grad_scale))
+      return fail(DN_E_INVALID_ARG, "parameters must be finite");
+    for (int32_t s = 0; s < k.steps; ++s) {
+      const double* c = k.coefficients[s];
+      if (!(std::fabs(c[0]) <= 64) || !(std::fabs(c[1]) <= 64) || !(std::fabs(c[2]) <= 64))
+        return fail(DN_E_INVALID_ARG, "coefficients must be in [-64, 64]");
+    }
+    int64_t tiles = 0;
+    for (int32_t i = 0; i < count; ++i) {
+      const dn_muon_tensor& t = tensors[i];
+      if (t.rows <= 0 || t.cols <= 0) return fail(DN_E_INVALID_ARG, "a matrix's rows and cols must be positive");
+      if (t.rows > (1 << 22) || t.cols > (1 << 22) || std::min(t.rows, t.cols) > (1 << 15))
+        return fail(DN_E_TOO_LARGE, "a matrix's rows or cols");
+      if (!std::isfinite(t.rate)) return fail(DN_E_INVALID_ARG, "a matrix's rate must be finite");
+      // (more workgroups than any launch has for it: pieces of 2048 values, and twice the tiles of 64 x 64 of its smaller side)
+      tiles += (t.rows * t.cols + 2047) / 2048 + ((std::min(t.rows, t.cols) + 63) / 64) * ((std::min(t.rows, t.cols) + 127) / 64) + 16384;
+    }
+    if (tiles > MAX_TILES) return fail(DN_E_TOO_LARGE, "the matrices of a call");
+    int st;
+    const size_t need = muon_bytes(tensors, count, p_dtype, k);
+    if ((st = check_work(d_workspace, workspace_bytes, need, bytes_needed)) || !d_workspace) return st;
+    for (int32_t i = 0; i < count; ++i) {
+      const dn_muon_tensor& t = tensors[i];
+      if (!t.p || !t.g) return fail(DN_E_INVALID_ARG, "null tensor pointer");
+      if (!t.m && k.momentum != 0) return fail(DN_E_INVALID_ARG, "momentum needs its state");
+      if ((uintptr_t)t.p % dtype_size(p_dtype) || (uintptr_t)t.g % dtype_size(g_dtype) || (uintptr_t)t.copy % 2 || (uintptr_t)t.m % 4)
+        return fail(DN_E_INVALID_ARG, "a tensor is not aligned to its elements");
+    }
+    if (count == 0) return DN_OK;
+    return run_step("muon", stream, [&] { return launch_muon(tensors, count, p_dtype, g_dtype, copy_dtype, k, d_workspace, stream); });
   } catch (...) {
     return fail(DN_E_INTERNAL, "unexpected exception");
   }

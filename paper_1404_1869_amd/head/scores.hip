@@ -1,0 +1,438 @@
+// Scores of rows of logits: log probability of a given token, entropy and best alternatives, and their gradient.
+//   x = scale l;  lse = log sum exp x;  logp_v = x_v - lse;  H = -sum p log p;  the `top` largest logits, lower index first among equals
+//   gradient: with A = dlse - dlogp - sum dtop - dH H,  dl_v = scale (p_v (A - dH log p_v) + dlogp [v = token] + dtop_j [v = id_j])
+// Bound by memory: a row is read once (the gradient: read once and written once).  Every lane keeps its own maximum m, sum S of
+// exp(x - m) and T of exp(x - m) (x - m) and rescales them where the maximum grows; lanes, waves and workgroups join theirs at
+// the end, in a fixed order.  H = log S - T / S, and a logit's part is taken as (x - m), so large logits lose no digits.
+// Alternatives: a wave keeps candidates above a bound that `top` values seen so far reach.  The first block sets the bound from
+// its lanes' maxima; after that few blocks have a larger value (about top ln(V / 1024) values in all for logits in no order),
+// and a full buffer is ranked and cut to `top`.  Candidates are 64-bit keys, value and then index, so that no two are equal and
+// their ranks do not depend on who found them first.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "head.h"
+
+namespace dn {
+namespace head {
+namespace {
+
+constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
+constexpr int MOST = DN_MAX_TOP;  // alternatives
+constexpr int CAP = 192;          // keys of a wave's buffer: `top` and two waves' worth
+constexpr int EV = 16;            // values of a lane in a block, twice eight
+constexpr int WAVE_BLOCK = 64 * EV;
+
+typedef unsigned long long Key;
+// Larger for larger values and, among equal ones, for lower indices.  0 and -0 are equal.
+__device__ inline uint32_t ordered(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ inline Key key_of(float x, uint32_t index) { return (Key)ordered(x) << 32 | ~index; }
+__device__ inline float value_of(Key k) {
+  const uint32_t o = (uint32_t)(k >> 32);
+  return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
+}
+constexpr Key NOTHING = (Key)0x007fffffu << 32 | 0xffffffffu;  // key of -infinity at index 0: no key of -infinity is above it
+
+// Maximum, sum of exponentials, and sum of exponentials times their base 2 logarithm (times scale: c = scale log2 e).
+struct Stats {
+  float m, s, t;
+};
+__device__ inline float below(float m, float top, float c) {  // base 2 logarithm of what a sum over m is worth over top
+  return m == -INFINITY ? 0.f : fmaxf((m - top) * c, -1000.f);  // (finite: of a mask of the type's lowest value 0 times it is 0)
+}
+__device__ inline Stats join(const Stats& a, const Stats& b, float c) {
+  const float m = fmaxf(a.m, b.m), da = below(a.m, m, c), db = below(b.m, m, c);
+  const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+  return Stats{m, a.s * fa + b.s * fb, fa * (a.t + a.s * da) + fb * (b.t + b.s * db)};
+}
+__device__ inline Stats lanes_join(Stats a, float c) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) a = join(a, Stats{__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)}, c);
+  return a;
+}
+
+// A wave's candidates.  All of it is the wave's own: no barriers.
+struct Candidates {
+  Key* buf;     // [CAP] in LDS
+  int count;    // wave-uniform
+  Key bound;    // `top` keys above or at it have been seen (or NOTHING)
+  int top;
+
+  __device__ inline void init(Key* b, int k) { buf = b, count = 0, bound = NOTHING, top = k; }
+  // The bound from one value per lane: the top-th largest of them.
+  __device__ inline void start(float lane_max) {
+    const uint32_t o = ordered(lane_max);
+    uint32_t at = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+      const uint32_t to = at | 1u << bit;
+      if (__popcll(__ballot(o >= to)) >= top) at = to;
+    }
+    const Key k = (Key)at << 32;
+    if (k > bound) bound = k - 1;
+  }
+  // Ranks all keys and keeps the first `top`, in order.
+  __device__ inline void cut() {
+    const int lane = threadIdx.x & 63;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    Key mine[CAP / 64];
+    int rank[CAP / 64];
+#pragma unroll
+    for (int i = 0; i < CAP / 64; ++i) mine[i] = lane + 64 * i < count ? buf[lane + 64 * i] : 0, rank[i] = 0;
+    for (int j = 0; j < count; ++j) {
+      const Key k = buf[j];
+#pragma unroll
+      for (int i = 0; i < CAP / 64; ++i) rank[i] += k > mine[i];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int i = 0; i < CAP / 64; ++i)
+      if (lane + 64 * i < count && rank[i] < top) buf[rank[i]] = mine[i];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (count >= top) {
+      count = top;
+      const Key last = buf[top - 1];
+      if (last > bound) bound = last;
+    }
+  }
+  // One key per lane (0: none), in any order of indices.  A key at the bound is one that is held already.
+  __device__ inline void offer(Key k) {
+    unsigned long long hits = __ballot(k > bound);
+    if (!hits) return;
+    if (count + __popcll(hits) > CAP) {
+      cut();
+      hits = __ballot(k > bound);
+    }
+    const int at = count + __builtin_amdgcn_mbcnt_hi((uint32_t)(hits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hits, 0));
+    if (k > bound) buf[at] = k;
+    count += __popcll(hits);
+  }
+};
+
+// Eight values from element i on, -infinity from element `end` on.
+template <typename T>
+__device__ inline typename Vec8<T>::type load_logits(const T* row, int i, int end) {
+  if (i + 8 <= end) return *(const typename Vec8<T>::type*)(row + i);
+  typename Vec8<T>::type r;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r[j] = i + j < end ? row[i + j] : (T)-INFINITY;
+  return r;
+}
+
+// Writes a row's results from its joined statistics and sorted keys (`count` of them); one wave.
+__device__ inline void write_row(const ScoresArgs& a, int64_t row, const Stats& z, float logit, bool has, const Key* keys, int count) {
+  const int lane = threadIdx.x & 63;
+  const bool bad = !(z.s < INFINITY);  // a NaN or +infinity among the logits
+  const bool empty = z.m == -INFINITY && !bad;
+  const float log_s = logf(z.s), nan = __uint_as_float(0x7fc00000u);
+  if (lane == 0) {
+    if (a.logp) a.logp[row] = !has || empty ? 0.f : bad ? nan : (logit - z.m) * a.scale - log_s;
+    if (a.entropy) a.entropy[row] = bad ? nan : empty ? 0.f : log_s - LN2 * (z.t / z.s);
+    a.lse[row] = bad ? nan : empty ? -INFINITY : z.m * a.scale + log_s;
+  }
+  for (int j = lane; j < a.top; j += 64) {
+    const bool found = j < count && !bad && !empty;
+    a.top_id[row * a.top + j] = found ? (int64_t)(uint32_t)~(uint32_t)keys[j] : -1;
+    a.top_logp[row * a.top + j] = found ? (value_of(keys[j]) - z.m) * a.scale - log_s : bad ? nan : -INFINITY;
+  }
+}
+
+// A wave's pass over blocks first, first + step, ... of a row's elements [0, end).
+template <typename T, bool TOP>
+__device__ inline Stats scan(const T* row, int64_t first, int64_t step, int end, float c, Candidates& cand) {
+  const int lane = threadIdx.x & 63;
+  Stats z{-INFINITY, 0.f, 0.f};
+  typedef typename Vec8<T>::type Raw;
+  Raw next[2];
+  auto load = [&](int64_t b) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) next[h] = load_logits(row, (int)std::min<int64_t>(b * WAVE_BLOCK + h * 512 + lane * 8, 0x7ffffff0), end);
+  };
+  const int64_t blocks = ((int64_t)end + WAVE_BLOCK - 1) / WAVE_BLOCK;
+  bool begun = false;
+  if (first < blocks) load(first);
+  for (int64_t b = first; b < blocks; b += step) {
+    float x[EV];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[8 * h + j] = (float)next[h][j];
+    if (b + step < blocks) load(b + step);
+    float top = x[0];
+#pragma unroll
+    for (int j = 1; j < EV; ++j) top = fmaxf(top, x[j]);
+    const float m = fmaxf(z.m, top), ref = m == -INFINITY ? 0.f : m;
+    const float d = below(z.m, m, c), f = __builtin_amdgcn_exp2f(d);
+    float s[2] = {z.s * f, 0.f}, t[2] = {f * (z.t + z.s * d), 0.f};
+#pragma unroll
+    for (int j = 0; j < EV; ++j) {
+      const float u = (x[j] - ref) * c, e = __builtin_amdgcn_exp2f(u);
+      s[j & 1] += e;
+      t[j & 1] = __builtin_fmaf(e, fmaxf(u, -200.f), t[j & 1]);  // (of -infinity: 0 times that)
+    }
+    z.m = m, z.s = s[0] + s[1], z.t = t[0] + t[1];
+    if constexpr (TOP) {
+      if (!begun) cand.start(top), begun = true;
+      // (a value equal to the bound's has a higher index than all that are held: blocks come in order)
+      if (__any(ordered(top) > (uint32_t)(cand.bound >> 32))) {
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t i = (uint32_t)(b * WAVE_BLOCK + h * 512 + lane * 8);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) cand.offer(key_of(h ? x[8 + j] : x[j], i + j));
+        }
+      }
+    }
+  }
+  return z;
+}
+
+// A workgroup of a split row leaves its statistics, and behind all rows' statistics `top` sorted keys (0: none).
+__device__ inline Key* part_keys(const ScoresArgs& a, int64_t row) {
+  return (Key*)((Stats*)a.work + (a.n * a.parts + 1) / 2 * 2) + row * a.parts * a.top;
+}
+
+// WAVE: a wave per row, four rows per workgroup.  Else a workgroup per row, or (SPLIT) one of `parts` workgroups of a row.
+template <typename T, bool WAVE, bool SPLIT, bool TOP>
+__global__ __launch_bounds__(256) void scores_kernel(ScoresArgs a) {
+  __shared__ Key s_keys[TOP ? 4 : 1][TOP ? CAP : 1];
+  __shared__ Key s_best[MOST];
+  __shared__ Stats s_stats[4];
+  __shared__ int s_count[4];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t row = WAVE ? (int64_t)blockIdx.x * 4 + wave : SPLIT ? blockIdx.x / a.parts : blockIdx.x;
+  if (row >= a.n) return;  // whole waves, only where WAVE (no barriers)
+  const int part = SPLIT ? (int)(blockIdx.x - row * a.parts) : 0;
+  const T* x = (const T*)a.x + row * a.x_stride;
+  const float c = a.scale * LOG2E;
+  Candidates cand;
+  cand.init(s_keys[TOP ? wave : 0], a.top);
+  Stats z = scan<T, TOP>(x, WAVE ? 0 : part * 4 + wave, WAVE ? 1 : SPLIT ? 4 * a.parts : 4, a.V, c, cand);
+  z = lanes_join(z, c);
+  if (TOP) cand.cut();
+  const int64_t token = !SPLIT && a.token ? a.token[row] : -1;
+  const bool has = token >= 0 && token < a.V;
+  if constexpr (WAVE) {
+    write_row(a, row, z, has ? (float)x[token] : 0.f, has, cand.buf, cand.count);
+    return;
+  }
+  if (lane == 0) s_stats[wave] = z, s_count[wave] = cand.count;
+  __syncthreads();
+  int count = 0;
+  if constexpr (TOP) {  // ranks among all waves' keys
+#pragma unroll
+    for (int w = 0; w < 4; ++w) count += s_count[w];
+    if (lane < cand.count) {
+      const Key mine = cand.buf[lane];
+      int rank = 0;
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        for (int j = 0; j < s_count[w]; ++j) rank += s_keys[w][j] > mine;
+      if (rank < a.top) s_best[rank] = mine;
+    }
+    count = min(count, a.top);
+    __syncthreads();
+  }
+  if (wave) return;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) z = join(z, s_stats[w], c);
+  if constexpr (SPLIT) {
+    if (lane == 0) ((Stats*)a.work)[row * a.parts + part] = z;
+    if (TOP && lane < a.top) part_keys(a, row)[part * a.top + lane] = lane < count ? s_best[lane] : 0;
+  } else {
+    write_row(a, row, z, has ? (float)x[token] : 0.f, has, s_best, count);
+  }
+}
+
+// Joins the parts of a row; one wave per row.
+template <typename T>
+__global__ __launch_bounds__(64) void join_scores_kernel(ScoresArgs a) {
+  __shared__ Key s_keys[CAP];
+  const int lane = threadIdx.x;
+  const int64_t row = blockIdx.x;
+  const Stats* p = (const Stats*)a.work + row * a.parts;
+  const float c = a.scale * LOG2E;
+  Stats z{-INFINITY, 0.f, 0.f};
+  Candidates cand;
+  cand.init(s_keys, a.top);
+  for (int q = lane; q < a.parts; q += 64) z = join(z, p[q], c);
+  z = lanes_join(z, c);
+  if (a.top) {
+    const Key* keys = part_keys(a, row);
+    const int all = a.parts * a.top;
+    for (int i = 0; i < all; i += 256) {  // four loads at a time
+      Key k[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) k[j] = i + 64 * j + lane < all ? keys[i + 64 * j + lane] : 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) cand.offer(k[j]);
+    }
+    cand.cut();
+  }
+  const int64_t token = a.token ? a.token[row] : -1;
+  const bool has = token >= 0 && token < a.V;
+  write_row(a, row, z, has ? (float)((const T*)a.x + row * a.x_stride)[token] : 0.f, has, s_keys, cand.count);
+}
+
+// Gradient: a workgroup takes SEGMENT elements of a row, or (WAVE: rows of up to SEGMENT / 4) each of its waves a row.  The
+// elements whose own gradients are not 0 (the token and the alternatives) are marked in a bitmap, a bit for eight, so that an
+// element is written once: the result may be the logits' own memory.
+constexpr int SEGMENT = 8192;
+template <typename T, bool WAVE>
+__global__ __launch_bounds__(256) void scores_back_kernel(ScoresBackArgs a) {
+  constexpr int TPR = WAVE ? 64 : 256, LEN = WAVE ? SEGMENT / 4 : SEGMENT, WORDS = LEN / 8 / 32;
+  __shared__ int s_id[WAVE ? 4 : 1][MOST + 1];
+  __shared__ float s_own[WAVE ? 4 : 1][MOST + 1];
+  __shared__ uint32_t s_bits[WAVE ? 4 : 1][WORDS];
+  const int wave = threadIdx.x >> 6, t = threadIdx.x % TPR, sub = WAVE ? wave : 0;
+  const int64_t row = WAVE ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x / a.segments;
+  if (row >= a.n) return;  // whole waves, only where WAVE (no barriers)
+  const int first = WAVE ? 0 : (int)(blockIdx.x - row * a.segments) * LEN, end = (int)std::min<int64_t>((int64_t)first + LEN, a.V);
+  auto sync = [] {
+    if constexpr (WAVE) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    else __syncthreads();
+  };
+  const int64_t token = a.token ? a.token[row] : -1;
+  const float dlogp = a.dlogp && token >= 0 && token < a.V ? a.dlogp[row] : 0.f;
+  const float dH = a.dentropy ? a.dentropy[row] : 0.f, lse = a.lse[row];
+  // what lies at special places, by every wave: lane j has alternative j
+  const int lane = threadIdx.x & 63;
+  int64_t id = -1;
+  float dtop = 0.f;
+  if (a.dtop && lane < a.top) {
+    id = a.top_id[row * a.top + lane];
+    if (id >= 0 && id < a.V) dtop = a.dtop[row * a.top + lane];
+  }
+  const float all = lanes_sum<64>(dtop);
+  const float A = (a.dlse ? a.dlse[row] : 0.f) - dlogp - all - (dH == 0.f ? 0.f : dH * a.entropy[row]);
+  for (int i = t; i < WORDS; i += TPR) s_bits[sub][i] = 0;
+  if (t < 64) {
+    s_id[sub][lane] = dtop != 0.f ? (int)id : -1, s_own[sub][lane] = dtop;
+    if (lane == 0) s_id[sub][MOST] = dlogp != 0.f ? (int)token : -1, s_own[sub][MOST] = dlogp;
+  }
+  sync();
+  if (t < 64) {
+    auto mark = [&](int64_t v, float own) {
+      if (own != 0.f && v >= first && v < end) atomicOr(&s_bits[sub][(v - first) >> 8], 1u << ((v - first) >> 3 & 31));
+    };
+    mark(id, dtop);
+    if (lane == 0) mark(token, dlogp);
+  }
+  sync();
+  // a row that nothing is asked of, or may be said in (-infinity alone), gets zeros, whatever it holds
+  const bool none = lse == -INFINITY || A == 0.f && dH == 0.f && dlogp == 0.f && !__any(dtop != 0.f);
+  const T* x = (const T*)a.x + row * a.x_stride;
+  T* dx = (T*)a.dx + row * a.dx_stride;
+  constexpr int STEPS = LEN / 8 / TPR;
+  typename Vec8<T>::type raw[STEPS];
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) raw[k] = load_logits(x, std::min(first + 8 * (t + k * TPR), end), end);
+#pragma unroll
+  for (int q = 0; q < STEPS; ++q) {
+    const int i = first + 8 * (t + q * TPR), unit = t + q * TPR;
+    if (i >= end) break;
+    float v[8], own[8] = {};
+    if (s_bits[sub][unit >> 5] >> (unit & 31) & 1)
+      for (int k = 0; k <= MOST; ++k) {  // (in order: the same sum every time)
+        const int at = s_id[sub][k] - i;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) own[j] += at == j ? s_own[sub][k] : 0.f;
+      }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float logp = __builtin_fmaf((float)raw[q][j], a.scale, -lse), p = __builtin_amdgcn_exp2f(logp * LOG2E);
+      v[j] = none ? 0.f : a.scale * (p * (A - dH * fmaxf(logp, -200.f)) + own[j]);
+    }
+    store8(dx, i, end, v);
+  }
+}
+
+template <typename F>
+int with_type(dn_dtype dt, F&& f) {
+  if (dt == DN_F32) return f(float{});
+  if (dt == DN_F16) return f(_Float16{});
+  return f(__bf16{});
+}
+
+constexpr int SHORT = 2048;  // rows of up to so many logits: a wave each
+
+}  // namespace
+
+// Workgroups of a row: enough of them for the chip where there are few rows, of at least two blocks a wave.
+int32_t scores_parts(int64_t n, int32_t V) {
+  if (V <= SHORT || n >= 1024 || n == 0) return 1;
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({(1024 + n - 1) / n, V / (8 * WAVE_BLOCK), 64}));
+}
+size_t scores_bytes(int64_t n, int32_t V, int32_t top) {
+  const int64_t parts = scores_parts(n, V);
+  return parts == 1 ? 0 : sizeof(Stats) * (size_t)((n * parts + 1) / 2 * 2) + sizeof(Key) * (size_t)(n * parts) * top;
+}
+
+int launch_token_scores(const ScoresArgs& all, dn_dtype dt, void* stream) {
+  return with_type(dt, [&](auto v) {
+    using T = decltype(v);
+    const hipStream_t st = (hipStream_t)stream;
+    const bool wave = all.V <= SHORT;
+    const int64_t most = MAX_LAUNCH_THREADS / 256 / all.parts * (wave ? 4 : 1);
+    for (int64_t at = 0; at < all.n; at += most) {  // (more than one launch's rows: never split)
+      ScoresArgs a = all;
+      a.n = std::min(all.n - at, most);
+      a.x = (const T*)all.x + at * all.x_stride;
+      a.lse = all.lse + at;
+      if (all.token) a.token = all.token + at;
+      if (all.logp) a.logp = all.logp + at;
+      if (all.entropy) a.entropy = all.entropy + at;
+      if (all.top) a.top_id = all.top_id + at * all.top, a.top_logp = all.top_logp + at * all.top;
+      const auto run = [&](auto top) {
+        constexpr bool TOP = decltype(top)::value;
+        if (wave)
+          scores_kernel<T, true, false, TOP><<<dim3((unsigned)((a.n + 3) / 4)), 256, 0, st>>>(a);
+        else if (a.parts == 1)
+          scores_kernel<T, false, false, TOP><<<dim3((unsigned)a.n), 256, 0, st>>>(a);
+        else
+          scores_kernel<T, false, true, TOP><<<dim3((unsigned)(a.n * a.parts)), 256, 0, st>>>(a);
+      };
+      if (a.top) run(std::true_type{});
+      else run(std::false_type{});
+      if (const int err = (int)hipGetLastError()) return err;
+      if (a.parts > 1) {
+        join_scores_kernel<T><<<dim3((unsigned)a.n), 64, 0, st>>>(a);
+        if (const int err = (int)hipGetLastError()) return err;
+      }
+    }
+    return 0;
+  });
+}
+
+int launch_token_scores_backward(const ScoresBackArgs& all, dn_dtype dt, void* stream) {
+  return with_type(dt, [&](auto v) {
+    using T = decltype(v);
+    const bool wave = all.V <= SHORT;
+    const int64_t segments = wave ? 1 : ((int64_t)all.V + SEGMENT - 1) / SEGMENT;
+    const int64_t most = MAX_LAUNCH_THREADS / 256 / segments * (wave ? 4 : 1);
+    for (int64_t at = 0; at < all.n; at += most) {
+      ScoresBackArgs a = all;
+      a.n = std::min(all.n - at, most), a.segments = (int32_t)segments;
+      a.x = (const T*)all.x + at * all.x_stride, a.dx = (T*)all.dx + at * all.dx_stride;
+      a.lse = all.lse + at;
+      if (all.token) a.token = all.token + at;
+      if (all.entropy) a.entropy = all.entropy + at;
+      if (all.dlogp) a.dlogp = all.dlogp + at;
+      if (all.dentropy) a.dentropy = all.dentropy + at;
+      if (all.dlse) a.dlse = all.dlse + at;
+      if (all.dtop) a.dtop = all.dtop + at * all.top, a.top_id = all.top_id + at * all.top;
+      if (wave)
+        scores_back_kernel<T, true><<<dim3((unsigned)((a.n + 3) / 4)), 256, 0, (hipStream_t)stream>>>(a);
+      else
+        scores_back_kernel<T, false><<<dim3((unsigned)(a.n * segments)), 256, 0, (hipStream_t)stream>>>(a);
+      if (const int err = (int)hipGetLastError()) return err;
+    }
+    return 0;
+  });
+}
+
+}  // namespace head
+}  // namespace dn

@@ -1,0 +1,528 @@
+"""The operators of a head in 8 bits (blocks of 128 in e4m3, their products, scores of logits, Muon) through the binding, against
+plain forms in 64 bits.
+
+Tolerances.  unit(type) is half a unit in the last place relative to a value: 2^-24, 2^-11, 2^-8 for fp32, fp16, bf16, 2^-4 for
+e4m3 (and 2^-10 of the scale for codes near 0, whose step is 2^-9); a stored result may be off by that, fp16's by 2^-25 near 0.
+What is computed in 32 bits before it is bounded from its terms: a sum of C products by (C / 8 + 16) 2^-24 of the sum of their
+magnitudes (eight or more are added at a time).
+"""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+UNIT = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f32": 1e-37, "f16": 2.0 ** -25, "bf16": 1e-37}
+F8 = torch.float8_e4m3fn
+E24 = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def D():
+    from paper_1404_1869_amd import densenet
+    assert torch.cuda.is_available()
+    densenet.lib()
+    return densenet
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def rows(g, n, C, dt, pad=0, scale=1.0, offset=0):
+    """[n][C] of normal values of uneven size, rows C + pad apart, the first `offset` elements into its memory."""
+    flat = (torch.randn(n * (C + pad) + offset, generator=g, device="cuda") * scale)
+    x = flat[offset:].view(n, C + pad)
+    x *= torch.exp(torch.randn(n, 1, generator=g, device="cuda"))
+    return flat.to(DT[dt])[offset:].view(n, C + pad)[:, :C]
+
+
+def same(got, want):
+    """Equal bit for bit, NaN and all."""
+    if got.dtype == F8:
+        got, want = got.contiguous().view(torch.uint8), want.contiguous().view(torch.uint8)
+    return got.shape == want.shape and torch.equal(torch.nan_to_num(got.double(), nan=1e300), torch.nan_to_num(want.double(), nan=1e300))
+
+
+def within(got, want, bound, what):
+    got, want = got.double(), want.double()
+    off = (got - want).abs()
+    bad = ~((off <= bound) | (got == want))
+    assert not bool(bad.any()), f"{what}: {int(bad.sum())} of {bad.numel()} off, by up to {float((off / bound)[bad].max()):.2f} bounds"
+
+
+def up(v, to=128):
+    return -(-v // to)
+
+
+def spread(scale, rows, n, C):
+    """A scale for each value."""
+    wide = scale.double().repeat_interleave(128, 1)[:, :C]
+    return wide if rows == 1 else wide.repeat_interleave(128, 0)[:n]
+
+
+def tops(x, rows):
+    n, C = x.shape
+    b = torch.nn.functional.pad(x.double(), (0, -C % 128, 0, -n % rows)).view(up(n, rows), rows, up(C), 128)
+    return b.abs().amax((1, 3))
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Quantising
+# ---------------------------------------------------------------------------------------------------------------------
+QUANT = [  # n, C, type, row padding, first element
+    (1, 1, "f32", 0, 0), (1, 4096, "bf16", 0, 0), (128, 128, "f16", 0, 0), (129, 127, "bf16", 3, 1), (5, 1000, "f32", 0, 0),
+    (300, 257, "f16", 8, 0), (1025, 641, "bf16", 0, 3), (17, 9216, "f32", 0, 0), (2000, 130, "bf16", 1, 0),
+]
+
+
+@pytest.mark.parametrize("n,C,dt,pad,off", QUANT)
+@pytest.mark.parametrize("block", [1, 128])
+def test_quantize(D, n, C, dt, pad, off, block):
+    g = gen(n * 7 + C)
+    x = rows(g, n, C, dt, pad, 0.01, off)
+    x[-1, :C // 2] = 0
+    q, k, t, tk = D.densenet_quantize_blocks(x, rows=block, turned=True)
+    assert q.shape == (n, C) and t.shape == (C, n) and q.dtype == t.dtype == F8 and q.stride(0) % 16 == 0
+    for codes, scale, want in ((q, k, x), (t, tk, x.T)):
+        m = want.shape
+        assert scale.shape == (m[0] if block == 1 else up(m[0]), up(m[1]))
+        within(scale, tops(want, block) / 448, 2 * E24 * tops(want, block) / 448, "scale")
+        wide = spread(scale, block, *m)
+        within(codes.double() * wide, want, (2.0 ** -4 + 4 * E24) * want.double().abs() + wide * 2.0 ** -10 * (1 + 2.0 ** -10), "values")
+    if block == 128:
+        assert same(t, q.T) and same(tk, k.T)
+    # each form alone, and in given memory of other strides, whose surroundings stay as they are
+    a = D.densenet_quantize_blocks(x, rows=block)
+    b = D.densenet_quantize_blocks(x, rows=block, codes=False, turned=True)
+    assert same(a[0], q) and torch.equal(a[1], k) and a[2] is None and a[3] is None
+    assert same(b[2], t) and torch.equal(b[3], tk) and b[0] is None and b[1] is None
+    held = torch.full((n + 1, C + 5), 7, dtype=torch.uint8, device="cuda")
+    turned = torch.full((C + 1, n + 3), 7, dtype=torch.uint8, device="cuda")
+    D.densenet_quantize_blocks(x, rows=block, out=held.view(F8)[:n, 1:C + 1], turned_out=turned.view(F8)[:C, 2:n + 2])
+    assert same(held.view(F8)[:n, 1:C + 1], q) and same(turned.view(F8)[:C, 2:n + 2], t)
+    for m, (r, c0, c1) in ((held, (n, 1, C + 1)), (turned, (C, 2, n + 2))):
+        assert bool((m[r:] == 7).all()) and bool((m[:, :c0] == 7).all()) and bool((m[:, c1:] == 7).all())
+
+
+def test_quantize_agrees_with_the_norm(D):
+    g = gen(5)
+    x = rows(g, 37, 1000, "bf16")
+    y, _, _ = D.densenet_rms_norm(x, out_dtype=D.DN_F32)
+    q, _, k = D.densenet_rms_norm(x, out_dtype=D.DN_F8, block=128)
+    a, b, _, _ = D.densenet_quantize_blocks(y, rows=1)
+    assert same(a, q) and torch.equal(b, k)
+
+
+@pytest.mark.parametrize("block", [1, 128])
+def test_quantize_special_values(D, block):
+    x = torch.zeros(256, 256, device="cuda")
+    x[0, 0], x[1, 1], x[2, 2], x[3, 3] = float("nan"), float("inf"), -float("inf"), 3.0
+    x[200, 130:140] = 1e-37  # a block too small for a scale's reciprocal
+    x[5, 140] = 3e38
+    q, k, t, tk = D.densenet_quantize_blocks(x, rows=block, turned=True)
+    for c in (q, t):
+        f = c.float()
+        assert bool(f[0, 0].isnan()) and bool(f[1, 1].isnan()) and bool(f[2, 2].isnan()) and int(f.isnan().sum()) == 3
+        assert float(f[3, 3]) == 448.0
+    assert float(q[5, 140].float()) == 448.0 and bool(torch.isfinite(k).all()) and bool(torch.isfinite(tk).all())
+    assert float(q[200].float().abs().max()) == 0 and float(t[:, 200].float().abs().max()) == 0
+    e = torch.empty(0, 100, device="cuda")
+    q, k, t, tk = D.densenet_quantize_blocks(e, rows=block, turned=True)
+    assert q.shape == (0, 100) and t.shape == (100, 0)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Products
+# ---------------------------------------------------------------------------------------------------------------------
+def operands(D, g, n, C, V, how="rows"):
+    a, ak, _, _ = D.densenet_quantize_blocks(rows(g, n, C, "f32"), rows=1)
+    w, wk, _, _ = D.densenet_quantize_blocks(rows(g, V, C, "f32", scale=0.05), rows=128)
+    if how == "tight":  # rows of C codes: not on 16 bytes unless C is a multiple of 16
+        a, w = (t.view(torch.uint8).contiguous().view(F8) for t in (a, w))
+    elif how == "odd":
+        def odd(t):
+            m = torch.full((t.shape[0], t.shape[1] + 7), 0x7f, dtype=torch.uint8, device="cuda")  # NaN around the codes
+            m[:, 3:3 + t.shape[1]] = t.view(torch.uint8)
+            return m.view(F8)[:, 3:3 + t.shape[1]]
+        a, w = odd(a), odd(w)
+    elif how == "rows":  # NaN in what is left of each row's last 16 bytes
+        for t in (a, w):
+            b = t.view(torch.uint8)
+            torch.as_strided(b, (b.shape[0], b.stride(0)), b.stride())[:, C:] = 0x7f
+    return a, ak, w, wk
+
+
+def plain_product(a, ak, w, wk):
+    n, C = a.shape
+    x, y = a.double() * spread(ak, 1, n, C), w.double() * spread(wk, 128, w.shape[0], C)
+    return x @ y.T, x.abs() @ y.abs().T
+
+
+def cut_off(a, ak, w, wk):
+    """What the 8-bit matrix instructions may leave out of results in 16 bits: of each eight products' bits those below 2^-13 of the
+    largest's leading one, so seven times 2^-13 of the largest of each eight at most.  (The largest of a times the largest of w.)"""
+    n, C = a.shape
+    pad = lambda t: torch.nn.functional.pad(t, (0, -C % 8)).view(len(t), -1, 8).abs().amax(2)  # noqa: E731
+    x, y = a.double() * spread(ak, 1, n, C), w.double() * spread(wk, 128, w.shape[0], C)
+    return 7 * 2.0 ** -13 * pad(x) @ pad(y).T
+
+
+PRODUCT = [  # n, C, V, y type, layout
+    (1, 1, 1, "f32", "rows"), (1, 4096, 500, "bf16", "rows"), (3, 16, 33, "f16", "rows"), (2, 17, 130, "f32", "rows"),
+    (32, 128, 128, "bf16", "rows"), (33, 129, 127, "f32", "rows"), (64, 1000, 300, "f16", "rows"), (65, 255, 257, "f32", "rows"),
+    (128, 512, 1024, "bf16", "rows"), (129, 2047, 129, "f32", "rows"), (300, 96, 700, "bf16", "rows"), (257, 640, 513, "f32", "rows"),
+    (1000, 384, 1000, "f16", "rows"), (520, 9216, 21, "f32", "rows"), (21, 9216, 520, "f32", "rows"), (700, 100, 900, "f32", "tight"),
+    (5, 1000, 300, "bf16", "odd"), (200, 333, 150, "f32", "odd"), (2049, 130, 2050, "bf16", "rows"), (1, 9216, 1, "f32", "rows"),
+]
+
+
+@pytest.mark.parametrize("n,C,V,yt,how", PRODUCT)
+def test_product(D, n, C, V, yt, how):
+    g = gen(n * 31 + C * 7 + V)
+    a, ak, w, wk = operands(D, g, n, C, V, how)
+    held = torch.full((n + 1, V + 9), 5.0, dtype=DT[yt], device="cuda")
+    y = held[:n, 4:V + 4]
+    got = D.densenet_block_product(a, ak, w, wk, out_dtype=D.DTYPES[yt], out=y)
+    assert got is y
+    want, size = plain_product(a, ak, w, wk)
+    lost = 0 if yt == "f32" else cut_off(a, ak, w, wk)
+    within(y, want, UNIT[yt] * (want.abs() + lost) + lost + (C / 8 + 16) * E24 * size + TINY[yt], "y")
+    assert bool((held[n:] == 5).all()) and bool((held[:, :4] == 5).all()) and bool((held[:, V + 4:] == 5).all())
+    assert torch.equal(D.densenet_block_product(a, ak, w, wk, out_dtype=D.DTYPES[yt]), y)  # the same bits every time
+
+
+def test_product_special_values(D):
+    g = gen(9)
+    a, ak, w, wk = operands(D, g, 40, 300, 50)
+    a.view(torch.uint8)[3, 299] = 0x7f   # a NaN in the last block of row 3 of a, one in the first of row 7 of w
+    w.view(torch.uint8)[7, 0] = 0xff
+    ak[5, 1] = float("inf")
+    y = D.densenet_block_product(a, ak, w, wk, out_dtype=0)
+    bad = torch.zeros(40, 50, dtype=torch.bool, device="cuda")
+    bad[3], bad[:, 7] = True, True
+    assert bool(y[bad].isnan().all()) and not bool(torch.isfinite(y[5]).any())
+    bad[5] = True
+    assert bool(torch.isfinite(y[~bad]).all())
+    assert D.densenet_block_product(a[:0], ak[:0], w, wk).shape == (0, 50)
+    # scales far apart from block to block
+    a, ak, w, wk = operands(D, g, 10, 1000, 70)
+    ak *= 10.0 ** torch.linspace(-12, 12, 8, device="cuda")
+    want, size = plain_product(a, ak, w, wk)
+    within(D.densenet_block_product(a, ak, w, wk, out_dtype=0), want, (1000 / 8 + 16) * E24 * size, "y")
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Scores
+# ---------------------------------------------------------------------------------------------------------------------
+def plain_scores(x, token, scale, top):
+    z = x.double() * scale
+    lse = torch.logsumexp(z, 1)
+    logp = z - lse[:, None]
+    p = logp.exp()
+    H = -torch.where(p > 0, p * logp, 0.0).sum(1)
+    has = (token >= 0) & (token < x.shape[1])
+    at = torch.where(has, logp.gather(1, token.clamp(0, x.shape[1] - 1)[:, None])[:, 0], 0.0)
+    v, ids = x.double().sort(dim=1, descending=True, stable=True)
+    ids = torch.where(v == -math.inf, -1, ids)[:, :top]
+    ids = torch.nn.functional.pad(ids, (0, top - ids.shape[1]), value=-1)
+    best = torch.where(ids >= 0, logp.gather(1, ids.clamp(min=0)), -math.inf) if top else None
+    # moments of the distance to the maximum, which errors grow with
+    u = torch.where(p > 0, z - z.amax(1, keepdim=True), 0.0)
+    d1, d2 = (p * u.abs()).sum(1), (p * u * u).sum(1)
+    return at, H, lse, ids, best, d1, d2, z.amax(1).abs()
+
+
+def logits(g, n, V, dt, pad=0, masked=0.0, offset=0):
+    x = 3 * torch.randn(n * (V + pad) + offset, generator=g, device="cuda")
+    x = torch.where(torch.rand(x.shape, generator=g, device="cuda") < masked, -math.inf, x).to(DT[dt])
+    x = x[offset:].view(n, V + pad)[:, :V]
+    x[:, 0] = torch.where(x[:, 0] == -math.inf, 0.0, x[:, 0])  # (no empty rows here)
+    return x
+
+
+SCORES = [  # n, V, type, top, scale, masked, row padding, first element
+    (1, 1, "f32", 1, 1.0, 0.0, 0, 0), (1, 131072, "bf16", 20, 1.25, 0.1, 0, 0), (3, 7, "f16", 10, 1.0, 0.0, 0, 1),
+    (130, 100, "bf16", 64, 0.5, 0.3, 3, 0), (9, 2048, "f32", 5, 2.0, 0.0, 0, 0), (6, 2049, "f16", 64, 1.0, 0.5, 7, 3),
+    (1100, 2500, "bf16", 3, 1.0, 0.0, 0, 0), (2, 50257, "f32", 64, 1.0, 0.9, 0, 0), (33, 16385, "f16", 1, 1.0, 0.0, 5, 0),
+    (5, 32000, "bf16", 0, 1.0, 0.0, 0, 0), (70, 300, "f32", 0, 3.0, 0.0, 1, 1), (1, 1000003, "bf16", 64, 1.0, 0.0, 0, 0),
+    (4, 65, "f32", 64, 1.0, 0.99, 0, 0),
+]
+
+
+@pytest.mark.parametrize("n,V,dt,top,scale,masked,pad,off", SCORES)
+def test_scores(D, n, V, dt, top, scale, masked, pad, off):
+    g = gen(n * 11 + V)
+    x = logits(g, n, V, dt, pad, masked, off)
+    token = torch.randint(-1, V + 1, (n,), generator=g, device="cuda")
+    logp, H, lse, ids, best = D.densenet_token_scores(x, token, top=top, scale=scale)
+    at, wH, wl, wi, wb, d1, d2, big = plain_scores(x, token, scale, top)
+    # log of the sum: each term is off by 3 roundings of its exponent (d1 of them, weighed) and two of the exponential; a lane adds
+    # V / 128 of them at most one after the other, and 24 joins follow
+    log_sum = E24 * (4 * d1 + V / 128 + 64)
+    within(lse, wl, log_sum + E24 * 4 * (big + wl.abs()), "lse")
+    within(H, wH, log_sum + E24 * (4 * d2 + 4 * d1 + (V / 128 + 64) * d1 + 4 * wH.abs()), "entropy")
+    within(logp, at, log_sum + E24 * 4 * at.abs(), "logp")
+    if top:
+        assert torch.equal(ids, wi), "ids"
+        within(torch.nan_to_num(best, neginf=0.0), torch.nan_to_num(wb, neginf=0.0),
+               log_sum[:, None] + E24 * 4 * torch.nan_to_num(wb, neginf=0.0).abs(), "best")
+        assert torch.equal(best == -math.inf, wi < 0)
+    else:
+        assert ids is None and best is None
+    again = D.densenet_token_scores(x, token, top=top, scale=scale)
+    for a, b in zip(again, (logp, H, lse, ids, best)):
+        assert b is None or torch.equal(a, b)
+    assert D.densenet_token_scores(x, None, top=top, scale=scale)[0] is None
+
+
+@pytest.mark.parametrize("V", [100, 3000, 70000])
+def test_scores_ties_and_order(D, V):
+    """Rows of equal values, in rising and falling order, and of 0 and -0: indices go by value and then by place."""
+    i = torch.arange(V, device="cuda").float()
+    x = torch.stack([torch.zeros(V, device="cuda"), i, -i, (i % 2) * -0.0, i % 7, -(i // 50), torch.full((V,), -5.0, device="cuda")])
+    x[3, ::2] = 0.0
+    x[3, 1::2] = -0.0
+    token = torch.zeros(7, dtype=torch.int64, device="cuda")
+    for dt in ("f32", "bf16"):
+        ids = D.densenet_token_scores(x.to(DT[dt]), token, top=64)[3]
+        want = plain_scores(x.to(DT[dt]), token, 1.0, 64)[3]
+        assert torch.equal(ids, want)
+
+
+@pytest.mark.parametrize("V", [10, 5000, 40000])
+def test_scores_of_empty_and_broken_rows(D, V):
+    g = gen(V)
+    x = logits(g, 6, V, "f32")
+    x[1] = -math.inf                # nothing may be said
+    x[2], x[2, V // 2] = -math.inf, 3.0   # one word may
+    x[3, V - 1] = float("nan")
+    x[4, V // 3] = math.inf
+    x[5] = torch.where(x[5] == 0, 0.0, torch.finfo(torch.float32).min)  # the type's lowest value as a mask, everywhere but ...
+    x[5, 1] = 2.0                   # ... here
+    token = torch.tensor([0, 0, V // 2, 0, 0, 1], device="cuda")
+    logp, H, lse, ids, best = D.densenet_token_scores(x, token, top=3)
+    assert float(lse[1]) == -math.inf and float(logp[1]) == 0 and float(H[1]) == 0
+    assert ids[1].tolist() == [-1] * 3 and best[1].tolist() == [-math.inf] * 3
+    assert float(logp[2]) == 0 and float(H[2]) == 0 and ids[2].tolist() == [V // 2, -1, -1] and float(best[2, 0]) == 0
+    for r in (3, 4):
+        assert all(bool(t[r].isnan().all()) for t in (logp, H, lse, best)) and ids[r].tolist() == [-1] * 3
+    assert float(logp[5]) == 0 and float(H[5]) == 0 and int(ids[5, 0]) == 1
+    assert bool(torch.isfinite(lse[0])) and bool(torch.isfinite(H[0]))
+    # the gradient: nothing where nothing may be said; where nothing is asked, zeros whatever a row holds
+    one = torch.ones(6, device="cuda")
+    dx = D.densenet_token_scores_backward(x, token, lse, entropy=H, dlogp=one, dentropy=one, top_id=ids, dtop=torch.ones(6, 3, device="cuda"))
+    assert bool(torch.isfinite(dx[[0, 1, 2, 5]]).all()) and float(dx[1].abs().max()) == 0 and bool(dx[3].isnan().any())
+    none = torch.zeros(6, device="cuda")
+    dx = D.densenet_token_scores_backward(x, token, lse, entropy=H, dlogp=none, dentropy=none)
+    assert float(dx.abs().max()) == 0
+    e = x[:0]
+    assert [t.shape[0] for t in D.densenet_token_scores(e, token[:0], top=2)] == [0] * 5
+    assert D.densenet_token_scores_backward(e, token[:0], lse[:0], dlogp=none[:0]).shape == (0, V)
+
+
+def plain_back(x, token, lse, H, dlogp, dH, dlse, ids, dtop, scale):
+    z = x.double() * scale - lse.double()[:, None]
+    p = z.exp()
+    V = x.shape[1]
+    dl = torch.where((token >= 0) & (token < V), dlogp.double(), 0.0)
+    dt = torch.where(ids >= 0, dtop.double(), 0.0) if dtop is not None else torch.zeros(len(x), 1, device="cuda", dtype=torch.float64)
+    A = dlse.double() - dl - dt.sum(1) - dH.double() * H.double()
+    logp = torch.where(p > 0, z, 0.0)
+    d = p * (A[:, None] - dH.double()[:, None] * logp)
+    size = dlse.double().abs() + dl.abs() + dt.abs().sum(1) + (dH * H).double().abs()
+    big = p * (size[:, None] + dH.double().abs()[:, None] * logp.abs()) * (logp.abs() + 8)
+    for j in range(dt.shape[1] if dtop is not None else 0):
+        r = torch.arange(len(x), device="cuda")
+        d[r, ids[:, j].clamp(min=0)] += dt[:, j]
+        big[r, ids[:, j].clamp(min=0)] += dt[:, j].abs()
+    d[torch.arange(len(x), device="cuda"), token.clamp(0, V - 1)] += dl
+    big[torch.arange(len(x), device="cuda"), token.clamp(0, V - 1)] += dl.abs()
+    return d * scale, big * scale
+
+
+BACK = [(1, 1, "f32", 1, 1.0, 0.0, 0, 0), (3, 7, "f16", 4, 1.0, 0.0, 1, 0), (130, 100, "bf16", 64, 0.5, 0.3, 3, 0), (9, 2048, "f32", 5, 2.0, 0.0, 0, 0),
+        (6, 2049, "f16", 64, 1.0, 0.5, 7, 3), (5, 8193, "bf16", 3, 1.0, 0.0, 0, 0), (2, 50257, "f32", 0, 1.0, 0.1, 0, 1),
+        (1, 131072, "bf16", 20, 1.25, 0.1, 0, 0)]
+
+
+@pytest.mark.parametrize("n,V,dt,top,scale,masked,pad,off", BACK)
+def test_scores_gradient(D, n, V, dt, top, scale, masked, pad, off):
+    g = gen(n * 13 + V)
+    x = logits(g, n, V, dt, pad, masked, off)
+    token = torch.randint(-1, V + 1, (n,), generator=g, device="cuda")
+    logp, H, lse, ids, _ = D.densenet_token_scores(x, token, top=top, scale=scale)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    dlogp, dH, dlse, dtop = r(n), 0.1 * r(n), r(n), r(n, top) if top else None
+    if top > 1:
+        ids[:, 1] = ids[:, 0]        # one alternative twice
+        ids[::2, 0] = token[::2]     # the token among them (also where it lies outside: -1 or V)
+    dx = D.densenet_token_scores_backward(x, token, lse, entropy=H, dlogp=dlogp, dentropy=dH, dlse=dlse, top_id=ids, dtop=dtop, scale=scale)
+    known = torch.where(ids < V, ids, -1) if top else None
+    want, size = plain_back(x, token, lse, H, dlogp, dH, dlse, known, dtop, scale)
+    # exponent: 3 roundings of log p; A: a rounding for each term added (top + 4), in units of all of them
+    bound = UNIT[dt] * want.abs() + E24 * (4 + top / 4) * size + TINY[dt]
+    within(dx, want, bound, "dx")
+    # into the logits' own memory, and into another place that is left as it is around
+    held = torch.full((n, V + 3), 5.0, dtype=DT[dt], device="cuda")
+    args = dict(entropy=H, dlogp=dlogp, dentropy=dH, dlse=dlse, top_id=ids, dtop=dtop, scale=scale)
+    D.densenet_token_scores_backward(x, token, lse, out=held[:, 1:V + 1], **args)
+    assert torch.equal(held[:, 1:V + 1], dx) and bool((held[:, 0] == 5).all()) and bool((held[:, V + 1:] == 5).all())
+    own = x.clone()
+    assert D.densenet_token_scores_backward(own, token, lse, out=own, **args) is own and torch.equal(own, dx)
+    # each gradient alone
+    parts = [D.densenet_token_scores_backward(x, token, lse, dlogp=dlogp, scale=scale),
+             D.densenet_token_scores_backward(x, token, lse, entropy=H, dentropy=dH, scale=scale),
+             D.densenet_token_scores_backward(x, None, lse, dlse=dlse, scale=scale)]
+    if top:
+        parts.append(D.densenet_token_scores_backward(x, None, lse, top_id=ids, dtop=dtop, scale=scale))
+    total = sum(t.double() for t in parts)
+    within(total, want, UNIT[dt] * sum(t.double().abs() for t in parts) + 4 * E24 * (4 + top / 4) * size + 4 * TINY[dt], "parts")
+
+
+def test_scores_gradient_against_differences(D):
+    g = gen(3)
+    x = logits(g, 4, 40, "f32").double()
+    token = torch.tensor([3, 0, 39, 7], device="cuda")
+    c = torch.randn(4, 3, generator=g, device="cuda").double()
+
+    def f(x):
+        at, H, lse, _, _, _, _, _ = plain_scores(x, token, 0.7, 0)
+        return (c[:, 0] * at + c[:, 1] * H + c[:, 2] * lse).sum()
+
+    _, H, lse, _, _ = D.densenet_token_scores(x.float(), token, scale=0.7)
+    k = [c[:, i].float().contiguous() for i in range(3)]
+    dx = D.densenet_token_scores_backward(x.float(), token, lse, entropy=H, dlogp=k[0], dentropy=k[1], dlse=k[2], scale=0.7)
+    for v in (0, 3, 17, 39):
+        step = torch.zeros_like(x)
+        for r in range(4):
+            step.zero_()
+            step[r, v] = 1e-5
+            want = (f(x.float().double() + step) - f(x.float().double() - step)) / 2e-5
+            # central differences: 1e-10 of third derivatives of size 1, 1e-15 of values of size 10 over 2e-5; and fp32's roundings
+            assert abs(float(dx[r, v]) - float(want)) < 1e-8 + 40 * E24 * float(c[r].abs().sum()) * 8
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Muon
+# ---------------------------------------------------------------------------------------------------------------------
+NS = (3.4445, -4.7750, 2.0315)
+
+
+def plain_muon(p, g, m, lr, beta, nesterov, wd, steps, coefs, eps, gs, rate, unit):
+    """The step in 64 bits, and a bound of X's error in the Frobenius norm where every value held is rounded to `unit`."""
+    x = g.double() * gs
+    m = m.double() * beta + x if m is not None else None
+    u = x if m is None else x + beta * m if nesterov else m
+    tall = u.shape[0] > u.shape[1]
+    X = (u.T if tall else u)
+    X = X / (torch.linalg.vector_norm(X) + eps)
+    norm = lambda t: float(torch.linalg.vector_norm(t))  # noqa: E731
+    spec = lambda t: float(torch.linalg.matrix_norm(t, 2))  # noqa: E731
+    err = 2 * unit * norm(X)
+    for a, b, c in coefs:
+        A = X @ X.T
+        P = b * A + c * A @ A
+        s = max(spec(X) + err, 1e-30)
+        # dA from X's error on either side, and from rounding A; of P likewise; of the new X from all, and rounding it
+        dA = 2 * s * err + 2 * unit * norm(A)
+        dP = abs(b) * dA + abs(c) * (2 * s * s * dA + 2 * unit * norm(A) * norm(A)) + 2 * unit * norm(P)
+        new = a * X + P @ X
+        err = abs(a) * err + spec(P) * err + dP * s + 2 * unit * norm(new) + 2 * unit * norm(P) * norm(X)
+        X = new
+    X = X.T if tall else X
+    return p.double() * (1 - lr * wd) - lr * rate * X, m, lr * rate * err
+
+
+MUON = [  # shapes, p type, g type, copy type, nesterov, momentum state, steps
+    ([(1, 1)], "f32", "f32", None, True, True, 1), ([(5, 7)], "f32", "f32", "bf16", True, True, 2), ([(7, 5)], "f32", "bf16", None, False, True, 2),
+    ([(64, 64), (128, 200), (200, 128)], "f32", "bf16", "bf16", True, True, 1), ([(1, 300), (300, 1)], "f32", "f32", "f16", True, True, 2),
+    ([(129, 257), (257, 129), (130, 130)], "bf16", "bf16", None, True, True, 1), ([(33, 1000)], "f16", "f16", None, True, False, 1),
+    ([(150, 1030), (1030, 150)], "f32", "f16", "bf16", True, True, 2),
+]
+
+
+@pytest.mark.parametrize("shapes,pt,gt,ct,nesterov,state,steps", MUON)
+def test_muon(D, shapes, pt, gt, ct, nesterov, state, steps):
+    g = gen(sum(r * 3 + c for r, c in shapes))
+    r = lambda s, dt, k: (torch.randn(s, generator=g, device="cuda") * k).to(DT[dt])  # noqa: E731
+    p, gr = [r(s, pt, 0.02) for s in shapes], [r(s, gt, 0.01) for s in shapes]
+    m = [r(s, "f32", 0.1) for s in shapes]
+    copies = [torch.empty(s, dtype=DT[ct], device="cuda") for s in shapes] if ct else None
+    beta = 0.9 if state else 0.0
+    rates = [0.2 * max(s) ** 0.5 for s in shapes]
+    unit = 2.0 ** -11 if pt == "bf16" else 2.0 ** -20   # two parts: 22 bits, products of which three of four are taken
+    want = [plain_muon(a, b, c if state else None, 0.02, beta, nesterov, 0.1, steps, [NS] * steps, 1e-7, 0.5, k, unit)
+            for a, b, c, k in zip(p, gr, m, rates)]
+    plan = D.MuonPlan(p, gr, m, copies=copies, rates=rates)
+    D.densenet_muon(plan, lr=0.02, momentum=beta, nesterov=nesterov, weight_decay=0.1, steps=steps, grad_scale=0.5)
+    for i, (wp, wm, err) in enumerate(want):
+        if state:
+            within(m[i], wm, 4 * E24 * (wm.abs() + gr[i].double().abs()), "m")
+        # no element is further off than the whole is in the Frobenius norm, and rounded once
+        bound = err + (UNIT[pt] + 4 * E24) * (wp.abs() + err) + 2 * E24 * p[i].double().abs() + TINY[pt]
+        within(p[i], wp, bound, "p")
+        off = float(torch.linalg.vector_norm(p[i].double() - wp))
+        assert off <= err + 2 * (UNIT[pt] + 4 * E24) * float(torch.linalg.vector_norm(wp)) + 1e-30
+        if ct:
+            within(copies[i], wp, bound + UNIT[ct] * (wp.abs() + err) + TINY[ct], "copy")
+
+
+@pytest.mark.parametrize("pt", ["f32", "bf16"])
+def test_muon_orthogonalises(D, pt):
+    """Five steps bring all singular values above 1e-2 of the largest to between 0.68 and 1.21 (by the polynomial's own course), from
+    updates as training has them: few strong directions over noise.  The result is that of 64 bits, to the roundings' size."""
+    g = gen(77)
+    shapes = [(200, 700), (700, 200), (256, 256)]
+    ups = []
+    for a, b in shapes:
+        u = torch.linalg.qr(torch.randn(a, min(a, b), generator=g, device="cuda", dtype=torch.float64))[0]
+        v = torch.linalg.qr(torch.randn(b, min(a, b), generator=g, device="cuda", dtype=torch.float64))[0]
+        s = torch.logspace(0, -2, min(a, b), device="cuda", dtype=torch.float64)
+        ups.append((u * s) @ v.T)
+    p = [torch.zeros(s, dtype=DT[pt], device="cuda") for s in shapes]
+    gr = [u.float() for u in ups]
+    plan = D.MuonPlan(p, gr, rates=[1.0] * 3)
+    D.densenet_muon(plan, lr=1.0, momentum=0.0)
+    for q, u in zip(p, gr):
+        want = plain_muon(torch.zeros_like(q), u, None, 1.0, 0.0, True, 0.0, 5, [NS] * 5, 1e-7, 1.0, 1.0, 0.0)[0]
+        s = torch.linalg.svdvals(q.double())
+        ws = torch.linalg.svdvals(want)
+        # A rounding of unit e to each value turns X by about e |X|, and each of the five steps grows that by at most 3.45 where
+        # singular values are small and less than 1.1 where they have grown; small ones take about three steps to grow: 3.45^3 = 41.
+        # The roundings are random: of r c values with step e |x| they add up to e |X| in the Frobenius norm, e in any direction.
+        e = 41 * 5 * (2.0 ** -11 if pt == "bf16" else 2.0 ** -20)
+        assert float(torch.linalg.matrix_norm(q.double() - want, 2)) <= e + 2 * UNIT[pt]
+        assert float((s - ws).abs().max()) <= e + 2 * UNIT[pt]
+
+
+def test_muon_coefficients_for_each_step_and_zero_updates(D):
+    g = gen(6)
+    p, u = torch.zeros(60, 90, device="cuda"), torch.randn(60, 90, generator=g, device="cuda")
+    coefs = [(4.0, -6.0, 3.0), (3.0, -3.0, 1.0), (1.875, -1.25, 0.375)]
+    want, _, err = plain_muon(p, u, None, 1.0, 0.0, True, 0.0, 3, coefs, 1e-7, 1.0, 1.0, 2.0 ** -20)
+    D.densenet_muon(D.MuonPlan([p], [u], rates=[1.0]), lr=1.0, momentum=0.0, steps=3, coefficients=coefs)
+    within(p, want, err + 4 * E24 * want.abs(), "p")
+    # an update of zeros moves nothing but the decay; one with a NaN spoils its own matrix alone
+    p = [torch.ones(40, 50, device="cuda"), torch.ones(50, 40, device="cuda"), torch.ones(30, 30, device="cuda")]
+    gr = [torch.zeros(40, 50, device="cuda"), torch.zeros(50, 40, device="cuda"), torch.zeros(30, 30, device="cuda")]
+    gr[2][3, 4] = float("nan")
+    D.densenet_muon(D.MuonPlan(p, gr), lr=0.1, weight_decay=0.5, momentum=0.9)
+    assert bool((p[0] == torch.tensor(0.95)).all()) and bool((p[1] == torch.tensor(0.95)).all()) and bool(p[2].isnan().all())
+
+
+def test_muon_many_matrices_step_as_each_alone(D):
+    g = gen(8)
+    shapes = [(10 + 7 * i % 90, 5 + 13 * i % 150) for i in range(70)]  # more than one launch holds
+    p = [torch.randn(s, generator=g, device="cuda") for s in shapes]
+    gr = [torch.randn(s, generator=g, device="cuda") for s in shapes]
+    alone = [t.clone() for t in p]
+    D.densenet_muon(D.MuonPlan(p, gr), lr=0.1)
+    for i, (a, s) in enumerate(zip(alone, shapes)):
+        start = a.clone()
+        D.densenet_muon(D.MuonPlan([a], [gr[i]]), lr=0.1)
+        # the sums may be split in another way: 22 bits of an update of size 0.2 sqrt(max)
+        within(a, p[i], 0.1 * 0.2 * max(s) ** 0.5 * 41 * 5 * 2.0 ** -20 + 4 * E24 * start.double().abs(), f"matrix {i}")
