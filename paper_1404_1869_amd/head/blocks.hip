@@ -150,10 +150,16 @@ struct P8Args {
   int64_t ldw, lda;
   const float *w_scale, *a_scale;
   int32_t M, N, K, blocks;  // blocks: of K, the scales' row length
-  int32_t tiles_m, tiles_n, splits;
-  void* out;  // [N][ldo]; a split's sums in fp32 at out + split * out_split
-  int64_t ldo, out_split;
+  int32_t tiles_m, tiles_n, first, tiles, splits;  // the launch's tiles: first .. first + tiles - 1, each in `splits` jobs
+  void* out;  // [N][ldo]; SLAB: sums in fp32, [splits][tiles][BN][BM]
+  int64_t ldo;
 };
+// Tile `id` of tiles_m x tiles_n, ordered as columns of 6 along n, which share their operands in an XCD's L2.
+__device__ inline void place_of(int id, int tiles_m, int tiles_n, int& tile_m, int& tile_n) {
+  constexpr int COL = 6;
+  const int col = id / (COL * tiles_m), width = min(COL, tiles_n - col * COL), in = id - col * COL * tiles_m;
+  tile_m = in / width, tile_n = col * COL + in % width;
+}
 
 // A tile of R rows x 128 codes in LDS, loaded straight from memory in 16-byte slots; slot s of row r at place s ^ (r / 2) % 8
 // (16 consecutive rows' reads of one slot meet 16 different places modulo 256 bytes).
@@ -161,57 +167,59 @@ template <int R, int NW>
 struct Codes {
   static constexpr int BYTES = R * B, PIECES = BYTES / 1024, PER = PIECES / NW;
   static_assert(PIECES % NW == 0 && NW % 2 == 0, "whole pieces per wave");
-  uint32_t voff[PER];
   const uint8_t* base;
-  int place;  // first k of this lane's slot: the same in each piece, since those are 8 rows each and NW is even
-  __device__ inline void init(const uint8_t* p, int64_t ld, int row0, int rows, int wave, int lane) {
+  uint32_t first, step;  // byte offset of this lane's slot in the first piece, and from piece to piece (8 NW rows)
+  int rows;              // pieces whose row is there
+  int place;             // first k of this lane's slot: the same in each piece, since those are 8 rows each and NW is even
+  __device__ inline void init(const uint8_t* p, int64_t ld, int row0, int all_rows, int wave, int lane) {
     base = p + (int64_t)row0 * ld;
-    const int line = lane >> 3;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int row = (wave + i * NW) * 8 + line, s = (lane & 7) ^ ((row >> 1) & 7);
-      voff[i] = row0 + row < rows ? (uint32_t)(row * ld + s * 16) : OOB;
-      place = s * 16;
-    }
+    const int row = wave * 8 + (lane >> 3);
+    place = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+    first = (uint32_t)(row * ld) + place, step = (uint32_t)(8 * NW * ld);
+    rows = (all_rows - row0 - row + 8 * NW - 1) / (8 * NW);  // (0 or less: none)
   }
-  __device__ inline void load(char* lds, int k0, int K, int wave, int lane) const {
+  // Pieces FIRST, FIRST + STEP, ... of the wave.  whole: all rows of the tile are there.  (The usual case leaves all addresses to the
+  // scalar unit: the vector unit has the products' scaling to do.)
+  template <int FIRST = 0, int STEP = 1>
+  __device__ inline void load(char* lds, int k0, int K, int wave, int lane, bool whole) const {
     const __amdgpu_buffer_rsrc_t rsrc = uniform_rsrc(base, 0x7fffffffu);
-    if (k0 + B <= K) {
+    if (whole && k0 + B <= K) {
 #pragma unroll
-      for (int i = 0; i < PER; ++i) direct16(rsrc, lds + (wave + i * NW) * 1024, voff[i], (uint32_t)k0);
+      for (int i = FIRST; i < PER; i += STEP) direct16(rsrc, lds + (wave + i * NW) * 1024, first, (uint32_t)k0 + i * step);
       return;
     }
+    uint32_t first = this->first;
+    asm volatile("" : "+v"(first));  // (the pieces' offsets are made here each time: held over the loop they would spill)
     const int k = k0 + place;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) direct16(rsrc, lds + (wave + i * NW) * 1024, k + 16 <= K ? voff[i] : OOB, (uint32_t)k0);
+    for (int i = FIRST; i < PER; i += STEP)
+      direct16(rsrc, lds + (wave + i * NW) * 1024, i < rows && k + 16 <= K ? first + i * step : OOB, (uint32_t)k0);
     if (K & 15) {  // the slot that the row ends in, a code at a time: what lies behind it may be anything
       wait_loads<0>();
 #pragma unroll 1
-      for (int i = 0; i < PER; ++i) {
-        if (k >= K || k + 16 <= K || voff[i] == OOB) continue;
+      for (int i = FIRST; i < PER; i += STEP) {
+        if (k >= K || k + 16 <= K || i >= rows) continue;
+        const uint8_t* p = base + (int64_t)(first + i * step) + k0;
         u32x4 v{};
 #pragma unroll
         for (int e = 0; e < 15; ++e)
-          if (k + e < K) v[e / 4] |= (uint32_t)base[(int64_t)voff[i] + k0 + e] << (8 * (e % 4));
+          if (k + e < K) v[e / 4] |= (uint32_t)p[e] << (8 * (e % 4));
         *(u32x4*)(lds + (wave + i * NW) * 1024 + lane * 16) = v;
       }
     }
   }
 };
 
-// The fragments of 32 rows from row r0 on: a lane's 64 codes of row lane % 32, for two MFMAs of 64 k.
-struct Frag {
-  i32x8 k[2];
-};
-__device__ inline void read_frag(const char* lds, int r0, int lane, Frag& f) {
-  const int row = r0 + (lane & 31), half = lane >> 5;
-  const char* p = lds + row * B;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const i32x4 lo = *(const i32x4*)(p + (((4 * h + 2 * half) ^ ((row >> 1) & 7)) * 16));
-    const i32x4 hi = *(const i32x4*)(p + (((4 * h + 2 * half + 1) ^ ((row >> 1) & 7)) * 16));
-    f.k[h] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-  }
+// The fragment of 16 rows from the row at `at` on: a lane's 32 codes of row lane % 16, for one MFMA of 128 k.  They are slots q and
+// q + 4 for q = lane / 16, in both operands (the order of k is theirs to choose): with neighbouring slots 2 q and 2 q + 1 the 16
+// lanes that LDS serves at a time, 8 of one q and 8 of the next, met each other's banks (half of all LDS cycles).
+__device__ inline uint32_t frag_at(int lane) {
+  const int row = lane & 15, q = lane >> 4;
+  return (uint32_t)(row * B + ((q ^ (row >> 1)) * 16));
+}
+__device__ inline i32x8 read_frag(const char* lds, uint32_t at) {  // at: frag_at, and 128 for each row before
+  const i32x4 lo = *(const i32x4*)(lds + at), hi = *(const i32x4*)(lds + (at ^ 64));
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 // Codes 8 j .. + 7 of a lane's 32 as fp16.
 __device__ inline f16x8 halves(const i32x8& k, int j) {
@@ -222,19 +230,16 @@ __device__ inline f16x8 halves(const i32x8& k, int j) {
   return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 // Sums of a block's 128 products.  The 8-bit MFMAs add the products of eight k with those bits only that lie within 2^-13 of the
-// largest one's leading bit, the rest cut off (found by products of powers of two; other lengths are added in full): for results
-// in 16 bits.  EXACT: codes become fp16, which they fit, for MFMAs that keep 24 bits, at half the rate: for results in fp32.
+// largest one's leading bit, the rest cut off (found by products of powers of two; beyond eight, sums are added in full): for
+// results in 16 bits.  EXACT: codes become fp16, which they fit, for MFMAs that keep 24 bits, at half the rate: for results in fp32.
 template <bool EXACT>
-__device__ inline f32x16 block_sum(const Frag& a, const Frag& b) {
-  f32x16 v{};
+__device__ inline f32x4 block_sum(const i32x8& a, const i32x8& b) {
+  f32x4 v{};
+  if constexpr (EXACT) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if constexpr (EXACT) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v = Mfma<_Float16>::mma(halves(a.k[h], j), halves(b.k[h], j), v);
-    } else {
-      v = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a.k[h], b.k[h], v, 0, 0, 0, 0, 0, 0);
-    }
+    for (int j = 0; j < 4; ++j) v = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves(a, j), halves(b, j), v, 0, 0, 0);
+  } else {
+    v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, v, 0, 0, 0, 0, 0, 0);
   }
   return v;
 }
@@ -242,120 +247,240 @@ __device__ inline f32x16 block_sum(const Frag& a, const Frag& b) {
 // Waves: WM x WN, each (BM / WM) x (BN / WN).  NST: stages of 128 k held in LDS.  SLAB: sums in fp32, a slab a split.
 template <int BM, int BN, int WM, int WN, int NST, typename O, bool SLAB, bool EXACT>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(P8Args g) {
-  constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
+  constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
   using OW = Codes<BM, NW>;
   using OA = Codes<BN, NW>;
-  constexpr int STAGE = OW::BYTES + OA::BYTES, PER = OW::PER + OA::PER;
+  constexpr int STAGE = OW::BYTES + OA::BYTES;
   constexpr int WROWS = BN / WN, WCOLS = BM / WM;
   using S = std::conditional_t<SLAB, float, O>;
-  constexpr int OUT_ROW = WCOLS * (int)sizeof(S) + 16, OUT_BYTES = NW * 32 * OUT_ROW;
-  constexpr int LDS = NST * STAGE > OUT_BYTES ? NST * STAGE : OUT_BYTES;
+  constexpr int OUT_ROW = WCOLS * (int)sizeof(S) + 16, OUT_BYTES = NW * 16 * OUT_ROW;
+  constexpr int STAGES = NST * STAGE + 3 * BN * 16, LDS = STAGES > OUT_BYTES ? STAGES : OUT_BYTES;
   __shared__ __align__(1024) char s_mem[LDS];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave % WM, wn = wave / WM, l32 = lane & 31, half = lane >> 5;
-  // each XCD takes a contiguous range of (split, tile), tiles ordered as columns of COL along n, which share their operands in
-  // its L2
-  constexpr int COL = 6;
+  const int wm = wave % WM, wn = wave / WM, l16 = lane & 15, q4 = lane >> 4;
+  // each XCD takes a contiguous range of (split, tile)
   const int all = gridDim.x, xcd = blockIdx.x % 8, per = all / 8, rem = all % 8;
-  const int job = xcd * per + min(xcd, rem) + blockIdx.x / 8, nt = g.tiles_m * g.tiles_n, split = job / nt, id = job - split * nt;
-  const int col = id / (COL * g.tiles_m), width = min(COL, g.tiles_n - col * COL), in = id - col * COL * g.tiles_m;
-  const int tile_m = in / width, tile_n = col * COL + in % width;
+  const int job = xcd * per + min(xcd, rem) + blockIdx.x / 8, split = job / g.tiles;
+  int tile_m, tile_n;
+  place_of(g.first + job - split * g.tiles, g.tiles_m, g.tiles_n, tile_m, tile_n);
   const int m0 = tile_m * BM, n0 = tile_n * BN;
 
   OW ow;
   OA oa;
   ow.init(g.w, g.ldw, m0, g.M, wave, lane);
   oa.init(g.a, g.lda, n0, g.N, wave, lane);
+  const bool whole_w = m0 + BM <= g.M, whole_a = n0 + BN <= g.N;
   const int s0 = (int)((int64_t)g.blocks * split / g.splits), s1 = (int)((int64_t)g.blocks * (split + 1) / g.splits);
-  auto load = [&](int s, int buf) {
-    char* at = s_mem + buf * STAGE;
-    ow.load(at, s * B, g.K, wave, lane);
-    oa.load(at + OW::BYTES, s * B, g.K, wave, lane);
-  };
-  // The scales: of the wave's rows of w one (its rows lie in one block of 128), of a one for each of a lane's rows.
+  // The scales: of the wave's rows of w one (its rows lie in one block of 128), of a one for each row.  Those of four blocks lie in
+  // LDS beside the codes, in three places by turns; with the loads of each stage a quarter of the rows' next four come along, a load
+  // for each wave.  (A load of one block's scales of 64 rows touches 64 lines; eight of them a stage cost as much as half of the
+  // codes.)
   static_assert(WCOLS <= B && B % WCOLS == 0, "a wave's rows of w share their scales");
   const float* ws = g.w_scale + (int64_t)(std::min(m0 + wm * WCOLS, g.M - 1) / B) * g.blocks;
-  const float* as[TN];
+  constexpr int CHUNK = 4, PART = BN / CHUNK / NW;  // rows of a wave's load
+  auto scales = [&](uint32_t chunk) { return s_mem + NST * STAGE + chunk % 3 * (BN * CHUNK * 4); };
+  auto load_quarter = [&](int chunk, int quarter) {  // (past the last block or row: the last one's)
+    const int first = (quarter * NW + wave) * PART, block = s0 + chunk * CHUNK + lane % CHUNK;
+    if (lane < PART * CHUNK)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          uniform_rsrc(g.a_scale + (int64_t)n0 * g.blocks, 0x7fffffffu),
+          (__attribute__((address_space(3))) void*)(scales(chunk) + first * CHUNK * 4), 4,
+          4u * (uint32_t)(min(first + lane / CHUNK, g.N - 1 - n0) * g.blocks + min(block, g.blocks - 1)), 0, 0, 0);
+  };
+  auto load_scales = [&](int s) { load_quarter((uint32_t)(s - s0) / CHUNK + 1, (uint32_t)(s - s0) % CHUNK); };
+  auto read_scales = [&](int s, float (&f)[TN]) {
+    const char* at = scales((uint32_t)(s - s0) / CHUNK) + (uint32_t)(s - s0) % CHUNK * 4;
 #pragma unroll
-  for (int t = 0; t < TN; ++t) as[t] = g.a_scale + (int64_t)std::min(n0 + wn * WROWS + 32 * t + l32, g.N - 1) * g.blocks;
-  float f[TN], next[TN];
-  auto factors = [&](int s, float (&to)[TN]) {
-    const float w = ws[s];
-#pragma unroll
-    for (int t = 0; t < TN; ++t) to[t] = as[t][s] * w;
+    for (int t = 0; t < TN; ++t) f[t] = *(const float*)(at + (wn * WROWS + 16 * t + l16) * (CHUNK * 4));
+  };
+  // w's scale of 64 blocks at a time, a lane each.  (The empty statement has the compiler wait for the load here, once in 64 blocks,
+  // and not before each use, where it would wait for the codes that are on their way.)
+  float w64;
+  auto w_scale = [&](int s) {
+    const int i = (s - s0) & 63;
+    if (i == 0) {
+      w64 = ws[std::min(s + lane, g.blocks - 1)];
+      asm volatile("" : "+v"(w64));
+    }
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w64), i));
+  };
+  auto load = [&](int s, int buf) {
+    char* at = s_mem + buf * STAGE;
+    load_scales(s);
+    ow.load(at, s * B, g.K, wave, lane, whole_w);
+    oa.load(at + OW::BYTES, s * B, g.K, wave, lane, whole_a);
   };
 
-  f32x16 acc[TM][TN];
+  const uint32_t a_at = frag_at(lane) + wm * WCOLS * B, b_at = frag_at(lane) + wn * WROWS * B;  // (128-byte rows: ^ 64 stays in them)
+  f32x4 acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int t = 0; t < TN; ++t) acc[i][t] = f32x16{};
+    for (int t = 0; t < TN; ++t) acc[i][t] = f32x4{};
+  auto add = [&](int i, int t, const f32x4& v, const float (&f)[TN]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc[i][t][r] = __builtin_fmaf(v[r], f[t], acc[i][t][r]);
+  };
 
-  if (s1 > s0) {
+  if constexpr (NW == 8) {
+    // Two waves per SIMD, in turns: while waves 0..3 run the MFMAs of half of their rows of w, waves 4..7 read fragments and send
+    // off loads, and the other way round, a barrier between the turns (waves 4..7 are one turn late).  What of a buffer all waves
+    // have read takes the loads of the stage after the next at once: those of a and of half of w's rows in the second turn of
+    // reading (LATER), those of the other half in the first turn of the next stage (SOON), so that loads have a stage and a half to
+    // come.
+    constexpr int HALF = TM / 2, LATER = OA::PER + OW::PER / 2 + 1, SOON = OW::PER / 2;
+    static_assert(WM == 2 && OW::PER == 4, "a wave's pieces 0 and 2 hold the first halves of the waves' rows of w");
+    const bool late = wave >= 4;
+    float f[TN];
+    i32x8 a[HALF], b[TN];
+    auto turn = [&]() {
+      __builtin_amdgcn_sched_barrier(0);
+      wave_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr int DEPTH = 2;  // sums on their way: the last ones of a turn are added in the next, beside the other waves' MFMAs
+    f32x4 v[DEPTH];
+    auto finish = [&](int h, int k) {  // sum k - DEPTH of half h
+      const int i = h * HALF + (k - DEPTH) / TN, t = (k - DEPTH) % TN;
+      add(i, t, v[k % DEPTH], f);
+      asm volatile("" : "+v"(acc[i][t]));  // (here, and not where the result is read: the sums would fill the registers)
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto wait = [&](bool more) {  // all loads but the last two groups
+      if (more) wait_loads<LATER + SOON>();
+      else wait_loads<0>();
+    };
+    auto compute = [&](int h, bool wait_here, bool more) {
+      __builtin_amdgcn_s_setprio(0);  // (the reading waves first: their loads are few, and on their way sooner)
+#pragma unroll
+      for (int k = 0; k < HALF * TN; ++k) {
+        if (k >= DEPTH) finish(h, k);
+        v[k % DEPTH] = block_sum<EXACT>(a[k / TN], b[k % TN]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (wait_here) wait(more);
+      turn();
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int k = HALF * TN; k < HALF * TN + DEPTH; ++k) finish(h, k);
+    };
+    auto read_a = [&](uint32_t at, int h) {
+#pragma unroll
+      for (int i = 0; i < HALF; ++i) a[i] = read_frag(s_mem + 16 * B * (h * HALF + i), at);
+    };
+    auto load_later = [&](int s, int buf) {
+      load_scales(s);
+      oa.load(s_mem + buf * STAGE + OW::BYTES, s * B, g.K, wave, lane, whole_a);
+      ow.template load<0, 2>(s_mem + buf * STAGE, s * B, g.K, wave, lane, whole_w);
+    };
+    auto load_soon = [&](int s, int buf) { ow.template load<1, 2>(s_mem + buf * STAGE, s * B, g.K, wave, lane, whole_w); };
+    auto stage = [&](int s, auto of) {
+      constexpr int buf = decltype(of)::value;
+      // (places in this buffer, in registers of their own: as constants beyond 64 KB each read would have an addition of its own)
+      uint32_t a_here = a_at + buf * STAGE, b_here = b_at + buf * STAGE + OW::BYTES;
+      asm volatile("" : "+v"(a_here), "+v"(b_here));
+#pragma unroll
+      for (int t = 0; t < TN; ++t) b[t] = read_frag(s_mem + 16 * B * t, b_here);
+      read_a(a_here, 0);
+      read_scales(s, f);
+      const float w = w_scale(s);
+      if (s + 1 < s1) load_soon(s + 1, buf ^ 1);
+      if (late) wait(s + 1 < s1);
+      wait_lds();
+#pragma unroll
+      for (int t = 0; t < TN; ++t) f[t] *= w;
+      turn();
+      compute(0, !late, s + 1 < s1);
+      read_a(a_here, 1);
+      if (s + 2 < s1) load_later(s + 2, buf);
+      if (late) wait(s + 2 < s1);
+      wait_lds();
+      turn();
+      compute(1, !late, s + 2 < s1);
+    };
+    if (s1 > s0) {
+#pragma unroll
+      for (int q = 0; q < CHUNK; ++q) load_quarter(0, q);
+      load_later(s0, 0);
+      load_soon(s0, 0);
+      if (s0 + 1 < s1) load_later(s0 + 1, 1);
+      wait(s0 + 1 < s1);
+    }
+    turn();
+    if (late) turn();
+    for (int s = s0; s < s1; s += 2) {
+      stage(s, std::integral_constant<int, 0>{});
+      if (s + 1 < s1) stage(s + 1, std::integral_constant<int, 1>{});
+    }
+    if (!late) turn();
+  } else if (s1 > s0) {
+    // Stage s computes from buffer (s - s0) % NST while the next NST - 1 stages' loads are on their way.
+    constexpr int PER = OW::PER + OA::PER + 1;
+    static_assert(PER * (NST - 1) < 64, "loads that can be counted");
+#pragma unroll
+    for (int q = 0; q < CHUNK; ++q) load_quarter(0, q);
 #pragma unroll
     for (int i = 0; i < NST; ++i)
       if (s0 + i < s1) load(s0 + i, i);
-    factors(s0, f);
     int buf = 0;
     for (int s = s0; s < s1; ++s) {
-      wait_loads<0>();
+      if (s + NST <= s1) wait_loads<PER * (NST - 1)>();
+      else wait_loads<0>();
       wave_barrier();
-      if (s + 1 < s1) factors(s + 1, next);
       const char* at = s_mem + buf * STAGE;
-      Frag b[TN];
+      float f[TN];
+      i32x8 b[TN];
+      const float w = w_scale(s);
+      read_scales(s, f);
 #pragma unroll
-      for (int t = 0; t < TN; ++t) read_frag(at + OW::BYTES, wn * WROWS + 32 * t, lane, b[t]);
+      for (int t = 0; t < TN; ++t) {
+        b[t] = read_frag(at + OW::BYTES + 16 * B * t, b_at);
+        f[t] *= w;
+      }
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
-        Frag a;
-        read_frag(at, wm * WCOLS + 32 * i, lane, a);
+        const i32x8 a = read_frag(at + 16 * B * i, a_at);
 #pragma unroll
-        for (int t = 0; t < TN; ++t) {
-          const f32x16 v = block_sum<EXACT>(a, b[t]);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[i][t][r] = __builtin_fmaf(v[r], f[t], acc[i][t][r]);
-        }
+        for (int t = 0; t < TN; ++t) add(i, t, block_sum<EXACT>(a, b[t]), f);
       }
       wait_lds();
       wave_barrier();
       if (s + NST < s1) load(s + NST, buf);
-#pragma unroll
-      for (int t = 0; t < TN; ++t) f[t] = next[t];
       buf = buf + 1 == NST ? 0 : buf + 1;
     }
   }
-  (void)PER;
 
-  // Element r of acc[i][t]: m = m0 + wm WCOLS + 32 i + 8 (r / 4) + 4 half + r % 4, n = n0 + wn WROWS + 32 t + l32.  Results leave
-  // through LDS, whole pieces of rows at a time.
+  // Element r of acc[i][t]: m = m0 + wm WCOLS + 16 i + 4 q4 + r, n = n0 + wn WROWS + 16 t + l16.  Results leave through LDS, whole
+  // pieces of rows at a time.
   constexpr int EV = 16 / (int)sizeof(S), LANES = WCOLS / EV, LINES = 64 / LANES;
   typedef S v4 __attribute__((ext_vector_type(4)));
   typedef S vec __attribute__((ext_vector_type(EV)));
   typedef S vec_any __attribute__((ext_vector_type(EV), aligned(sizeof(S))));
+  static_assert(16 % LINES == 0, "whole pieces");
   __syncthreads();
-  char* stg = s_mem + wave * 32 * OUT_ROW;
-  S* out = (S*)g.out + (SLAB ? split * g.out_split : 0);
+  char* stg = s_mem + wave * 16 * OUT_ROW;
+  // a slab is the tile's own, whole and aligned
+  const int64_t ldo = SLAB ? BM : g.ldo;
+  S* out = SLAB ? (S*)g.out + (int64_t)job * (BM * BN) - (int64_t)n0 * BM - m0 : (S*)g.out;
 #pragma unroll
   for (int t = 0; t < TN; ++t) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < TM; ++i) {
+      v4 v;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        v4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (S)acc[i][t][4 * q + e];
-        *(v4*)(stg + l32 * OUT_ROW + (32 * i + 8 * q + 4 * half) * (int)sizeof(S)) = v;
-      }
+      for (int e = 0; e < 4; ++e) v[e] = (S)acc[i][t][e];
+      *(v4*)(stg + l16 * OUT_ROW + (16 * i + 4 * q4) * (int)sizeof(S)) = v;
+    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     const int c = (lane % LANES) * EV, m = m0 + wm * WCOLS + c;
 #pragma unroll
-    for (int k = 0; k < 32 / LINES; ++k) {
-      const int line = k * LINES + lane / LANES, n = n0 + wn * WROWS + 32 * t + line;
+    for (int k = 0; k < 16 / LINES; ++k) {
+      const int line = k * LINES + lane / LANES, n = n0 + wn * WROWS + 16 * t + line;
       const vec v = *(const vec*)(stg + line * OUT_ROW + c * (int)sizeof(S));
       if (n >= g.N) continue;
-      S* dst = out + (int64_t)n * g.ldo + m;
-      if (SLAB || m + EV <= g.M) {  // (a slab's rows are padded to whole tiles)
+      S* dst = out + n * ldo + m;
+      if (SLAB || m + EV <= g.M) {
         *(vec_any*)dst = v;
       } else {
 #pragma unroll
@@ -367,24 +492,26 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(P8Args g) {
   }
 }
 
-// y = sum of the splits' slabs, rounded.
+// y = sum of a tile's slabs, rounded: `per` workgroups a tile, a tile BN x BM.
 template <typename O>
-__global__ __launch_bounds__(256) void join_splits_kernel(const float* __restrict__ slab, int64_t ld, int64_t stride, int splits,
-                                                          int64_t rows, int C, O* __restrict__ out, int64_t ldo) {
-  const int per = (C + 7) / 8;
-  const int64_t total = rows * per;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / per;
-    const int c = (int)(i - row * per) * 8;
+__global__ __launch_bounds__(256) void join_splits_kernel(P8Args g, const float* __restrict__ slab, int BM, int BN, int per, O* __restrict__ out) {
+  const int tile = blockIdx.x / per, vectors = BN * BM / 8;
+  int tile_m, tile_n;
+  place_of(g.first + tile, g.tiles_m, g.tiles_n, tile_m, tile_n);
+  const float* p = slab + (int64_t)tile * (BM * BN);
+  const int64_t stride = (int64_t)g.tiles * (BM * BN);
+  for (int i = (blockIdx.x - tile * per) * 256 + threadIdx.x; i < vectors; i += per * 256) {
+    const int n = i * 8 / BM, c = i * 8 - n * BM, row = tile_n * BN + n, m = tile_m * BM + c;
+    if (row >= g.N || m >= g.M) continue;
     float v[8] = {};
 #pragma unroll 4
-    for (int s = 0; s < splits; ++s) {
+    for (int s = 0; s < g.splits; ++s) {
       float w[8];
-      load8(slab + s * stride + row * ld + c, w);
+      load8(p + s * stride + i * 8, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += w[j];
     }
-    store8(out + row * ldo, c, C, v);
+    store8(out + row * g.ldo, m, g.M, v);
   }
 }
 
@@ -427,43 +554,69 @@ struct Work {  // offsets in the workspace, 256-byte aligned
 enum Tile { T256, T128, T64, T32 };
 int tile_m(Tile t) { return t == T256 ? 256 : 128; }
 int tile_n(Tile t) { return t == T256 ? 256 : t == T128 ? 128 : t == T64 ? 64 : 32; }
+int64_t tiles_of(Tile t, int64_t n, int64_t V) { return (up(V, tile_m(t)) / tile_m(t)) * (up(n, tile_n(t)) / tile_n(t)); }
+int round_of(Tile t) { return t == T256 ? 256 : 512; }  // workgroups that run together
 
+// What is computed how: the first `full` tiles a workgroup each, the rest in `splits` workgroups along k, whose sums a launch joins.
 struct Plan8 {
   Tile tile;
+  int64_t full, rest;
   int splits;
   bool copy_a, copy_w;
-  int64_t ld, slab_ld;  // ld: of the copies
+  int64_t ld;  // of the copies
   size_t a_at, w_at, slab_at, total;
 };
+
+// The time of `jobs` workgroups of `stages` blocks in us, by what launches of many shapes took.
+double jobs_us(Tile t, double jobs, double stages, bool exact) {
+  if (jobs == 0) return 0;
+  const double fill = std::min(1.0, jobs / round_of(t)), rounds = std::ceil(jobs / round_of(t));
+  const double stage = t == T256 ? 1.2 + 0.55 * fill : t == T128 ? (exact ? 1.1 + 1.1 * fill : 0.7 + 0.5 * fill) : t == T64 ? 0.55 + 0.25 * fill : 0.5 + 0.15 * fill;
+  return rounds * (stages * stage + (t == T256 ? 5 : 3));
+}
+double plan_us(Tile t, int64_t full, int64_t rest, int splits, int64_t blocks, bool exact) {
+  double us = jobs_us(t, full, blocks, exact);
+  if (rest) us += 3 + jobs_us(t, (double)rest * splits, (double)((blocks + splits - 1) / splits), exact);
+  if (rest && splits > 1) us += 3 + (double)rest * splits * tile_m(t) * tile_n(t) * 8 / 6e6;
+  return us;
+}
 bool lies_well(const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 16 == 0 && ld <= MAX_LD; }
-Plan8 plan_product(const ProductArgs& a) {
+Plan8 plan_product(const ProductArgs& a, bool exact) {
   Plan8 p{};
   Work w;
-  p.tile = a.n <= 32 ? T32 : a.n <= 64 ? T64 : T128;
-  const int64_t tiles = (up(a.V, tile_m(p.tile)) / tile_m(p.tile)) * (up(a.n, tile_n(p.tile)) / tile_n(p.tile));
   const int64_t blocks = (a.C + B - 1) / B;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / tiles, blocks / 4, 64}));
+  double best = 1e300;
+  for (const Tile t : {T256, T128, T64, T32}) {
+    if ((t == T256 && exact) || (t == T32 && a.n > 32) || (t == T64 && (a.n <= 32 || a.n > 64)) || (t < T64 && a.n <= 64)) continue;
+    const int64_t tiles = tiles_of(t, a.n, a.V), whole = tiles / round_of(t) * round_of(t);
+    for (const int64_t full : {tiles, whole, (int64_t)0})
+      for (int s = full == tiles ? 1 : 2; s <= (full == tiles ? 1 : 16) && (s == 1 || blocks / s >= 2); ++s) {
+        // (a launch's threads, and slabs of up to 1 GiB)
+        if ((tiles - full) * s * tile_m(t) * tile_n(t) > (1 << 28) || std::max(full, (tiles - full) * s) > MAX_LAUNCH_THREADS / 512) continue;
+        const double us = plan_us(t, full, tiles - full, s, blocks, exact);
+        if (us < best * 0.999) best = us, p.tile = t, p.full = full, p.rest = tiles - full, p.splits = s;
+      }
+  }
   p.copy_a = !lies_well(a.a, a.a_stride), p.copy_w = !lies_well(a.w, a.w_stride);
   p.ld = up(a.C, 16);
   if (p.copy_a) p.a_at = w.take((size_t)a.n * p.ld);
   if (p.copy_w) p.w_at = w.take((size_t)a.V * p.ld);
-  p.slab_ld = up(a.V, 256);
-  if (p.splits > 1) p.slab_at = w.take((size_t)p.splits * a.n * p.slab_ld * 4);
+  if (p.rest) p.slab_at = w.take((size_t)p.rest * p.splits * tile_m(p.tile) * tile_n(p.tile) * 4);
   p.total = w.total;
   return p;
 }
 
 template <int BM, int BN, int WM, int WN, int NST, typename O, bool SLAB, bool EXACT>
 int run_product(P8Args& g, hipStream_t st) {
-  g.tiles_m = (g.M + BM - 1) / BM, g.tiles_n = (g.N + BN - 1) / BN;
-  product_kernel<BM, BN, WM, WN, NST, O, SLAB, EXACT>
-      <<<dim3((unsigned)(g.tiles_m * g.tiles_n * g.splits)), 64 * WM * WN, 0, st>>>(g);
+  product_kernel<BM, BN, WM, WN, NST, O, SLAB, EXACT><<<dim3((unsigned)(g.tiles * g.splits)), 64 * WM * WN, 0, st>>>(g);
   return (int)hipGetLastError();
 }
 template <typename O, bool SLAB, bool EXACT>
 int run_tile(Tile t, P8Args& g, hipStream_t st) {
-  if (t == T32) return run_product<128, 32, 4, 1, 4, O, SLAB, EXACT>(g, st);
+  if (t == T32) return run_product<128, 32, 4, 1, 3, O, SLAB, EXACT>(g, st);
   if (t == T64) return run_product<128, 64, 2, 2, 3, O, SLAB, EXACT>(g, st);
+  if constexpr (!EXACT)  // (the conversions' registers do not fit)
+    if (t == T256) return run_product<256, 256, 2, 4, 2, O, SLAB, EXACT>(g, st);
   return run_product<128, 128, 2, 2, 2, O, SLAB, EXACT>(g, st);
 }
 
@@ -491,15 +644,17 @@ int launch_quantize_blocks(const QuantArgs& a, dn_dtype dt, void* stream) {
   });
 }
 
-size_t block_product_bytes(const ProductArgs& a) { return plan_product(a).total; }
+size_t block_product_bytes(const ProductArgs& a, dn_dtype dt) { return plan_product(a, dt == DN_F32).total; }
 
 int launch_block_product(const ProductArgs& a, dn_dtype dt, void* d_work, void* stream) {
-  const Plan8 p = plan_product(a);
+  const Plan8 p = plan_product(a, dt == DN_F32);
   const hipStream_t st = (hipStream_t)stream;
   char* work = (char*)d_work;
+  const int bm = tile_m(p.tile), bn = tile_n(p.tile);
   P8Args g{};
   g.a = a.a, g.lda = a.a_stride, g.w = a.w, g.ldw = a.w_stride, g.a_scale = a.a_scale, g.w_scale = a.w_scale;
-  g.M = a.V, g.N = (int)a.n, g.K = a.C, g.blocks = (a.C + B - 1) / B, g.splits = p.splits;
+  g.M = a.V, g.N = (int)a.n, g.K = a.C, g.blocks = (a.C + B - 1) / B;
+  g.tiles_m = (g.M + bm - 1) / bm, g.tiles_n = (g.N + bn - 1) / bn;
   int err;
   if (p.copy_a) {
     if ((err = align(a.a, a.a_stride, a.n, a.C, (uint8_t*)work + p.a_at, p.ld, st))) return err;
@@ -509,19 +664,20 @@ int launch_block_product(const ProductArgs& a, dn_dtype dt, void* d_work, void* 
     if ((err = align(a.w, a.w_stride, a.V, a.C, (uint8_t*)work + p.w_at, p.ld, st))) return err;
     g.w = (uint8_t*)work + p.w_at, g.ldw = p.ld;
   }
-  if (p.splits == 1) {
-    g.out = a.y, g.ldo = a.y_stride;
-    return with_type(dt, [&](auto v) {
-      using O = decltype(v);
-      return run_tile<O, false, std::is_same<O, float>::value>(p.tile, g, st);
-    });
-  }
-  g.out = work + p.slab_at, g.ldo = p.slab_ld, g.out_split = a.n * p.slab_ld;
-  if ((err = dt == DN_F32 ? run_tile<float, true, true>(p.tile, g, st) : run_tile<float, true, false>(p.tile, g, st))) return err;
+  g.ldo = a.y_stride;
   return with_type(dt, [&](auto v) {
-    const unsigned grid = (unsigned)std::min<int64_t>((a.n * ((a.V + 7) / 8) + 255) / 256, 8192);
-    join_splits_kernel<<<grid, 256, 0, st>>>((const float*)g.out, p.slab_ld, g.out_split, p.splits, a.n, a.V, (decltype(v)*)a.y,
-                                             a.y_stride);
+    using O = decltype(v);
+    constexpr bool exact = std::is_same<O, float>::value;
+    if (p.full) {
+      g.out = a.y, g.first = 0, g.tiles = (int)p.full, g.splits = 1;
+      if ((err = run_tile<O, false, exact>(p.tile, g, st))) return err;
+    }
+    if (!p.rest) return 0;
+    g.out = work + p.slab_at, g.first = (int)p.full, g.tiles = (int)p.rest, g.splits = p.splits;
+    if ((err = run_tile<float, true, exact>(p.tile, g, st))) return err;
+    // (enough workgroups for the chip, of at least a vector a thread)
+    const int per = (int)std::max<int64_t>(1, std::min<int64_t>(bm * bn / 8 / 256, 2048 / p.rest));
+    join_splits_kernel<O><<<dim3((unsigned)(p.rest * per)), 256, 0, st>>>(g, (const float*)g.out, bm, bn, per, (O*)a.y);
     return (int)hipGetLastError();
   });
 }

@@ -125,7 +125,7 @@ struct ProductArgs {
   void* y;
   int64_t y_stride;
 };
-size_t block_product_bytes(const ProductArgs& a);
+size_t block_product_bytes(const ProductArgs& a, dn_dtype dt);
 int launch_block_product(const ProductArgs& a, dn_dtype dt, void* d_work, void* stream);
 
 size_t muon_bytes(const dn_muon_tensor* tensors, int32_t count, dn_dtype p_dt, const dn_muon_params& k);

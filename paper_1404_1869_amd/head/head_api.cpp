@@ -294,7 +294,7 @@ int densenet_block_product(const void* d_a, int64_t a_stride, const float* d_a_s
     if ((st = check_rows("a", d_a, a_stride, n, C, 1))) return st;
     if ((st = check_rows("w", d_w, w_stride, V, C, 1))) return st;
     // (never 0, so that a caller's workspace is never the null pointer of a size query)
-    const size_t need = std::max<size_t>(n ? block_product_bytes(a) : 0, 256);
+    const size_t need = std::max<size_t>(n ? block_product_bytes(a, y_dtype) : 0, 256);
     if ((st = check_work(d_workspace, workspace_bytes, need, bytes_needed)) || !d_workspace) return st;
     if (n == 0) return DN_OK;
     if (!d_a_scale || !d_w_scale) return fail(DN_E_INVALID_ARG, "null scale pointer");
