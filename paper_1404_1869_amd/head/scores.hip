@@ -4,10 +4,10 @@
 // Bound by memory: a row is read once (the gradient: read once and written once).  Every lane keeps its own maximum m, sum S of
 // exp(x - m) and T of exp(x - m) (x - m) and rescales them where the maximum grows; lanes, waves and workgroups join theirs at
 // the end, in a fixed order.  H = log S - T / S, and a logit's part is taken as (x - m), so large logits lose no digits.
-// Alternatives: a wave keeps candidates above a bound that `top` values seen so far reach.  The first block sets the bound from
-// its lanes' maxima; after that few blocks have a larger value (about top ln(V / 1024) values in all for logits in no order),
-// and a full buffer is ranked and cut to `top`.  Candidates are 64-bit keys, value and then index, so that no two are equal and
-// their ranks do not depend on who found them first.
+// Alternatives: a wave keeps candidates above a bound that `top` values of the row are known to reach.  The top-th largest of the
+// lanes' maxima so far is such a bound; it is looked for where a block of 1024 has a value above the last one, and the waves of a row
+// tell each other theirs.  Few blocks have (of logits in no order about top ln(V / 1024)); a full buffer is ranked and cut to `top`.
+// Candidates are 64-bit keys, value and then index, so no two are equal, and results do not depend on who found them first.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -55,24 +55,42 @@ __device__ inline Stats lanes_join(Stats a, float c) {
   return a;
 }
 
-// A wave's candidates.  All of it is the wave's own: no barriers.
+// A wave's candidates.  All of it is the wave's own, but for the other waves' bounds of the row: no barriers.
 struct Candidates {
-  Key* buf;     // [CAP] in LDS
-  int count;    // wave-uniform
-  Key bound;    // `top` keys above or at it have been seen (or NOTHING)
+  Key* buf;                 // [CAP] in LDS
+  volatile uint32_t* seen;  // [4] in LDS: values that the row's waves know `top` values of the row to reach (null: a row of its own)
+  int count;                // wave-uniform
+  Key bound;                // `top` keys above or at it have been seen (or NOTHING)
   int top;
 
-  __device__ inline void init(Key* b, int k) { buf = b, count = 0, bound = NOTHING, top = k; }
-  // The bound from one value per lane: the top-th largest of them.
-  __device__ inline void start(float lane_max) {
+  __device__ inline void init(Key* b, volatile uint32_t* s, int k) { buf = b, seen = s, count = 0, bound = NOTHING, top = k; }
+  __device__ inline void raise(Key to) {
+    if (to > bound) bound = to;
+  }
+  // The bound from one value per lane, the lane's largest so far: the top-th largest of these.  BITS: low bits that are 0 in T.
+  template <int BITS>
+  __device__ inline void raise_to(float lane_max) {
     const uint32_t o = ordered(lane_max);
     uint32_t at = 0;
-    for (int bit = 31; bit >= 0; --bit) {
+#pragma unroll 4
+    for (int bit = 31; bit >= BITS; --bit) {
       const uint32_t to = at | 1u << bit;
       if (__popcll(__ballot(o >= to)) >= top) at = to;
     }
-    const Key k = (Key)at << 32;
-    if (k > bound) bound = k - 1;
+    if (at) raise(((Key)at << 32) - 1);
+    tell();
+  }
+  // (the value that `top` keys reach: the bound's own, or of a bound from lanes' maxima the one after it)
+  __device__ inline void tell() {
+    if (seen && (threadIdx.x & 63) == 0) seen[threadIdx.x >> 6] = (uint32_t)((bound + 1) >> 32);
+  }
+  __device__ inline void hear() {
+    if (!seen) return;
+    uint32_t v = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) v = max(v, seen[w]);
+    v = __builtin_amdgcn_readfirstlane(v);
+    if (v) raise(((Key)v << 32) - 1);  // equal values stay: theirs may have lower indices than what others hold
   }
   // Ranks all keys and keeps the first `top`, in order.
   __device__ inline void cut() {
@@ -82,10 +100,18 @@ struct Candidates {
     int rank[CAP / 64];
 #pragma unroll
     for (int i = 0; i < CAP / 64; ++i) mine[i] = lane + 64 * i < count ? buf[lane + 64 * i] : 0, rank[i] = 0;
-    for (int j = 0; j < count; ++j) {
-      const Key k = buf[j];
+    if (lane < 8 && count + lane < CAP) buf[count + lane] = 0;  // eight are read at a time; no key is below 0
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int rows = (count + 63) / 64;
+    for (int j = 0; j < count; j += 8) {
+      Key k[8];
 #pragma unroll
-      for (int i = 0; i < CAP / 64; ++i) rank[i] += k > mine[i];
+      for (int e = 0; e < 8; ++e) k[e] = buf[j + e];
+#pragma unroll
+      for (int i = 0; i < CAP / 64; ++i)
+        if (i < rows)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) rank[i] += k[e] > mine[i];
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
@@ -94,8 +120,8 @@ struct Candidates {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     if (count >= top) {
       count = top;
-      const Key last = buf[top - 1];
-      if (last > bound) bound = last;
+      raise(buf[top - 1]);
+      tell();
     }
   }
   // One key per lane (0: none), in any order of indices.  A key at the bound is one that is held already.
@@ -152,7 +178,6 @@ __device__ inline Stats scan(const T* row, int64_t first, int64_t step, int end,
     for (int h = 0; h < 2; ++h) next[h] = load_logits(row, (int)std::min<int64_t>(b * WAVE_BLOCK + h * 512 + lane * 8, 0x7ffffff0), end);
   };
   const int64_t blocks = ((int64_t)end + WAVE_BLOCK - 1) / WAVE_BLOCK;
-  bool begun = false;
   if (first < blocks) load(first);
   for (int64_t b = first; b < blocks; b += step) {
     float x[EV];
@@ -175,15 +200,14 @@ __device__ inline Stats scan(const T* row, int64_t first, int64_t step, int end,
     }
     z.m = m, z.s = s[0] + s[1], z.t = t[0] + t[1];
     if constexpr (TOP) {
-      if (!begun) cand.start(top), begun = true;
       // (a value equal to the bound's has a higher index than all that are held: blocks come in order)
       if (__any(ordered(top) > (uint32_t)(cand.bound >> 32))) {
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t i = (uint32_t)(b * WAVE_BLOCK + h * 512 + lane * 8);
+        cand.hear();
+        cand.template raise_to<std::is_same<T, float>::value ? 0 : std::is_same<T, __bf16>::value ? 16 : 13>(m);
+        const float least = value_of(cand.bound);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) cand.offer(key_of(h ? x[8 + j] : x[j], i + j));
-        }
+        for (int j = 0; j < EV; ++j)
+          if (__any(!(x[j] < least))) cand.offer(key_of(x[j], (uint32_t)(b * WAVE_BLOCK + (j / 8) * 512 + lane * 8 + j % 8)));
       }
     }
   }
@@ -200,6 +224,7 @@ template <typename T, bool WAVE, bool SPLIT, bool TOP>
 __global__ __launch_bounds__(256) void scores_kernel(ScoresArgs a) {
   __shared__ Key s_keys[TOP ? 4 : 1][TOP ? CAP : 1];
   __shared__ Key s_best[MOST];
+  __shared__ uint32_t s_seen[4];
   __shared__ Stats s_stats[4];
   __shared__ int s_count[4];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -209,7 +234,11 @@ __global__ __launch_bounds__(256) void scores_kernel(ScoresArgs a) {
   const T* x = (const T*)a.x + row * a.x_stride;
   const float c = a.scale * LOG2E;
   Candidates cand;
-  cand.init(s_keys[TOP ? wave : 0], a.top);
+  cand.init(s_keys[TOP ? wave : 0], WAVE ? nullptr : s_seen, a.top);
+  if (TOP && !WAVE) {
+    if (threadIdx.x < 4) s_seen[threadIdx.x] = 0;
+    __syncthreads();
+  }
   Stats z = scan<T, TOP>(x, WAVE ? 0 : part * 4 + wave, WAVE ? 1 : SPLIT ? 4 * a.parts : 4, a.V, c, cand);
   z = lanes_join(z, c);
   if (TOP) cand.cut();
@@ -230,6 +259,7 @@ __global__ __launch_bounds__(256) void scores_kernel(ScoresArgs a) {
       int rank = 0;
 #pragma unroll
       for (int w = 0; w < 4; ++w)
+#pragma unroll 8
         for (int j = 0; j < s_count[w]; ++j) rank += s_keys[w][j] > mine;
       if (rank < a.top) s_best[rank] = mine;
     }
@@ -257,7 +287,7 @@ __global__ __launch_bounds__(64) void join_scores_kernel(ScoresArgs a) {
   const float c = a.scale * LOG2E;
   Stats z{-INFINITY, 0.f, 0.f};
   Candidates cand;
-  cand.init(s_keys, a.top);
+  cand.init(s_keys, nullptr, a.top);
   for (int q = lane; q < a.parts; q += 64) z = join(z, p[q], c);
   z = lanes_join(z, c);
   if (a.top) {
@@ -278,16 +308,15 @@ __global__ __launch_bounds__(64) void join_scores_kernel(ScoresArgs a) {
 }
 
 // Gradient: a workgroup takes SEGMENT elements of a row, or (WAVE: rows of up to SEGMENT / 4) each of its waves a row.  The
-// elements whose own gradients are not 0 (the token and the alternatives) are marked in a bitmap, a bit for eight, so that an
-// element is written once: the result may be the logits' own memory.
+// gradients of the token's and the alternatives' own logits wait in LDS at their elements' places, eights of elements that hold one
+// marked in a bitmap, so that an element is written once (the result may be the logits' own memory) and no other is looked at.
 constexpr int SEGMENT = 8192;
 template <typename T, bool WAVE>
 __global__ __launch_bounds__(256) void scores_back_kernel(ScoresBackArgs a) {
-  constexpr int TPR = WAVE ? 64 : 256, LEN = WAVE ? SEGMENT / 4 : SEGMENT, WORDS = LEN / 8 / 32;
-  __shared__ int s_id[WAVE ? 4 : 1][MOST + 1];
-  __shared__ float s_own[WAVE ? 4 : 1][MOST + 1];
+  constexpr int TPR = WAVE ? 64 : 256, LEN = WAVE ? SEGMENT / 4 : SEGMENT, WORDS = LEN / 8 / 32, STEPS = LEN / 8 / TPR;
+  __shared__ __align__(16) float s_own[WAVE ? 4 : 1][LEN];
   __shared__ uint32_t s_bits[WAVE ? 4 : 1][WORDS];
-  const int wave = threadIdx.x >> 6, t = threadIdx.x % TPR, sub = WAVE ? wave : 0;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, t = threadIdx.x % TPR, sub = WAVE ? wave : 0;
   const int64_t row = WAVE ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x / a.segments;
   if (row >= a.n) return;  // whole waves, only where WAVE (no barriers)
   const int first = WAVE ? 0 : (int)(blockIdx.x - row * a.segments) * LEN, end = (int)std::min<int64_t>((int64_t)first + LEN, a.V);
@@ -295,57 +324,66 @@ __global__ __launch_bounds__(256) void scores_back_kernel(ScoresBackArgs a) {
     if constexpr (WAVE) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     else __syncthreads();
   };
-  const int64_t token = a.token ? a.token[row] : -1;
-  const float dlogp = a.dlogp && token >= 0 && token < a.V ? a.dlogp[row] : 0.f;
-  const float dH = a.dentropy ? a.dentropy[row] : 0.f, lse = a.lse[row];
-  // what lies at special places, by every wave: lane j has alternative j
-  const int lane = threadIdx.x & 63;
-  int64_t id = -1;
-  float dtop = 0.f;
-  if (a.dtop && lane < a.top) {
-    id = a.top_id[row * a.top + lane];
-    if (id >= 0 && id < a.V) dtop = a.dtop[row * a.top + lane];
-  }
-  const float all = lanes_sum<64>(dtop);
-  const float A = (a.dlse ? a.dlse[row] : 0.f) - dlogp - all - (dH == 0.f ? 0.f : dH * a.entropy[row]);
-  for (int i = t; i < WORDS; i += TPR) s_bits[sub][i] = 0;
-  if (t < 64) {
-    s_id[sub][lane] = dtop != 0.f ? (int)id : -1, s_own[sub][lane] = dtop;
-    if (lane == 0) s_id[sub][MOST] = dlogp != 0.f ? (int)token : -1, s_own[sub][MOST] = dlogp;
-  }
-  sync();
-  if (t < 64) {
-    auto mark = [&](int64_t v, float own) {
-      if (own != 0.f && v >= first && v < end) atomicOr(&s_bits[sub][(v - first) >> 8], 1u << ((v - first) >> 3 & 31));
-    };
-    mark(id, dtop);
-    if (lane == 0) mark(token, dlogp);
-  }
-  sync();
-  // a row that nothing is asked of, or may be said in (-infinity alone), gets zeros, whatever it holds
-  const bool none = lse == -INFINITY || A == 0.f && dH == 0.f && dlogp == 0.f && !__any(dtop != 0.f);
   const T* x = (const T*)a.x + row * a.x_stride;
   T* dx = (T*)a.dx + row * a.dx_stride;
-  constexpr int STEPS = LEN / 8 / TPR;
   typename Vec8<T>::type raw[STEPS];
 #pragma unroll
   for (int k = 0; k < STEPS; ++k) raw[k] = load_logits(x, std::min(first + 8 * (t + k * TPR), end), end);
+  // what is asked of special places, in every wave: lane j has alternative j
+  const int64_t token = a.token ? a.token[row] : -1;
+  float dlogp = a.dlogp ? a.dlogp[row] : 0.f, dtop = 0.f;
+  const float dH = a.dentropy ? a.dentropy[row] : 0.f, lse = a.lse[row], H = a.dentropy ? a.entropy[row] : 0.f;
+  int64_t id = -1;
+  if (a.dtop && lane < a.top) id = a.top_id[row * a.top + lane], dtop = a.dtop[row * a.top + lane];
+  const float dlse = a.dlse ? a.dlse[row] : 0.f;
+  if (token < 0 || token >= a.V) dlogp = 0.f;
+  if (id < 0 || id >= a.V) dtop = 0.f;
+  const float A = dlse - dlogp - lanes_sum<64>(dtop) - (dH == 0.f ? 0.f : dH * H);
+  for (int i = t; i < WORDS; i += TPR) s_bits[sub][i] = 0;
+  sync();
+  if (t < 64) {
+    const auto mark = [&](bool is, int64_t v) {
+      if (!is || v < first || v >= end) return;
+      const int at = (int)(v - first) & ~7;
+      atomicOr(&s_bits[sub][at >> 8], 1u << (at >> 3 & 31));
+      *(f32x4*)&s_own[sub][at] = f32x4{};
+      *(f32x4*)&s_own[sub][at + 4] = f32x4{};
+    };
+    mark(dtop != 0.f, id);
+    mark(lane == 0 && dlogp != 0.f, token);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    // An element may be asked for more than once (an id twice, the token as an alternative): each lane adds all that its element
+    // is asked for, in order, and all of them write the same sum.
+    float mine = 0.f, at_token = 0.f;
+    if (a.dtop)
+      for (int k = 0; k < a.top; ++k) {
+        const int other = __builtin_amdgcn_readlane((int)id, k);  // (of an id outside, dtop is 0)
+        const float d = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, dtop), k));
+        mine += other == (int)id ? d : 0.f;
+        at_token += other == (int)token ? d : 0.f;
+      }
+    if (dlogp != 0.f && id == token) mine += dlogp;
+    if (dtop != 0.f && id >= first && id < end) s_own[sub][id - first] = mine;
+    if (lane == 0 && dlogp != 0.f && token >= first && token < end) s_own[sub][token - first] = at_token + dlogp;
+  }
+  sync();
+  // a row that nothing is asked of, or may be said in (-infinity alone), gets zeros, whatever it holds
+  const bool none = lse == -INFINITY || (A == 0.f && dH == 0.f && dlogp == 0.f && !__any(dtop != 0.f));
 #pragma unroll
   for (int q = 0; q < STEPS; ++q) {
-    const int i = first + 8 * (t + q * TPR), unit = t + q * TPR;
+    const int unit = t + q * TPR, i = first + 8 * unit;
     if (i >= end) break;
-    float v[8], own[8] = {};
-    if (s_bits[sub][unit >> 5] >> (unit & 31) & 1)
-      for (int k = 0; k <= MOST; ++k) {  // (in order: the same sum every time)
-        const int at = s_id[sub][k] - i;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) own[j] += at == j ? s_own[sub][k] : 0.f;
-      }
+    float v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float logp = __builtin_fmaf((float)raw[q][j], a.scale, -lse), p = __builtin_amdgcn_exp2f(logp * LOG2E);
-      v[j] = none ? 0.f : a.scale * (p * (A - dH * fmaxf(logp, -200.f)) + own[j]);
+      v[j] = p * (A - dH * fmaxf(logp, -200.f));
     }
+    if (s_bits[sub][unit >> 5] >> (unit & 31) & 1)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += s_own[sub][8 * unit + j];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = none ? 0.f : a.scale * v[j];
     store8(dx, i, end, v);
   }
 }
