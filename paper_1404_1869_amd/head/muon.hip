@@ -22,7 +22,6 @@ namespace head {
 namespace {
 
 constexpr int XS = 13;  // X and A are held times 2^XS
-constexpr int T = 128;  // a tile's sides
 constexpr int SUMS = 1024;  // partial sums of a matrix's norm
 
 // A matrix in a launch, passed by value.
@@ -143,58 +142,165 @@ __global__ __launch_bounds__(256) void start_kernel(MuonLaunch l) {
   }
 }
 
-// A = X X' (SQUARE: A A) into slabs [splits][r][up(r, T)]: the tiles of the lower half.  TALL: X' X.
-template <bool TALL, bool SQUARE, int PARTS>
-__global__ __launch_bounds__(256) void gram_kernel(MuonLaunch l) {
-  constexpr int NST = 2, STAGE = 2 * T * BK * 2, OUT_ROW = 64 * 4 + 16;
-  __shared__ __align__(1024) char s_mem[NST * STAGE > 4 * 32 * OUT_ROW ? NST * STAGE : 4 * 32 * OUT_ROW];
+// Tile shapes: 256 x 256 by eight waves, a workgroup per CU, or 128 x 128 by four, two per CU.
+template <int T>
+struct Shape {
+  static constexpr int WM = 2, WN = T == 256 ? 4 : 2, NW = WM * WN, NST = 2, STAGE = 2 * T * BK * 2;
+  static constexpr int WCOLS = T / WM, WROWS = T / WN, TM = WCOLS / 32, TN = WROWS / 32;
+  static constexpr int OUT_ROW = WCOLS * 4 + 16, OUT = NW * 32 * OUT_ROW;
+  static constexpr int LDS = NST * STAGE > OUT ? NST * STAGE : OUT;
+};
+// The tile's rows n on their way out, through LDS: `row(n, c, v)` gets eight values of row n of the tile from column c on.
+template <int T, typename F>
+__device__ inline void rows_out(char* s_mem, int wave, int lane, const f32x16 (&acc)[Shape<T>::TM][Shape<T>::TN], F&& row) {
+  using S = Shape<T>;
+  const int l32 = lane & 31, half = lane >> 5, wm = wave % S::WM, wn = wave / S::WM;
+  constexpr int LANES = S::WCOLS / 8, LINES = 64 / LANES;
+  __syncthreads();
+  char* stg = s_mem + wave * 32 * S::OUT_ROW;
+#pragma unroll
+  for (int b = 0; b < S::TN; ++b) {
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][b][4 * q + e];
+        *(f32x4*)(stg + l32 * S::OUT_ROW + (32 * i + 8 * q + 4 * half) * 4) = v;
+      }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int k = 0; k < 32 / LINES; ++k) {
+      const int line = LINES * k + lane / LANES, c = lane % LANES * 8;
+      const f32x4 lo = *(const f32x4*)(stg + line * S::OUT_ROW + c * 4), hi = *(const f32x4*)(stg + line * S::OUT_ROW + c * 4 + 16);
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = j < 4 ? lo[j & 3] : hi[j & 3];
+      row(wn * S::WROWS + 32 * b + line, wm * S::WCOLS + c, v);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+}
+
+// The tile's columns m on their way out as rows: `row(m, n, v)` gets eight values of column m from row n on.
+template <int T, typename F>
+__device__ inline void columns_out(char* s_mem, int wave, int lane, const f32x16 (&acc)[Shape<T>::TM][Shape<T>::TN], F&& row) {
+  using S = Shape<T>;
+  const int l32 = lane & 31, half = lane >> 5, wm = wave % S::WM, wn = wave / S::WM;
+  constexpr int ROW = S::WROWS * 4 + 16, LANES = S::WROWS / 8, LINES = 64 / LANES;
+  static_assert(S::NW * 32 * ROW <= S::LDS, "a wave's 32 columns fit");
+  __syncthreads();
+  char* stg = s_mem + wave * 32 * ROW;
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+#pragma unroll
+    for (int b = 0; b < S::TN; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) *(float*)(stg + (8 * (e / 4) + 4 * half + e % 4) * ROW + (32 * b + l32) * 4) = acc[i][b][e];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int k = 0; k < 32 / LINES; ++k) {
+      const int line = LINES * k + lane / LANES, c = lane % LANES * 8;
+      const f32x4 lo = *(const f32x4*)(stg + line * ROW + c * 4), hi = *(const f32x4*)(stg + line * ROW + c * 4 + 16);
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = j < 4 ? lo[j & 3] : hi[j & 3];
+      row(wm * S::WCOLS + 32 * i + line, wn * S::WROWS + c, v);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+}
+
+// Eight values of a matrix held in parts.
+template <int PARTS>
+__device__ inline void load_parts(const _Float16* p, int64_t part, float (&v)[8]) {
+  load8(p, v);
+  if constexpr (PARTS == 2) {
+    float lo[8];
+    load8(p + part, lo);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += lo[j];
+  }
+}
+// An entry of A (held times 2^XS) from X X', or (SQUARE) of P = b A + c A^2 from A's and A A's.
+template <bool SQUARE>
+struct Entry {
+  float fa, fs;
+  __device__ inline Entry(const MuonLaunch& l) {
+    fa = SQUARE ? ldexpf(l.b, l.poly_shift - XS) : 0.f;
+    fs = SQUARE ? ldexpf(l.c, l.poly_shift - 2 * XS) : ldexpf(1.f, -XS);
+  }
+  __device__ inline float operator()(float sum, float a) const { return SQUARE ? __builtin_fmaf(fa, a, fs * sum) : fs * sum; }
+};
+
+// A = X X' (of a tall matrix X' X), or (SQUARE) P = b A + c A A: the tiles of the lower half, written in both places.  SLABS: their
+// sums alone, a slab [r][up(r, T)] for each split; mirror_kernel does the rest.
+template <bool SQUARE, int PARTS, int T, bool SLABS>
+__global__ __launch_bounds__(64 * Shape<T>::NW) void gram_kernel(MuonLaunch l) {
+  using S = Shape<T>;
+  __shared__ __align__(1024) char s_mem[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int all = gridDim.x, xcd = blockIdx.x % 8, per = all / 8, rem = all % 8;
   const int job = xcd * per + min(xcd, rem) + blockIdx.x / 8;  // each XCD takes a contiguous range
   const Mat& t = mat_of(l, job);
   const int r = min(t.rows, t.cols), tiles = (r + T - 1) / T, half_tiles = tiles * (tiles + 1) / 2;
-  const int in = job - t.first, split = in / half_tiles, id = in - split * half_tiles;
+  const int in = job - t.first, split = SLABS ? in / half_tiles : 0, id = in - split * half_tiles;
   int tm = (int)((sqrtf(8.f * id + 1.f) - 1.f) * 0.5f);  // id = tm (tm + 1) / 2 + tn, tn <= tm
   while (tm * (tm + 1) / 2 > id) --tm;
   while ((tm + 1) * (tm + 2) / 2 <= id) ++tm;
   const int tn = id - tm * (tm + 1) / 2, m0 = tm * T, n0 = tn * T;
   const int ld = up8(SQUARE ? r : t.cols);
   const int64_t part = (int64_t)(SQUARE ? r : t.rows) * ld;
-  const void* x = l.work + (SQUARE ? t.a : t.x[l.from]);
-  const int rows = SQUARE ? r : TALL ? ld : t.rows, K = SQUARE ? r : TALL ? t.rows : t.cols;
-  f32x16 acc[2][2];
-  multiply<_Float16, TALL, TALL, T, T, 2, 2, NST, PARTS == 2>(
-      s_mem, Multiplied{x, x, ld, ld, part, part, rows, rows, TALL ? K : up8(K), PARTS == 2 ? 3 : 1}, m0, n0, split, t.splits, wave, lane, acc);
-
-  const int l32 = lane & 31, half = lane >> 5, wm = wave % 2, wn = wave / 2;
-  const int64_t slab_ld = (int64_t)tiles * T;
-  float* out = (float*)(l.work + t.slab) + split * r * slab_ld;
-  __syncthreads();
-  char* stg = s_mem + wave * 32 * OUT_ROW;
+  const _Float16* x = (const _Float16*)(l.work + (SQUARE ? t.a : t.x[l.from]));
+  f32x16 acc[S::TM][S::TN];
+  Multiplied op{x, x, ld, ld, part, part, SQUARE ? r : t.rows, SQUARE ? r : t.rows, ld, PARTS == 2 ? 3 : 1};
+  const int splits = SLABS ? t.splits : 1;
+  if (SQUARE || t.rows <= t.cols) {
+    multiply<_Float16, false, false, T, T, S::WM, S::WN, S::NST, PARTS == 2>(s_mem, op, m0, n0, split, splits, wave, lane, acc);
+  } else if constexpr (!SQUARE) {
+    op.a_rows = op.b_rows = ld, op.K = t.rows;
+    multiply<_Float16, true, true, T, T, S::WM, S::WN, S::NST, PARTS == 2>(s_mem, op, m0, n0, split, splits, wave, lane, acc);
+  }
+  if constexpr (SLABS) {
+    const int64_t slab_ld = (int64_t)tiles * T;
+    float* out = (float*)(l.work + t.slab) + split * r * slab_ld;
+    rows_out<T>(s_mem, wave, lane, acc, [&](int n, int m, const float (&v)[8]) {
+      if (n0 + n < r) store8(out + (n0 + n) * slab_ld + m0 + m, v);
+    });
+  } else {
+    const int lda = up8(r);
+    const int64_t apart = (int64_t)r * lda;
+    _Float16* to = (_Float16*)(l.work + (SQUARE ? t.poly : t.a));
+    const Entry<SQUARE> entry(l);
+    if (tm != tn)  // the mirrored tile (one on the diagonal is its own mirror, within roundings)
+      columns_out<T>(s_mem, wave, lane, acc, [&](int m, int n, float (&v)[8]) {
+        n += n0, m += m0;  // (n is below r: its tile is a whole one)
+        if (m >= r) return;
+        const int64_t at = (int64_t)m * lda + n;
+        float a[8] = {};
+        if constexpr (SQUARE) load_parts<PARTS>(x + at, apart, a);
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+        for (int j = 0; j < 8; ++j) v[j] = entry(v[j], a[j]);
+        store_parts<PARTS>(to + at, apart, v);
+      });
+    rows_out<T>(s_mem, wave, lane, acc, [&](int n, int m, float (&v)[8]) {
+      n += n0, m += m0;
+      if (n >= r || m >= lda) return;
+      const int64_t at = (int64_t)n * lda + m;
+      float a[8] = {};
+      if constexpr (SQUARE) load_parts<PARTS>(x + at, apart, a);
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        f32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][b][4 * q + e];
-        *(f32x4*)(stg + l32 * OUT_ROW + (32 * i + 8 * q + 4 * half) * 4) = v;
-      }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int line = 4 * k + (lane >> 4), n = n0 + wn * 64 + 32 * b + line, m = m0 + wm * 64 + (lane & 15) * 4;
-      if (n < r) *(f32x4*)(out + n * slab_ld + m) = *(const f32x4*)(stg + line * OUT_ROW + (lane & 15) * 16);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      for (int j = 0; j < 8; ++j) v[j] = entry(v[j], a[j]);  // (0 past column r)
+      store_parts<PARTS>(to + at, apart, v);
+    });
   }
 }
 
-// Adds the slabs of a 64 x 64 block and its mirror: A (POLY: P = b A + c A^2), in parts, both blocks.
-template <bool POLY, int PARTS>
-__global__ __launch_bounds__(256) void mirror_kernel(MuonLaunch l) {
+// Adds the slabs of a 64 x 64 block and its mirror: A (POLY: P = b A + c A^2), in parts, both blocks.  T: the slabs' tiles.  (A
+// thread has four values of a slab: there are few blocks, and each waits for memory.)
+template <bool POLY, int PARTS, int T>
+__global__ __launch_bounds__(1024) void mirror_kernel(MuonLaunch l) {
   __shared__ float s_v[64][65];
   const Mat& t = mat_of(l, blockIdx.x);
   const int r = min(t.rows, t.cols), id = blockIdx.x - t.first;
@@ -205,63 +311,40 @@ __global__ __launch_bounds__(256) void mirror_kernel(MuonLaunch l) {
   const int64_t slab_ld = (r + T - 1) / T * T;
   const float* slab = (const float*)(l.work + t.slab);
   const int c4 = (threadIdx.x & 15) * 4, row0 = threadIdx.x >> 4;
+  f32x4 sum{};
+  if (bn * 64 + row0 < r)
+#pragma unroll 8
+    for (int s = 0; s < t.splits; ++s) sum += *(const f32x4*)(slab + (s * (int64_t)r + bn * 64 + row0) * slab_ld + bm * 64 + c4);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int rr = row0 + 16 * k, n = bn * 64 + rr;
-    f32x4 v{};
-    if (n < r)
-#pragma unroll 4
-      for (int s = 0; s < t.splits; ++s) v += *(const f32x4*)(slab + (s * (int64_t)r + n) * slab_ld + bm * 64 + c4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s_v[rr][c4 + e] = v[e];
-  }
+  for (int e = 0; e < 4; ++e) s_v[row0][c4 + e] = sum[e];
   __syncthreads();
   const int ld = up8(r);
   const int64_t part = (int64_t)r * ld;
   const _Float16* A = (const _Float16*)(l.work + t.a);
   _Float16* to = (_Float16*)(l.work + (POLY ? t.poly : t.a));
-  // block (bn, bm) as it lies, then (bm, bn): rows of 64 in units of eight
-  for (int side = 0; side < (bm == bn ? 1 : 2); ++side) {
+  const Entry<POLY> entry(l);
+  // the first half of the threads: block (bn, bm) as it lies, the other: (bm, bn); rows of 64 in units of eight
+  const int side = threadIdx.x >> 9, unit = threadIdx.x & 511, rr = unit >> 3, cc = (unit & 7) * 8;
+  const int n = (side ? bm : bn) * 64 + rr, m = (side ? bn : bm) * 64 + cc;
+  if (n >= r || m >= ld || (side && bm == bn)) return;
+  float v[8], own[8] = {};
+  const int64_t at = (int64_t)n * ld + m;
+  if constexpr (POLY) load_parts<PARTS>(A + at, part, own);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int unit = threadIdx.x + 256 * k, rr = unit >> 3, cc = (unit & 7) * 8;
-      const int n = (side ? bm : bn) * 64 + rr, m = (side ? bn : bm) * 64 + cc;
-      if (n >= r || m >= ld) continue;
-      float v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        // a block on the diagonal is symmetric to the bit too: the half with the larger column counts
-        const bool swap = side || (bm == bn && cc + j < rr);
-        const float x = swap ? s_v[cc + j][rr] : s_v[rr][cc + j];
-        v[j] = m + j < r ? x : 0.f;
-      }
-      const int64_t at = (int64_t)n * ld + m;
-      if constexpr (POLY) {
-        float a[8];
-        load8(A + at, a);
-        if constexpr (PARTS == 2) {
-          float lo[8];
-          load8(A + part + at, lo);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) a[j] += lo[j];
-        }
-        const float fa = ldexpf(l.b, l.poly_shift - XS), fs = ldexpf(l.c, l.poly_shift - 2 * XS);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = __builtin_fmaf(fa, a[j], fs * v[j]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = ldexpf(v[j], -XS);
-      }
-      store_parts<PARTS>(to + at, part, v);
-    }
+  for (int j = 0; j < 8; ++j) {
+    // a block on the diagonal is symmetric to the bit too: the half with the larger column counts
+    const bool swap = side || (bm == bn && cc + j < rr);
+    const float x = swap ? s_v[cc + j][rr] : s_v[rr][cc + j];
+    v[j] = entry(m + j < r ? x : 0.f, own[j]);
   }
+  store_parts<PARTS>(to + at, part, v);
 }
 
-// X = a X + P X (TALL: a X + X P), into the other buffer, or (LAST) p's step.
-template <bool TALL, int PARTS, bool LAST, typename P, typename O>
-__global__ __launch_bounds__(256) void update_kernel(MuonLaunch l) {
-  constexpr int NST = 2, STAGE = 2 * T * BK * 2, OUT_ROW = 64 * 4 + 16;
-  __shared__ __align__(1024) char s_mem[NST * STAGE > 4 * 32 * OUT_ROW ? NST * STAGE : 4 * 32 * OUT_ROW];
+// X = a X + P X (of a tall matrix a X + X P), into the other buffer, or (LAST) p's step.
+template <int PARTS, int T, bool LAST, typename P, typename O>
+__global__ __launch_bounds__(64 * Shape<T>::NW) void update_kernel(MuonLaunch l) {
+  using S = Shape<T>;
+  __shared__ __align__(1024) char s_mem[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int all = gridDim.x, xcd = blockIdx.x % 8, per = all / 8, rem = all % 8;
   const int job = xcd * per + min(xcd, rem) + blockIdx.x / 8;
@@ -274,58 +357,36 @@ __global__ __launch_bounds__(256) void update_kernel(MuonLaunch l) {
   const int64_t part = (int64_t)t.rows * ld, ppart = (int64_t)r * ldp;
   const _Float16* x = (const _Float16*)(l.work + t.x[l.from]);
   const void* poly = l.work + t.poly;
-  f32x16 acc[2][2];
-  const Multiplied wide{x, poly, ld, ldp, part, ppart, ld, r, r, PARTS == 2 ? 3 : 1};
-  const Multiplied tall{poly, x, ldp, ld, ppart, part, r, t.rows, ldp, PARTS == 2 ? 3 : 1};
-  multiply<_Float16, !TALL, false, T, T, 2, 2, NST, PARTS == 2>(s_mem, TALL ? tall : wide, m0, n0, 0, 1, wave, lane, acc);
+  f32x16 acc[S::TM][S::TN];
+  if (t.rows <= t.cols)
+    multiply<_Float16, true, false, T, T, S::WM, S::WN, S::NST, PARTS == 2>(
+        s_mem, Multiplied{x, poly, ld, ldp, part, ppart, ld, r, r, PARTS == 2 ? 3 : 1}, m0, n0, 0, 1, wave, lane, acc);
+  else
+    multiply<_Float16, false, false, T, T, S::WM, S::WN, S::NST, PARTS == 2>(
+        s_mem, Multiplied{poly, x, ldp, ld, ppart, part, r, t.rows, ldp, PARTS == 2 ? 3 : 1}, m0, n0, 0, 1, wave, lane, acc);
 
-  const int l32 = lane & 31, half = lane >> 5, wm = wave % 2, wn = wave / 2;
   const float unscale = ldexpf(1.f, -l.poly_shift), rate = ldexpf(l.lr * t.rate, -XS);
   _Float16* to = (_Float16*)(l.work + t.x[l.from ^ 1]);
-  __syncthreads();
-  char* stg = s_mem + wave * 32 * OUT_ROW;
+  rows_out<T>(s_mem, wave, lane, acc, [&](int n, int m, float (&v)[8]) {
+    n += n0, m += m0;
+    if (n >= t.rows || m >= ld) return;
+    const int64_t at = (int64_t)n * ld + m;
+    float old[8];
+    load_parts<PARTS>(x + at, part, old);
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+    for (int j = 0; j < 8; ++j) v[j] = __builtin_fmaf(l.a, old[j], v[j] * unscale);
+    if constexpr (!LAST) {
+      store_parts<PARTS>(to + at, part, v);
+    } else {
+      P* p = (P*)t.p + (int64_t)n * t.cols;
+      float w[8];
+      load8(p, m, t.cols, w);
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        f32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][b][4 * q + e];
-        *(f32x4*)(stg + l32 * OUT_ROW + (32 * i + 8 * q + 4 * half) * 4) = v;
-      }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {  // eight columns of a row
-      const int line = 8 * k + (lane >> 3), n = n0 + wn * 64 + 32 * b + line, c = (lane & 7) * 8, m = m0 + wm * 64 + c;
-      if (n >= t.rows || m >= ld) continue;
-      float v[8], old[8];
-      const f32x4 lo = *(const f32x4*)(stg + line * OUT_ROW + c * 4), hi = *(const f32x4*)(stg + line * OUT_ROW + c * 4 + 16);
-      const int64_t at = (int64_t)n * ld + m;
-      load8(x + at, old);
-      if constexpr (PARTS == 2) {
-        float rest[8];
-        load8(x + part + at, rest);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) old[j] += rest[j];
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = __builtin_fmaf(l.a, old[j], (j < 4 ? lo[j & 3] : hi[j & 3]) * unscale);
-      if constexpr (!LAST) {
-        store_parts<PARTS>(to + at, part, v);
-      } else {
-        P* p = (P*)t.p + (int64_t)n * t.cols;
-        float w[8];
-        load8(p, m, t.cols, w);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = __builtin_fmaf(-rate, v[j], w[j] * l.decay);
-        store8(p, m, t.cols, w);
-        if (t.copy) store8((O*)t.copy + (int64_t)n * t.cols, m, t.cols, w);
-      }
+      for (int j = 0; j < 8; ++j) w[j] = __builtin_fmaf(-rate, v[j], w[j] * l.decay);
+      store8(p, m, t.cols, w);
+      if (t.copy) store8((O*)t.copy + (int64_t)n * t.cols, m, t.cols, w);
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  }
+  });
 }
 
 template <typename F>
@@ -349,32 +410,72 @@ int64_t half_tiles(int64_t r, int64_t side) {
   const int64_t tiles = (r + side - 1) / side;
   return tiles * (tiles + 1) / 2;
 }
-int splits_of(int64_t tiles, int64_t stages) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), stages / 8, 16}));
+int64_t all_tiles(int64_t rows, int64_t cols, int64_t side) { return ((rows + side - 1) / side) * ((cols + side - 1) / side); }
+
+// The time of a launch of `jobs` tiles of `stages` of 64 k in us, by what launches of many shapes took: a stage of 256 x 256 takes
+// 1.25 us on an idle chip and 1.75 on a full one, of 128 x 128 0.62 alone on a CU and 1.15 for two.
+double launch_us(int T, double jobs, double stages) {
+  if (T == 256) return std::ceil(jobs / 256) * (stages * (1.25 + 0.5 * std::min(1.0, jobs / 256)) + 8);
+  if (jobs <= 256) return stages * (0.62 + 0.25 * jobs / 256) + 5;
+  return std::ceil(jobs / 512) * (stages * 1.15 + 6);
+}
+struct Tiling {
+  int T, splits;
+};
+// Of products of half the tiles of r x r over `stages`: tiles and splits with the least time.  Splits cost the slabs' way through
+// memory and a launch more.
+Tiling choose(const dn_muon_tensor* ts, int count, int products, bool square) {
+  Tiling best{128, 1};
+  double least = 1e300;
+  for (const int T : {256, 128})
+    for (int s = 1; s <= 16; ++s) {
+      double jobs = 0, stages = 0, area = 0;
+      for (int i = 0; i < count; ++i) {
+        const int64_t r = std::min(ts[i].rows, ts[i].cols), k = square ? r : std::max(ts[i].rows, ts[i].cols);
+        jobs += (double)half_tiles(r, T) * s, area += (double)half_tiles(r, T) * T * T;
+        stages = std::max(stages, (double)((k + BK - 1) / BK * products));
+      }
+      if (s > 1 && stages / s < 4) break;
+      const double us = launch_us(T, jobs, std::ceil(stages / s)) + (s > 1 ? 5 + s * area * 8 / 6e6 : 0);
+      if (us < least * 0.999) least = us, best = Tiling{T, s};
+    }
+  return best;
 }
 
 // A group of matrices that share launches, laid out in the workspace.
 struct Group {
   MuonLaunch l;
-  int32_t gram_splits[MATS], square_splits[MATS];
+  Tiling gram, square;
+  int update;  // tiles of the update
   size_t total;
 };
 void plan_group(const dn_muon_tensor* ts, int count, int parts, Group& gr) {
   gr.l = MuonLaunch{};
   Work w;
-  int64_t tiles = 0;
-  for (int i = 0; i < count; ++i) tiles += half_tiles(std::min(ts[i].rows, ts[i].cols), T);
+  const int products = parts == 2 ? 3 : 1;
+  gr.gram = choose(ts, count, products, false), gr.square = choose(ts, count, products, true);
+  double us[2] = {};
+  for (int k = 0; k < 2; ++k) {
+    double jobs = 0, stages = 0;
+    for (int i = 0; i < count; ++i) {
+      jobs += (double)all_tiles(ts[i].rows, ts[i].cols, k ? 128 : 256);
+      stages = std::max(stages, (double)((std::min(ts[i].rows, ts[i].cols) + BK - 1) / BK * products));
+    }
+    us[k] = launch_us(k ? 128 : 256, jobs, stages);
+  }
+  gr.update = us[0] < us[1] ? 256 : 128;
   int32_t sums = 0;
   for (int i = 0; i < count; ++i) {
     Mat& t = gr.l.t[i];
     t.g = ts[i].g, t.m = ts[i].m, t.p = ts[i].p, t.copy = ts[i].copy;
     t.rows = (int32_t)ts[i].rows, t.cols = (int32_t)ts[i].cols, t.rate = (float)ts[i].rate;
-    const int64_t r = std::min(t.rows, t.cols), c = std::max(t.rows, t.cols);
+    const int64_t r = std::min(t.rows, t.cols);
     for (int b = 0; b < 2; ++b) t.x[b] = w.take((size_t)parts * t.rows * up8(t.cols) * 2);
     t.a = w.take((size_t)parts * r * up8((int32_t)r) * 2), t.poly = w.take((size_t)parts * r * up8((int32_t)r) * 2);
-    const int products = parts == 2 ? 3 : 1;
-    gr.gram_splits[i] = splits_of(tiles, (c + BK - 1) / BK * products), gr.square_splits[i] = splits_of(tiles, (r + BK - 1) / BK * products);
-    t.slab = w.take((size_t)std::max(gr.gram_splits[i], gr.square_splits[i]) * r * up(r, T) * 4);
+    size_t slab = 0;
+    for (const Tiling& k : {gr.gram, gr.square})
+      if (k.splits > 1) slab = std::max(slab, (size_t)k.splits * r * up(r, k.T) * 4);
+    t.slab = w.take(slab);
     t.sums = (int32_t)std::min<int64_t>(SUMS, ((int64_t)t.rows * t.cols + 2047) / 2048);
     t.norm = sums, sums += t.sums;
   }
@@ -383,87 +484,69 @@ void plan_group(const dn_muon_tensor* ts, int count, int parts, Group& gr) {
   gr.total = w.total;
 }
 
-// The launch of those matrices that `take` chooses, each with `units` workgroups and `splits` splits.
-template <typename Take, typename Units>
-int64_t select(const MuonLaunch& all, MuonLaunch& l, Take&& take, Units&& units) {
-  l = all;
-  l.count = 0;
+// A launch of all matrices, each with `units` workgroups.
+template <typename Units>
+int64_t spread(MuonLaunch& l, Units&& units) {
   int64_t total = 0;
-  for (int i = 0; i < all.count; ++i)
-    if (take(i)) {
-      Mat& t = l.t[l.count++];
-      t = all.t[i];
-      t.first = (int32_t)total;
-      total += units(i, t);
-    }
+  for (int i = 0; i < l.count; ++i) {
+    l.t[i].first = (int32_t)total;
+    total += units(l.t[i]);
+  }
   return total;
+}
+
+template <bool SQUARE, int PARTS>
+int run_gram(MuonLaunch& l, const Tiling& k, hipStream_t st) {
+  const auto side = [](const Mat& t) { return std::min(t.rows, t.cols); };
+  const dim3 grid((unsigned)spread(l, [&](Mat& t) { return t.splits = k.splits, half_tiles(side(t), k.T) * k.splits; }));
+  if (k.splits == 1) {
+    if (k.T == 256) gram_kernel<SQUARE, PARTS, 256, false><<<grid, 512, 0, st>>>(l);
+    else gram_kernel<SQUARE, PARTS, 128, false><<<grid, 256, 0, st>>>(l);
+    return (int)hipGetLastError();
+  }
+  if (k.T == 256) gram_kernel<SQUARE, PARTS, 256, true><<<grid, 512, 0, st>>>(l);
+  else gram_kernel<SQUARE, PARTS, 128, true><<<grid, 256, 0, st>>>(l);
+  if (const int err = (int)hipGetLastError()) return err;
+  const dim3 blocks((unsigned)spread(l, [&](Mat& t) { return half_tiles(side(t), 64); }));
+  if (k.T == 256) mirror_kernel<SQUARE, PARTS, 256><<<blocks, 1024, 0, st>>>(l);
+  else mirror_kernel<SQUARE, PARTS, 128><<<blocks, 1024, 0, st>>>(l);
+  return (int)hipGetLastError();
+}
+template <int PARTS, bool LAST, typename P, typename O>
+int run_update(MuonLaunch& l, int T, hipStream_t st) {
+  const dim3 grid((unsigned)spread(l, [&](const Mat& t) { return all_tiles(t.rows, t.cols, T); }));
+  if (T == 256) update_kernel<PARTS, 256, LAST, P, O><<<grid, 512, 0, st>>>(l);
+  else update_kernel<PARTS, 128, LAST, P, O><<<grid, 256, 0, st>>>(l);
+  return (int)hipGetLastError();
 }
 
 template <int PARTS>
 int run_group(Group& gr, const dn_muon_params& k, dn_dtype p_dt, dn_dtype g_dt, dn_dtype copy_dt, hipStream_t st) {
-  MuonLaunch l;
-  const auto any = [](int) { return true; };
-  int64_t n = select(gr.l, l, any, [](int, const Mat& t) { return (int64_t)t.sums; });
-  with_type(g_dt, [&](auto g) {
+  MuonLaunch& l = gr.l;
+  int err = with_type(g_dt, [&](auto g) {
+    const int64_t n = spread(l, [](const Mat& t) { return (int64_t)t.sums; });
     momentum_kernel<decltype(g)><<<dim3((unsigned)n), 256, 0, st>>>(l);
-    return 0;
+    return (int)hipGetLastError();
   });
-  if (const int err = (int)hipGetLastError()) return err;
-  n = select(gr.l, l, any, [](int, const Mat& t) { return ((int64_t)t.rows * (up8(t.cols) / 8) + 1023) / 1024; });
-  with_type(g_dt, [&](auto g) {
+  if (err) return err;
+  err = with_type(g_dt, [&](auto g) {
+    const int64_t n = spread(l, [](const Mat& t) { return ((int64_t)t.rows * (up8(t.cols) / 8) + 1023) / 1024; });
     start_kernel<decltype(g), PARTS><<<dim3((unsigned)n), 256, 0, st>>>(l);
-    return 0;
+    return (int)hipGetLastError();
   });
-  if (const int err = (int)hipGetLastError()) return err;
-  const auto tall = [&](int i) { return gr.l.t[i].rows > gr.l.t[i].cols; };
-  const auto wide = [&](int i) { return !tall(i); };
-  const auto side = [](const Mat& t) { return std::min(t.rows, t.cols); };
-  for (int s = 0; s < k.steps; ++s) {
-    gr.l.a = (float)k.coefficients[s][0], gr.l.b = (float)k.coefficients[s][1], gr.l.c = (float)k.coefficients[s][2];
+  for (int s = 0; s < k.steps && !err; ++s) {
+    l.a = (float)k.coefficients[s][0], l.b = (float)k.coefficients[s][1], l.c = (float)k.coefficients[s][2];
     // |P| <= |b| |A| + |c| |A|^2, which is at most 2.25 |c| + 1.5 |b| for singular values up to 1.22, and twice that to spare
     const double most = 2 * (1.5 * std::fabs(k.coefficients[s][1]) + 2.25 * std::fabs(k.coefficients[s][2]));
-    gr.l.poly_shift = std::min(XS, (int)std::floor(std::log2(65504 / std::max(most, 1e-6))));
-    gr.l.from = s & 1;
-    const auto gram = [&](int i, Mat& t) {
-      t.splits = gr.gram_splits[i];
-      return half_tiles(side(t), T) * t.splits;
-    };
-    if ((n = select(gr.l, l, wide, gram))) gram_kernel<false, false, PARTS><<<dim3((unsigned)n), 256, 0, st>>>(l);
-    if ((n = select(gr.l, l, tall, gram))) gram_kernel<true, false, PARTS><<<dim3((unsigned)n), 256, 0, st>>>(l);
-    n = select(gr.l, l, any, [&](int i, Mat& t) { return t.splits = gr.gram_splits[i], half_tiles(side(t), 64); });
-    mirror_kernel<false, PARTS><<<dim3((unsigned)n), 256, 0, st>>>(l);
-    n = select(gr.l, l, any, [&](int i, Mat& t) {
-      t.splits = gr.square_splits[i];
-      return half_tiles(side(t), T) * t.splits;
+    l.poly_shift = std::min(XS, (int)std::floor(std::log2(65504 / std::max(most, 1e-6))));
+    l.from = s & 1;
+    if ((err = run_gram<false, PARTS>(l, gr.gram, st)) || (err = run_gram<true, PARTS>(l, gr.square, st))) return err;
+    err = s + 1 < k.steps ? run_update<PARTS, false, float, __bf16>(l, gr.update, st) : with_type(p_dt, [&](auto p) {
+      using P = decltype(p);
+      return copy_dt == DN_F16 ? run_update<PARTS, true, P, _Float16>(l, gr.update, st) : run_update<PARTS, true, P, __bf16>(l, gr.update, st);
     });
-    gram_kernel<false, true, PARTS><<<dim3((unsigned)n), 256, 0, st>>>(l);
-    n = select(gr.l, l, any, [&](int i, Mat& t) { return t.splits = gr.square_splits[i], half_tiles(side(t), 64); });
-    mirror_kernel<true, PARTS><<<dim3((unsigned)n), 256, 0, st>>>(l);
-    const auto update = [&](int, Mat& t) { return (int64_t)((t.rows + T - 1) / T) * ((t.cols + T - 1) / T); };
-    for (int shape = 0; shape < 2; ++shape) {
-      n = shape ? select(gr.l, l, tall, update) : select(gr.l, l, wide, update);
-      if (!n) continue;
-      const dim3 grid((unsigned)n);
-      if (s + 1 < k.steps) {
-        if (shape) update_kernel<true, PARTS, false, float, __bf16><<<grid, 256, 0, st>>>(l);
-        else update_kernel<false, PARTS, false, float, __bf16><<<grid, 256, 0, st>>>(l);
-        continue;
-      }
-      with_type(p_dt, [&](auto p) {
-        using P = decltype(p);
-        const auto go = [&](auto o) {
-          using O = decltype(o);
-          if (shape) update_kernel<true, PARTS, true, P, O><<<grid, 256, 0, st>>>(l);
-          else update_kernel<false, PARTS, true, P, O><<<grid, 256, 0, st>>>(l);
-        };
-        if (copy_dt == DN_F16) go(_Float16{});
-        else go(__bf16{});
-        return 0;
-      });
-    }
-    if (const int err = (int)hipGetLastError()) return err;
   }
-  return 0;
+  return err;
 }
 
 }  // namespace
