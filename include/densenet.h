@@ -434,7 +434,7 @@ int densenet_quantize_blocks(const void* d_x, int64_t x_stride, int64_t n, int32
  * A block's products are summed in 32 bits and multiplied by the product of its two scales (which has to be in fp32's range).
  * d_y [n][V]: `y_dtype`, any of DN_F32, DN_F16, DN_BF16.  d_workspace: NULL for a size query into *bytes_needed (which depends on
  * the codes' alignment and strides: pass the same).  Codes whose rows start on 16 bytes are read as they lie, others are copied to
- * such rows first.  Limits (DN_E_TOO_LARGE): C <= 2^20; n, V <= 2^31 - 256; n V in tiles of 128 x 32 below 2^24. */
+ * such rows first.  Limits (DN_E_TOO_LARGE): C <= 2^20; n, V <= 2^31 - 256; n V in tiles of 128 x 128 below 2^24. */
 int densenet_block_product(const void* d_a, int64_t a_stride, const float* d_a_scale, const void* d_w,
                            int64_t w_stride, const float* d_w_scale, int64_t n, int32_t C, int32_t V,
                            void* d_y, int64_t y_stride, dn_dtype y_dtype, void* d_workspace,

@@ -616,7 +616,7 @@ Plan8 plan_product(const ProductArgs& a, bool exact) {
     for (const int64_t full : {tiles, whole, (int64_t)0})
       for (int s = full == tiles ? 1 : 2; s <= (full == tiles ? 1 : 16) && (s == 1 || blocks / s >= 2); ++s) {
         // (a launch's threads, and slabs of up to 1 GiB)
-        if ((tiles - full) * s * tile_m(t) * tile_n(t) > (1 << 28) || std::max(full, (tiles - full) * s) > MAX_LAUNCH_THREADS / 512) continue;
+        if ((tiles - full) * s * tile_m(t) * tile_n(t) > (1 << 28) || std::max(full, (tiles - full) * s) > MAX_LAUNCH_THREADS / (t == T256 ? 512 : 256)) continue;
         const double us = plan_us(t, full, tiles - full, s, blocks, exact);
         if (us < best * 0.999) best = us, p.tile = t, p.full = full, p.rest = tiles - full, p.splits = s;
       }

@@ -288,7 +288,7 @@ int densenet_block_product(const void* d_a, int64_t a_stride, const float* d_a_s
     if (!valid_dtype(y_dtype)) return fail(DN_E_UNSUPPORTED, "unknown dtype");
     if (n < 0 || C <= 0 || V <= 0) return fail(DN_E_INVALID_ARG, "n must be >= 0, C and V positive");
     if (n > MAX_ROWS || V > MAX_ROWS || C > (1 << 20)) return fail(DN_E_TOO_LARGE, "n, V or C");
-    if (((n + 31) / 32) * blocks_of(V) > MAX_TILES) return fail(DN_E_TOO_LARGE, "n times V");
+    if (blocks_of(n) * blocks_of(V) > MAX_TILES) return fail(DN_E_TOO_LARGE, "n times V");
     ProductArgs a{(const uint8_t*)d_a, (const uint8_t*)d_w, d_a_scale, d_w_scale, a_stride, w_stride, n, C, V, d_y, y_stride};
     int st;
     if ((st = check_rows("a", d_a, a_stride, n, C, 1))) return st;

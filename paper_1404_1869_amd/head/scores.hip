@@ -52,7 +52,9 @@ __device__ inline Stats join(const Stats& a, const Stats& b, float c) {
 __device__ inline Stats lanes_join(Stats a, float c) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) a = join(a, Stats{__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)}, c);
-  return a;
+  // (lanes that join the same two the other way round may differ in a last bit, and equal logits would in their log probabilities)
+  const auto first = [](float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); };
+  return Stats{first(a.m), first(a.s), first(a.t)};
 }
 
 // A wave's candidates.  All of it is the wave's own, but for the other waves' bounds of the row: no barriers.

@@ -291,6 +291,12 @@ def test_scores_ties_and_order(D, V):
         ids = D.densenet_token_scores(x.to(DT[dt]), token, top=64)[3]
         want = plain_scores(x.to(DT[dt]), token, 1.0, 64)[3]
         assert torch.equal(ids, want)
+    # equal logits have equal probabilities, to the bit
+    g = gen(V)
+    x = (torch.randn(50, V, generator=g, device="cuda") * 4).round() / 4
+    _, _, _, ids, best = D.densenet_token_scores(x, top=64)
+    v = x.gather(1, ids)
+    assert bool(((v[:, :-1] != v[:, 1:]) | (best[:, :-1] == best[:, 1:])).all()) and bool((best[:, :-1] >= best[:, 1:]).all())
 
 
 @pytest.mark.parametrize("V", [10, 5000, 40000])

@@ -1,0 +1,136 @@
+"""The entry points of a head in 8 bits on a machine without a GPU: size queries, limits, and bad arguments refused on the host
+before any device work, with a status and a message."""
+import ctypes
+
+import pytest
+
+from paper_1404_1869_amd import densenet as D
+
+P = ctypes.c_void_p(4096)   # never read: every call below ends on the host
+ODD = ctypes.c_void_p(4097)
+INV, LARGE, SMALL, UNS = D.DN_E_INVALID_ARG, D.DN_E_TOO_LARGE, D.DN_E_BUFFER_TOO_SMALL, D.DN_E_UNSUPPORTED
+NAN, INF = float("nan"), float("inf")
+
+
+def quant(x=P, xs=64, n=4, C=64, dt=D.DN_BF16, rows=1, q=P, qs=64, k=P, t=None, ts=0, tk=None):
+    return D.lib().densenet_quantize_blocks(x, xs, n, C, dt, rows, q, qs, k, t, ts, tk, None)
+
+
+def product(a=P, as_=64, ak=P, w=P, ws=64, wk=P, n=4, C=64, V=100, y=P, ys=100, dt=D.DN_BF16, work=P, size=1 << 40, need=None):
+    return D.lib().densenet_block_product(a, as_, ak, w, ws, wk, n, C, V, y, ys, dt, work, size, need, None)
+
+
+def scores(x=P, xs=100, tok=P, n=4, V=100, dt=D.DN_BF16, scale=1.0, top=0, logp=P, H=P, lse=P, ids=None, best=None, work=P, size=1 << 40,
+           need=None):
+    return D.lib().densenet_token_scores(x, xs, tok, n, V, dt, scale, top, logp, H, lse, ids, best, work, size, need, None)
+
+
+def back(x=P, xs=100, tok=P, lse=P, H=P, dlogp=P, dH=None, dlse=None, ids=None, dtop=None, n=4, V=100, dt=D.DN_BF16, scale=1.0, top=0, dx=P,
+         dxs=100):
+    return D.lib().densenet_token_scores_backward(x, xs, tok, lse, H, dlogp, dH, dlse, ids, dtop, n, V, dt, scale, top, dx, dxs, None)
+
+
+def muon(rows=10, cols=20, rate=1.0, count=1, p=4096, g=4096, copy=None, m=4096, pdt=D.DN_F32, gdt=D.DN_F32, cdt=D.DN_BF16, params=True,
+         table=True, work=P, size=1 << 40, need=None, coef=(3.4445, -4.775, 2.0315), **kw):
+    t = (D.dn_muon_tensor * max(1, count))()
+    for e in t:
+        e.p, e.g, e.copy, e.m, e.rows, e.cols, e.rate = p, g, copy, m, rows, cols, rate
+    k = dict(lr=0.02, momentum=0.95, weight_decay=0.0, grad_scale=1.0, eps=1e-7)
+    steps = kw.pop("steps", 5)
+    parts = kw.pop("parts", 0)
+    k.update(kw)
+    q = D.dn_muon_params(*(k[f] for f in ("lr", "momentum", "weight_decay", "grad_scale", "eps")))
+    for c in q.coefficients:
+        c[:] = coef
+    q.steps, q.nesterov, q.parts = steps, 1, parts
+    return D.lib().densenet_muon(t if table else None, count, pdt, gdt, cdt, ctypes.byref(q) if params else None, work, size, need, None)
+
+
+@pytest.mark.parametrize("call,kw,status", [
+    (quant, dict(x=None), INV), (quant, dict(x=ODD), INV), (quant, dict(xs=63), INV), (quant, dict(qs=63), INV), (quant, dict(n=-1), INV),
+    (quant, dict(C=0), INV), (quant, dict(dt=3), UNS), (quant, dict(rows=64), UNS), (quant, dict(rows=0), UNS), (quant, dict(k=None), INV),
+    (quant, dict(q=None), INV), (quant, dict(q=None, k=None), INV), (quant, dict(t=P, ts=4), INV), (quant, dict(tk=P), INV),
+    (quant, dict(t=P, ts=3, tk=P), INV), (quant, dict(k=ODD), INV), (quant, dict(t=P, ts=4, tk=ODD), INV), (quant, dict(n=1 << 31), LARGE),
+    (quant, dict(n=1 << 30, C=1 << 10, xs=1 << 10, qs=1 << 10), LARGE), (quant, dict(xs=1 << 41), LARGE),
+    (product, dict(a=None), INV), (product, dict(w=None), INV), (product, dict(y=None), INV), (product, dict(ak=None), INV),
+    (product, dict(wk=None), INV), (product, dict(ak=ODD), INV), (product, dict(wk=ODD), INV), (product, dict(as_=63), INV),
+    (product, dict(ws=63), INV), (product, dict(ys=99), INV), (product, dict(y=ODD), INV), (product, dict(n=-1), INV), (product, dict(C=0), INV),
+    (product, dict(V=0), INV), (product, dict(dt=3), UNS), (product, dict(as_=60, size=8), INV), (product, dict(a=ODD, size=8), SMALL),
+    (product, dict(work=ctypes.c_void_p(4100)), INV), (product, dict(C=(1 << 20) + 1, as_=1 << 21, ws=1 << 21), LARGE),
+    (product, dict(n=1 << 31), LARGE), (product, dict(n=1 << 30, V=1 << 12, ys=1 << 12), LARGE),
+    (scores, dict(x=None), INV), (scores, dict(x=ODD), INV), (scores, dict(xs=99), INV), (scores, dict(tok=ODD), INV), (scores, dict(n=-1), INV),
+    (scores, dict(V=0), INV), (scores, dict(dt=3), UNS), (scores, dict(scale=0.0), INV), (scores, dict(scale=-1.0), INV),
+    (scores, dict(scale=NAN), INV), (scores, dict(scale=INF), INV), (scores, dict(top=-1), UNS), (scores, dict(top=65), UNS),
+    (scores, dict(top=3), INV), (scores, dict(top=3, ids=P), INV), (scores, dict(top=3, ids=ctypes.c_void_p(4100), best=P), INV),
+    (scores, dict(lse=None), INV), (scores, dict(lse=ODD), INV), (scores, dict(logp=ODD), INV), (scores, dict(size=8), SMALL),
+    (scores, dict(work=ctypes.c_void_p(4100)), INV), (scores, dict(n=1 << 31), LARGE), (scores, dict(V=(1 << 31) - 256, xs=1 << 31), LARGE),
+    (back, dict(x=None), INV), (back, dict(dx=None), INV), (back, dict(lse=None), INV), (back, dict(dxs=99), INV), (back, dict(dxs=101), INV),
+    (back, dict(dH=P, H=None), INV), (back, dict(tok=None), INV), (back, dict(top=2, dtop=P), INV), (back, dict(dlogp=ODD), INV),
+    (back, dict(top=2, dtop=P, ids=ODD), INV), (back, dict(scale=0.0), INV), (back, dict(top=70), UNS), (back, dict(dt=9), UNS),
+    (back, dict(dx=ODD), INV),
+    (muon, dict(params=False), INV), (muon, dict(table=False), INV), (muon, dict(count=-1), INV), (muon, dict(p=None), INV),
+    (muon, dict(g=None), INV), (muon, dict(m=None), INV), (muon, dict(p=4098), INV), (muon, dict(g=4097), INV), (muon, dict(m=4098), INV),
+    (muon, dict(copy=4097), INV), (muon, dict(rows=0), INV), (muon, dict(cols=-3), INV), (muon, dict(rows=1 << 23, cols=2), LARGE),
+    (muon, dict(rows=1 << 16, cols=1 << 16), LARGE), (muon, dict(pdt=3), UNS), (muon, dict(gdt=3), UNS), (muon, dict(cdt=0), UNS),
+    (muon, dict(steps=0), UNS), (muon, dict(steps=17), UNS), (muon, dict(parts=3), UNS), (muon, dict(parts=-1), UNS),
+    (muon, dict(momentum=1.0), INV), (muon, dict(momentum=-0.1), INV), (muon, dict(momentum=NAN), INV), (muon, dict(eps=0.0), INV),
+    (muon, dict(eps=1e-60), INV), (muon, dict(eps=INF), INV), (muon, dict(lr=NAN), INV), (muon, dict(grad_scale=INF), INV),
+    (muon, dict(weight_decay=NAN), INV), (muon, dict(rate=NAN), INV), (muon, dict(coef=(NAN, 0, 0)), INV), (muon, dict(coef=(1, 1, 65)), INV),
+    (muon, dict(size=8), SMALL), (muon, dict(work=ctypes.c_void_p(4100)), INV),
+])
+def test_refuses(call, kw, status):
+    assert call(**kw) == status
+    assert D.last_error()
+
+
+def test_nothing_to_do():
+    assert quant(n=0, x=None) == D.DN_OK and quant(n=0, x=None, q=None, k=None) == D.DN_OK
+    assert product(n=0, a=None, y=None, ak=None) == D.DN_OK
+    assert scores(n=0, x=None, tok=None, lse=None) == D.DN_OK
+    assert back(n=0, x=None, dx=None, lse=None) == D.DN_OK
+    assert muon(count=0) == D.DN_OK
+
+
+def test_size_queries():
+    need = ctypes.c_size_t(77)
+    q = dict(work=None, need=ctypes.byref(need))
+    # rows that start on 16 bytes are read as they lie; others are copied
+    big = dict(n=4096, C=1000, V=16384, ys=16384, **q)
+    assert product(as_=1008, ws=1008, **big) == D.DN_OK
+    plain = need.value
+    assert 0 < plain < 4096 * 1000
+    assert product(as_=1001, ws=1008, **big) == D.DN_OK and need.value >= plain + 4096 * 1000
+    assert product(as_=1008, ws=1008, w=ctypes.c_void_p(4104), **big) == D.DN_OK and need.value >= plain + 16384 * 1000
+    # sums in parts take no more than 1 GiB
+    for n, C, V in ((1, 1 << 20, 128), (4096, 1 << 20, 4096), (300, 1 << 16, 5000), ((1 << 31) - 256, 16, 32)):
+        assert product(n=n, C=C, V=V, as_=C, ws=C, ys=V, **q) == D.DN_OK and need.value <= (1 << 30) + 256
+    # a workspace is never empty, so that a caller's is never taken for a query
+    for call in (lambda: product(n=0, **q), lambda: scores(**q), lambda: scores(n=0, **q), lambda: muon(count=0, **q)):
+        need.value = 0
+        assert call() == D.DN_OK and need.value >= 256
+    assert scores(n=1, V=131072, xs=131072, top=20, ids=P, best=P, **q) == D.DN_OK and need.value < 1 << 16
+    assert scores(n=(1 << 31) - 256, V=40, xs=40, top=5, ids=P, best=P, **q) == D.DN_OK and need.value == 256
+    # Muon: two buffers of X, A and P in one or two fp16 parts, and partial sums
+    X = 1000 * 9216
+    assert muon(rows=1000, cols=9216, parts=1, **q) == D.DN_OK
+    one = need.value
+    assert muon(rows=1000, cols=9216, parts=2, **q) == D.DN_OK and need.value >= one + 2 * 2 * X
+    assert muon(rows=1000, cols=9216, pdt=D.DN_BF16, **q) == D.DN_OK and need.value == one
+    # matrices past one launch's share the workspace of a launch
+    assert muon(rows=100, cols=100, count=32, **q) == D.DN_OK
+    many = need.value
+    assert muon(rows=100, cols=100, count=320, **q) == D.DN_OK and need.value == many
+
+
+def test_binding_refuses():
+    torch = pytest.importorskip("torch")
+    x, f8 = torch.zeros(4, 64), torch.zeros(4, 64, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    i, one = torch.zeros(4, dtype=torch.int64), torch.ones(4, 1)
+    for call in (lambda: D.densenet_quantize_blocks(x), lambda: D.densenet_quantize_blocks(f8), lambda: D.densenet_quantize_blocks(x, rows=2),
+                 lambda: D.densenet_quantize_blocks(x, codes=False), lambda: D.densenet_block_product(f8, one, f8, one[:1]),
+                 lambda: D.densenet_block_product(x, one, x, one), lambda: D.densenet_token_scores(x, i),
+                 lambda: D.densenet_token_scores(x, i, top=65), lambda: D.densenet_token_scores_backward(x, i, one[:, 0], dlogp=one[:, 0]),
+                 lambda: D.MuonPlan([x], [x]), lambda: D.MuonPlan([], []), lambda: D.MuonPlan([x[0]], [x[0]]),
+                 lambda: D.MuonPlan([x], [x], parts=3)):
+        with pytest.raises(D.DenseNetError):
+            call()
