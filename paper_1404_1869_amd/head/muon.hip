@@ -389,6 +389,199 @@ __global__ __launch_bounds__(64 * Shape<T>::NW) void update_kernel(MuonLaunch l)
   });
 }
 
+// A small matrix's whole step by one workgroup, X and A in LDS (a tall one turned, so that rows are the smaller side): of the general
+// path's 17 launches each takes 8 us and more for next to no work (four matrices of 96 x 256 in fp32: 178 us, so 81).
+// X: [r32][c32 + 8] in parts, zeros past r and c; A, and P over it: [r32][r32 + 8].  Rows 16 bytes longer than a multiple of 64
+// spread over the banks.  Waves take 32 x 32 tiles of A and A A, and columns of 32 of P X, whose rows they replace.
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+constexpr int SMALL_WAVES = 16, SMALL_LDS = 159 * 1024;
+__host__ __device__ inline int up32(int x) { return (x + 31) / 32 * 32; }
+__host__ __device__ inline int64_t small_bytes(int64_t rows, int64_t cols, int parts) {
+  const int64_t r = (rows < cols ? rows : cols), c = rows < cols ? cols : rows;
+  if (r > 128 || c > 4096) return SMALL_LDS + 1;
+  return (int64_t)parts * 2 * up32((int)r) * (up32((int)c) + 8 + up32((int)r) + 8);
+}
+struct SmallMat {
+  const void* g;
+  float* m;
+  void *p, *copy;
+  int32_t rows, cols;
+  float rate;
+};
+constexpr int SMALL_MATS = 48;
+struct SmallLaunch {
+  SmallMat t[SMALL_MATS];
+  float beta, grad_scale, eps, lr, decay;
+  int32_t nesterov, steps;
+  float coef[DN_MAX_NS_STEPS][3];
+  int32_t poly_shift[DN_MAX_NS_STEPS];
+};
+template <int PARTS, typename P, typename G, typename O>
+__global__ __launch_bounds__(64 * SMALL_WAVES) void small_kernel(SmallLaunch l) {
+  extern __shared__ __align__(16) char s_mem[];
+  __shared__ float s_sum[SMALL_WAVES];
+  const SmallMat& t = l.t[blockIdx.x];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
+  const bool tall = t.rows > t.cols;
+  const int r = tall ? t.cols : t.rows, c = tall ? t.rows : t.cols, r32 = up32(r), c32 = up32(c), lx = c32 + 8, la = r32 + 8;
+  const int xpart = r32 * lx, apart = r32 * la;
+  _Float16 *X = (_Float16*)s_mem, *A = X + PARTS * xpart;
+  const int n = t.rows * t.cols;
+  const auto put = [&](_Float16* at, int part, float v) {
+    asm("" : "+v"(v));  // (see store_parts)
+    const _Float16 hi = (_Float16)v;
+    *at = hi;
+    if constexpr (PARTS == 2) at[part] = (_Float16)(v - (float)hi);
+  };
+  const auto get = [&](const _Float16* at, int part) { return PARTS == 2 ? (float)at[0] + (float)at[part] : (float)at[0]; };
+  // u of eight values at a time, whose loads go out together; `first`: momentum makes its step
+  constexpr int STEP = 64 * SMALL_WAVES;
+  const auto updates = [&](int i0, bool first, float (&u)[8]) {
+    float m[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = min(i0 + j * STEP, n - 1);
+      u[j] = (float)((const G*)t.g)[i] * l.grad_scale, m[j] = t.m ? t.m[i] : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (first) m[j] = __builtin_fmaf(l.beta, m[j], u[j]);
+      if (first && t.m && i0 + j * STEP < n) t.m[i0 + j * STEP] = m[j];
+      if (t.m) u[j] = l.nesterov ? __builtin_fmaf(l.beta, m[j], u[j]) : m[j];
+    }
+  };
+  float ss = 0.f;
+  for (int i = threadIdx.x; i < n; i += 8 * STEP) {
+    float u[8];
+    updates(i, true, u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss += i + j * STEP < n ? u[j] * u[j] : 0.f;
+  }
+  ss = lanes_sum<64>(ss);
+  if (lane == 0) s_sum[wave] = ss;
+  for (int i = threadIdx.x; i < PARTS * xpart / 8; i += 64 * SMALL_WAVES) *(f32x4*)(X + 8 * i) = f32x4{};
+  __syncthreads();
+  ss = 0.f;
+  for (int w = 0; w < SMALL_WAVES; ++w) ss += s_sum[w];
+  const float mul = ldexpf(1.f / (sqrtf(ss) + l.eps), XS);
+  for (int i0 = threadIdx.x; i0 < n; i0 += 8 * STEP) {  // (a thread reads the momentum that it wrote)
+    float u[8];
+    updates(i0, false, u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = i0 + j * STEP, row = i / t.cols, col = i - row * t.cols;
+      if (i < n) put(X + (tall ? col * lx + row : row * lx + col), xpart, u[j] * mul);
+    }
+  }
+  __syncthreads();
+  const int tiles = r32 / 32;
+  const int ways = c32 / 32 * tiles <= SMALL_WAVES ? tiles : tiles > 1 && c32 / 32 * 2 <= SMALL_WAVES ? 2 : 1;  // waves to 32 columns of X
+  const int each = (tiles + ways - 1) / ways;
+  // a tile's products of k from rows of p (rows from i0) and of q (from j0): D[i][j]
+  const auto rows_product = [&](const _Float16* p, int ld, int part, int i0, int j0, int k, f32x16& acc) {
+#pragma unroll
+    for (int pr = PARTS == 2 ? 0 : 2; pr < 3; ++pr) {  // parts (1, 0), (0, 1), (0, 0)
+      const _Float16* a = p + (pr == 0 ? part : 0) + (i0 + l32) * ld + 8 * half;
+      const _Float16* b = p + (pr == 1 ? part : 0) + (j0 + l32) * ld + 8 * half;
+#pragma unroll 4
+      for (int k0 = 0; k0 < k; k0 += 16) acc = Mfma<_Float16>::mma(*(const f16x8*)(a + k0), *(const f16x8*)(b + k0), acc);
+    }
+  };
+  for (int s = 0; s < l.steps; ++s) {
+    // A = X X', all tiles (the mirrored ones too: there are waves to spare)
+    for (int id = wave; id < tiles * tiles; id += SMALL_WAVES) {
+      const int i0 = id / tiles * 32, j0 = id % tiles * 32;
+      f32x16 acc{};
+      rows_product(X, lx, xpart, i0, j0, c32, acc);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) put(A + (i0 + 8 * (e / 4) + 4 * half + e % 4) * la + j0 + l32, apart, ldexpf(acc[e], -XS));
+    }
+    __syncthreads();
+    // P = b A + c A A, over A once all waves have read it (16 waves: a tile each)
+    f32x16 square{};
+    const int i0 = wave / tiles * 32, j0 = wave % tiles * 32;
+    const bool is = wave < tiles * tiles;
+    if (is) rows_product(A, la, apart, i0, j0, r32, square);
+    __syncthreads();
+    if (is) {
+      const float fa = ldexpf(l.coef[s][1], l.poly_shift[s] - XS), fs = ldexpf(l.coef[s][2], l.poly_shift[s] - 2 * XS);
+      const auto place = [&](int e) { return A + (i0 + 8 * (e / 4) + 4 * half + e % 4) * la + j0 + l32; };
+#pragma unroll
+      for (int e = 0; e < 16; ++e) square[e] = __builtin_fmaf(fa, get(place(e), apart), fs * square[e]);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) put(place(e), apart, square[e]);
+    }
+    __syncthreads();
+    // X = a X + P X: `each` blocks of 32 rows of 32 columns a wave, D[m][n] = sum_k X[k][m] P[n][k]
+    const float unscale = ldexpf(1.f, -l.poly_shift[s]);
+    for (int first = 0; first < c32; first += SMALL_WAVES / ways * 32) {
+      const int m0 = first + wave / ways * 32, b0 = wave % ways * each, count = m0 < c32 ? min(each, tiles - b0) : 0;
+      f32x16 acc[4];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) acc[b] = f32x16{};
+#pragma unroll
+      for (int pr = PARTS == 2 ? 0 : 2; pr < 3; ++pr) {
+        const _Float16* x = X + (pr == 0 ? xpart : 0) + m0;
+        const _Float16* q = A + (pr == 1 ? apart : 0);
+        if (count <= 0) continue;
+#pragma unroll 2
+        for (int k0 = 0; k0 < r32; k0 += 16) {
+          f16x8 a;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) a[j] = x[(k0 + 8 * half + j) * lx + l32];
+#pragma unroll
+          for (int b = 0; b < 4; ++b)
+            if (b < count) acc[b] = Mfma<_Float16>::mma(a, *(const f16x8*)(q + (32 * (b0 + b) + l32) * la + k0 + 8 * half), acc[b]);
+        }
+      }
+      if (ways > 1) __syncthreads();  // other waves read these columns too
+      // element e of acc[b]: column m0 + 8 (e / 4) + 4 half + e % 4 of row 32 (b0 + b) + l32
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        if (b >= count) continue;
+        const int row = 32 * (b0 + b) + l32, col0 = m0 + 4 * half;
+        _Float16* mine = X + row * lx + col0;
+        // (all of X's old values before the first is written)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          const f16x4 hi = *(const f16x4*)(mine + 2 * e), lo = PARTS == 2 ? *(const f16x4*)(mine + xpart + 2 * e) : f16x4{};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            acc[b][e + j] = __builtin_fmaf(l.coef[s][0], (float)hi[j] + (float)lo[j], acc[b][e + j] * unscale);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          f16x4 hi, lo;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float v = acc[b][e + j];
+            asm("" : "+v"(v));
+            hi[j] = (_Float16)v, lo[j] = (_Float16)(v - (float)hi[j]);
+          }
+          *(f16x4*)(mine + 2 * e) = hi;
+          if constexpr (PARTS == 2) *(f16x4*)(mine + xpart + 2 * e) = lo;
+        }
+      }
+    }
+    __syncthreads();
+  }
+  // the weights, in their own order (from the accumulators, each lane with values of its own row, this took 29 us more)
+  const float rate = ldexpf(l.lr * t.rate, -XS);
+  for (int i0 = threadIdx.x; i0 < n; i0 += 8 * STEP) {
+    float w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = (float)((const P*)t.p)[min(i0 + j * STEP, n - 1)];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = i0 + j * STEP, row = i / t.cols, col = i - row * t.cols;
+      if (i >= n) continue;
+      w[j] = __builtin_fmaf(-rate, get(X + (tall ? col * lx + row : row * lx + col), xpart), w[j] * l.decay);
+      ((P*)t.p)[i] = (P)w[j];
+      if (t.copy) ((O*)t.copy)[i] = (O)w[j];
+    }
+  }
+}
+
 template <typename F>
 int with_type(dn_dtype dt, F&& f) {
   if (dt == DN_F32) return f(float{});
@@ -404,6 +597,12 @@ struct Work {  // offsets in the workspace, 256-byte aligned
     return at;
   }
 };
+
+int poly_shift_of(const double* c) {
+  // |P| <= |b| |A| + |c| |A|^2, which is at most 2.25 |c| + 1.5 |b| for singular values up to 1.22, and twice that to spare
+  const double most = 2 * (1.5 * std::fabs(c[1]) + 2.25 * std::fabs(c[2]));
+  return std::min(XS, (int)std::floor(std::log2(65504 / std::max(most, 1e-6))));
+}
 
 int parts_of(const dn_muon_params& k, dn_dtype p_dt) { return k.parts ? k.parts : p_dt == DN_BF16 ? 1 : 2; }
 int64_t half_tiles(int64_t r, int64_t side) {
@@ -536,9 +735,7 @@ int run_group(Group& gr, const dn_muon_params& k, dn_dtype p_dt, dn_dtype g_dt, 
   });
   for (int s = 0; s < k.steps && !err; ++s) {
     l.a = (float)k.coefficients[s][0], l.b = (float)k.coefficients[s][1], l.c = (float)k.coefficients[s][2];
-    // |P| <= |b| |A| + |c| |A|^2, which is at most 2.25 |c| + 1.5 |b| for singular values up to 1.22, and twice that to spare
-    const double most = 2 * (1.5 * std::fabs(k.coefficients[s][1]) + 2.25 * std::fabs(k.coefficients[s][2]));
-    l.poly_shift = std::min(XS, (int)std::floor(std::log2(65504 / std::max(most, 1e-6))));
+    l.poly_shift = poly_shift_of(k.coefficients[s]);
     l.from = s & 1;
     if ((err = run_gram<false, PARTS>(l, gr.gram, st)) || (err = run_gram<true, PARTS>(l, gr.square, st))) return err;
     err = s + 1 < k.steps ? run_update<PARTS, false, float, __bf16>(l, gr.update, st) : with_type(p_dt, [&](auto p) {
@@ -549,31 +746,84 @@ int run_group(Group& gr, const dn_muon_params& k, dn_dtype p_dt, dn_dtype g_dt, 
   return err;
 }
 
+// Whether a matrix is a workgroup's own.
+bool is_small(const dn_muon_tensor& t, int parts) { return small_bytes(t.rows, t.cols, parts) <= SMALL_LDS; }
+
+template <int PARTS>
+int run_small(const dn_muon_tensor* const* ts, int count, const dn_muon_params& k, dn_dtype p_dt, dn_dtype g_dt, dn_dtype copy_dt,
+              hipStream_t st) {
+  SmallLaunch l{};
+  l.beta = (float)k.momentum, l.grad_scale = (float)k.grad_scale, l.eps = (float)k.eps, l.lr = (float)k.lr;
+  l.decay = (float)(1 - k.lr * k.weight_decay), l.nesterov = k.nesterov, l.steps = k.steps;
+  for (int s = 0; s < k.steps; ++s) {
+    for (int j = 0; j < 3; ++j) l.coef[s][j] = (float)k.coefficients[s][j];
+    l.poly_shift[s] = poly_shift_of(k.coefficients[s]);
+  }
+  int64_t bytes = 0;
+  for (int i = 0; i < count; ++i) {
+    const dn_muon_tensor& t = *ts[i];
+    l.t[i] = SmallMat{t.g, t.m, t.p, t.copy, (int32_t)t.rows, (int32_t)t.cols, (float)t.rate};
+    bytes = std::max(bytes, small_bytes(t.rows, t.cols, PARTS));
+  }
+  return with_type(p_dt, [&](auto p) {
+    return with_type(g_dt, [&](auto g) {
+      const auto go = [&](auto o) {
+        const auto kernel = small_kernel<PARTS, decltype(p), decltype(g), decltype(o)>;
+        // (more than 64 KB has to be asked for, each time: which device this is may change)
+        if (const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, SMALL_LDS)) return (int)e;
+        kernel<<<dim3((unsigned)count), 64 * SMALL_WAVES, (size_t)bytes, st>>>(l);
+        return (int)hipGetLastError();
+      };
+      return copy_dt == DN_F16 ? go(_Float16{}) : go(__bf16{});
+    });
+  });
+}
+
 }  // namespace
 
 size_t muon_bytes(const dn_muon_tensor* tensors, int32_t count, dn_dtype p_dt, const dn_muon_params& k) {
   size_t most = 256;
   Group gr;
-  for (int32_t at = 0; at < count; at += MATS) {
-    plan_group(tensors + at, std::min(count - at, MATS), parts_of(k, p_dt), gr);
-    most = std::max(most, gr.total);
+  const int parts = parts_of(k, p_dt);
+  dn_muon_tensor large[MATS];
+  int held = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    if (!is_small(tensors[i], parts)) large[held++] = tensors[i];
+    if (held == MATS || (i + 1 == count && held)) {
+      plan_group(large, held, parts, gr);
+      most = std::max(most, gr.total), held = 0;
+    }
   }
   return most;
 }
 
 int launch_muon(const dn_muon_tensor* tensors, int32_t count, dn_dtype p_dt, dn_dtype g_dt, dn_dtype copy_dt, const dn_muon_params& k,
                 void* d_work, void* stream) {
-  for (int32_t at = 0; at < count; at += MATS) {  // groups share the workspace: the stream keeps them apart
-    Group gr;
-    const int parts = parts_of(k, p_dt);
-    plan_group(tensors + at, std::min(count - at, MATS), parts, gr);
-    gr.l.work = (char*)d_work;
-    gr.l.sums = (float*)((char*)d_work + (size_t)gr.l.sums);
-    gr.l.beta = (float)k.momentum, gr.l.grad_scale = (float)k.grad_scale, gr.l.eps = (float)k.eps, gr.l.lr = (float)k.lr;
-    gr.l.decay = (float)(1 - k.lr * k.weight_decay), gr.l.nesterov = k.nesterov;
-    const int err = parts == 2 ? run_group<2>(gr, k, p_dt, g_dt, copy_dt, (hipStream_t)stream)
-                               : run_group<1>(gr, k, p_dt, g_dt, copy_dt, (hipStream_t)stream);
-    if (err) return err;
+  const int parts = parts_of(k, p_dt);
+  const hipStream_t st = (hipStream_t)stream;
+  const dn_muon_tensor* small[SMALL_MATS];
+  dn_muon_tensor large[MATS];
+  int n_small = 0, n_large = 0;
+  for (int32_t i = 0; i < count; ++i) {  // groups share the workspace: the stream keeps them apart
+    if (is_small(tensors[i], parts)) small[n_small++] = &tensors[i];
+    else large[n_large++] = tensors[i];
+    const bool end = i + 1 == count;
+    if (n_small == SMALL_MATS || (end && n_small)) {
+      const int err = parts == 2 ? run_small<2>(small, n_small, k, p_dt, g_dt, copy_dt, st) : run_small<1>(small, n_small, k, p_dt, g_dt, copy_dt, st);
+      if (err) return err;
+      n_small = 0;
+    }
+    if (n_large == MATS || (end && n_large)) {
+      Group gr;
+      plan_group(large, n_large, parts, gr);
+      gr.l.work = (char*)d_work;
+      gr.l.sums = (float*)((char*)d_work + (size_t)gr.l.sums);
+      gr.l.beta = (float)k.momentum, gr.l.grad_scale = (float)k.grad_scale, gr.l.eps = (float)k.eps, gr.l.lr = (float)k.lr;
+      gr.l.decay = (float)(1 - k.lr * k.weight_decay), gr.l.nesterov = k.nesterov;
+      const int err = parts == 2 ? run_group<2>(gr, k, p_dt, g_dt, copy_dt, st) : run_group<1>(gr, k, p_dt, g_dt, copy_dt, st);
+      if (err) return err;
+      n_large = 0;
+    }
   }
   return 0;
 }

@@ -448,6 +448,8 @@ MUON = [  # shapes, p type, g type, copy type, nesterov, momentum state, steps
     ([(64, 64), (128, 200), (200, 128)], "f32", "bf16", "bf16", True, True, 1), ([(1, 300), (300, 1)], "f32", "f32", "f16", True, True, 2),
     ([(129, 257), (257, 129), (130, 130)], "bf16", "bf16", None, True, True, 1), ([(33, 1000)], "f16", "f16", None, True, False, 1),
     ([(150, 1030), (1030, 150)], "f32", "f16", "bf16", True, True, 2),
+    ([(128, 160), (161, 127), (16, 2000), (3000, 2)], "f32", "bf16", "f16", True, True, 2),  # some of a workgroup each, some not
+    ([(128, 400), (401, 128), (31, 33), (1, 4097)], "bf16", "bf16", None, False, True, 1),
 ]
 
 
@@ -482,7 +484,7 @@ def test_muon_orthogonalises(D, pt):
     """Five steps bring all singular values above 1e-2 of the largest to between 0.68 and 1.21 (by the polynomial's own course), from
     updates as training has them: few strong directions over noise.  The result is that of 64 bits, to the roundings' size."""
     g = gen(77)
-    shapes = [(200, 700), (700, 200), (256, 256)]
+    shapes = [(200, 700), (700, 200), (256, 256), (96, 200), (200, 96)]
     ups = []
     for a, b in shapes:
         u = torch.linalg.qr(torch.randn(a, min(a, b), generator=g, device="cuda", dtype=torch.float64))[0]
@@ -491,7 +493,7 @@ def test_muon_orthogonalises(D, pt):
         ups.append((u * s) @ v.T)
     p = [torch.zeros(s, dtype=DT[pt], device="cuda") for s in shapes]
     gr = [u.float() for u in ups]
-    plan = D.MuonPlan(p, gr, rates=[1.0] * 3)
+    plan = D.MuonPlan(p, gr, rates=[1.0] * 5)
     D.densenet_muon(plan, lr=1.0, momentum=0.0)
     for q, u in zip(p, gr):
         want = plain_muon(torch.zeros_like(q), u, None, 1.0, 0.0, True, 0.0, 5, [NS] * 5, 1e-7, 1.0, 1.0, 0.0)[0]

@@ -124,6 +124,28 @@ def test_step_in_a_graph(D):
         assert torch.equal(plans[0].params[0], plans[1].params[0]) and torch.equal(plans[0].momentum[0], plans[1].momentum[0])
 
 
+def test_muon_in_a_graph(D):
+    """Small matrices (a workgroup each) and larger ones, captured and replayed with other work between."""
+    g = gen(12)
+    shapes = [(96, 256), (300, 400), (5, 9), (700, 130)]
+    make = lambda: [torch.randn(s, generator=gen(13), device="cuda") for s in shapes]  # noqa: E731
+    grads = [torch.randn(s, generator=g, device="cuda").bfloat16() for s in shapes]
+    a, b = D.MuonPlan(make(), grads), D.MuonPlan(make(), grads)
+    D.densenet_muon(D.MuonPlan(make(), grads), lr=0.01)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        D.densenet_muon(a, lr=0.01, weight_decay=0.1)
+    for _ in range(4):
+        for t in grads:
+            t.normal_(generator=g)
+        graph.replay()
+        D.densenet_muon(b, lr=0.01, weight_decay=0.1)
+        torch.cuda.synchronize()
+        for x, y in zip(a.params + a.momentum, b.params + b.momentum):
+            assert torch.equal(x, y)
+
+
 def test_two_streams_and_two_graphs(D):
     """Two streams at once, and two graphs replayed at once, give what each gives alone: no memory is shared but the caller's."""
     sets = [inputs(20, 150, 300, 700), inputs(21, 33, 1000, 5000)]
