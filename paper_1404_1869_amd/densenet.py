@@ -8,6 +8,7 @@ On top of the raw entry points, ``convnet_featpyramid`` mirrors the paper's inte
 """
 from __future__ import annotations
 
+import bisect
 import ctypes
 import functools
 import os
@@ -861,8 +862,12 @@ class AdamWPlan:
         elif m_scale is not None or v_scale is not None:
             raise _bad("scales belong to 8-bit states")
         self.p_dtype = _code(self.params[0], "params")
+        self.copies = [None if c is not None and (c.data_ptr(), c.dtype, c.shape, c.stride()) == (p.data_ptr(), p.dtype, p.shape, p.stride())
+                       else c for c, p in zip(self.copies, self.params)]
         given = [c for c in self.copies if c is not None]
         self.copy_dtype = _code(given[0], "copies") if given else DN_BF16
+        if self.copy_dtype not in (DN_F16, DN_BF16):
+            raise DenseNetError(DN_E_UNSUPPORTED, "copies: bf16 or fp16")
         self.table = (dn_adamw_tensor * len(self.params))()
         for e, p, c, b in zip(self.table, self.params, self.copies, self.blocks):
             self._fits(p, "params", p, self.params[0])
@@ -1056,8 +1061,11 @@ def densenet_token_scores_backward(logits, tokens, lse, entropy=None, dlogp=None
 
 class MuonPlan:
     """Matrices that step together by Muon: parameters (one type, updated in place), their gradients' buffers (one type), momentum
-    (fp32, made as zeros if not given), 16-bit copies of the parameters (optional; None entries allowed), and a rate for each that
-    multiplies the learning rate (by default 0.2 sqrt(max(rows, cols)), which gives updates of AdamW's size).  parts: fp16 parts of a value in the products (0: 1 for bf16 parameters, else 2)."""
+    (fp32, made as zeros if not given), 16-bit copies of the parameters (optional; None entries allowed, and so is a parameter that
+    is its own copy, as `p.to(torch.bfloat16)` gives of a bf16 one: nothing else is written for it), and a rate for each that
+    multiplies the learning rate (by default 0.2 sqrt(max(rows, cols)), which gives updates of AdamW's size).  parts: fp16 parts of
+    a value in the products (0: 1 for bf16 parameters, else 2).  Nothing that is stepped may meet another tensor of the plan in
+    memory."""
 
     def __init__(self, params, grads, momentum=None, copies=None, rates=None, parts=0):
         torch = _torch()
@@ -1069,8 +1077,12 @@ class MuonPlan:
             raise DenseNetError(DN_E_UNSUPPORTED, "parts: 0, 1 or 2")
         self.device = self.params[0].device
         self.p_dtype = _code(self.params[0], "params")
+        self.copies = [None if c is not None and (c.data_ptr(), c.dtype, c.shape, c.stride()) == (p.data_ptr(), p.dtype, p.shape, p.stride())
+                       else c for c, p in zip(self.copies, self.params)]
         given = [c for c in self.copies if c is not None]
         self.copy_dtype = _code(given[0], "copies") if given else DN_BF16
+        if self.copy_dtype not in (DN_F16, DN_BF16):
+            raise DenseNetError(DN_E_UNSUPPORTED, "copies: bf16 or fp16")
         if momentum is None:
             momentum = [torch.zeros(p.shape, dtype=torch.float32, device=self.device) for p in self.params]
         self.momentum = list(momentum)
@@ -1087,8 +1099,8 @@ class MuonPlan:
                 self._fits(c, "copies", p, given[0].dtype)
             e.p, e.copy, e.m = p.data_ptr(), None if c is None else c.data_ptr(), m.data_ptr()
             e.rows, e.cols, e.rate = p.shape[0], p.shape[1], rate
-        held = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in self.params + self.momentum + given)
-        if any(a + size > b for (a, size), (b, _) in zip(held, held[1:])):
+        self._held = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self.params + self.momentum + given)
+        if any(end > at for (_, end), (at, _) in zip(self._held, self._held[1:])):
             raise _bad("two of the tensors that are stepped meet in memory")
         self.set_grads(grads)
 
@@ -1103,6 +1115,9 @@ class MuonPlan:
             raise _bad("as many gradients as parameters expected")
         for g, p in zip(grads, self.params):
             self._fits(g, "grads", p, grads[0].dtype)
+            at = bisect.bisect_left(self._held, (g.data_ptr() + g.numel() * g.element_size(), 0))
+            if at and self._held[at - 1][1] > g.data_ptr():
+                raise _bad("a gradient meets a tensor that is stepped in memory")
         self.grads, self.g_dtype = grads, _code(grads[0], "grads")
         for e, g in zip(self.table, grads):
             e.g = g.data_ptr()

@@ -534,3 +534,23 @@ def test_muon_many_matrices_step_as_each_alone(D):
         D.densenet_muon(D.MuonPlan([a], [gr[i]]), lr=0.1)
         # the sums may be split in another way: 22 bits of an update of size 0.2 sqrt(max)
         within(a, p[i], 0.1 * 0.2 * max(s) ** 0.5 * 41 * 5 * 2.0 ** -20 + 4 * E24 * start.double().abs(), f"matrix {i}")
+
+
+def test_muon_plan_memory(D):
+    """A bf16 parameter is its own copy; what is stepped meets neither another stepped tensor nor a gradient."""
+    g = gen(41)
+    mem = torch.zeros(4, 64, 96, device="cuda")
+    mem[0], mem[1] = torch.randn(64, 96, generator=g, device="cuda"), torch.randn(64, 96, generator=g, device="cuda")
+    p = mem[0].bfloat16()
+    alone = p.clone()
+    D.densenet_muon(D.MuonPlan([p], [mem[1]], copies=[p.to(torch.bfloat16)]), lr=0.1)
+    D.densenet_muon(D.MuonPlan([alone], [mem[1]]), lr=0.1)
+    assert torch.equal(p, alone)
+    over = mem.view(-1)[32 * 96:].narrow(0, 0, 64 * 96).view(64, 96)  # half of each of the first two
+    for plan in (lambda: D.MuonPlan([mem[0], over], [mem[3]] * 2), lambda: D.MuonPlan([mem[0]], [mem[2]], momentum=[over]),
+                 lambda: D.MuonPlan([mem[0]], [over]), lambda: D.MuonPlan([over], [mem[1]]), lambda: D.MuonPlan([mem[0]], [mem[0]]),
+                 lambda: D.MuonPlan([mem[0]], [mem[1]], momentum=[mem[1]]),
+                 lambda: D.MuonPlan([mem[0].half()], [mem[1]], copies=[mem[0]])):
+        with pytest.raises(D.DenseNetError):
+            plan()
+    D.MuonPlan([mem[0], mem[2]], [mem[1], mem[1]])  # one gradient for two is fine
