@@ -458,8 +458,8 @@ int densenet_token_scores(const void* d_logits, int64_t stride, const int64_t* d
  *   dl_v = scale (p_v (dlse - dlogp - sum_j dtop_j - dentropy (log p_v + entropy)) + dlogp [v = token] + sum_j dtop_j [v = id_j])
  * d_dlogp, d_dentropy, d_dlse: fp32 [n], d_dtop: fp32 [n][top], each NULL for 0; d_entropy is needed with d_dentropy, d_top_id with
  * d_dtop, d_token with d_dlogp.  A token or id outside [0, V) has no gradient; an id may be there more than once, or be the token.
- * A row of which nothing is asked (all its gradients 0) gets zeros, whatever it holds, and so does a row of -infinity alone.  d_dlogits: `dtype`; it may be the logits'
- * own memory (same stride). */
+ * A row of which nothing is asked (all its gradients 0) gets zeros, whatever it holds, and so does a row of -infinity alone.
+ * d_dlogits: `dtype`; it may be the logits' own memory (same stride). */
 int densenet_token_scores_backward(const void* d_logits, int64_t stride, const int64_t* d_token,
                                    const float* d_lse, const float* d_entropy, const float* d_dlogp,
                                    const float* d_dentropy, const float* d_dlse, const int64_t* d_top_id,
@@ -472,11 +472,11 @@ int densenet_token_scores_backward(const void* d_logits, int64_t stride, const i
  *   p = p (1 - lr weight_decay) - lr rate X
  * p, g: contiguous [rows][cols] of p_dtype and g_dtype; copy (or NULL): the new p in copy_dtype (DN_F16 or DN_BF16); m: fp32
  * [rows][cols], or NULL with momentum 0.  No two tensors of a call may meet in memory.  |u| is taken in fp32: squares have to be in
- * its range.
+ * its range.  eps: 1e-30 at least.
  * steps: 1 .. DN_MAX_NS_STEPS; step s takes coefficients[s] = (a, b, c), which have to keep the singular values of X below 4 and
  * those of b A + c A^2 below 2 (1.5 |b| + 2.25 |c|), as the usual ones (3.4445, -4.775, 2.0315) do.
  * parts: fp16 parts of a value in the products, 1 (11 bits) or 2 (22 bits); 0: 1 for DN_BF16 weights, 2 for others.
- * d_workspace: NULL for a size query into *bytes_needed.  Limits (DN_E_TOO_LARGE): rows, cols <= 2^22, the smaller <= 2^15. */
+ * d_workspace: NULL for a size query into *bytes_needed.  Limits (DN_E_TOO_LARGE): rows, cols <= 2^21, the smaller <= 2^15. */
 #define DN_MAX_NS_STEPS 16
 typedef struct {
   void* p;

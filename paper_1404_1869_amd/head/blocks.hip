@@ -230,6 +230,7 @@ struct Codes {
           if (k + e < K) v[e / 4] |= (uint32_t)p[e] << (8 * (e % 4));
         *(u32x4*)(lds + (wave + i * NW) * 1024 + lane * 16) = v;
       }
+      wait_lds();  // (stores, which the waits for loads before the next barrier do not cover)
     }
   }
 };

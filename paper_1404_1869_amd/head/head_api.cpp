@@ -365,7 +365,8 @@ int densenet_muon(const dn_muon_tensor* tensors, int32_t count, dn_dtype p_dtype
     if (k.steps < 1 || k.steps > DN_MAX_NS_STEPS) return fail(DN_E_UNSUPPORTED, "steps must be 1 .. DN_MAX_NS_STEPS");
     if (k.parts < 0 || k.parts > 2) return fail(DN_E_UNSUPPORTED, "parts must be 0, 1 or 2");
     if (!(k.momentum >= 0 && k.momentum < 1)) return fail(DN_E_INVALID_ARG, "momentum must be in [0, 1)");
-    if (!((float)k.eps > 0) || !std::isfinite(k.eps)) return fail(DN_E_INVALID_ARG, "eps must be positive in fp32");
+    // (2^13 / eps, which an update of zeros is multiplied by, has to be finite)
+    if (!(k.eps >= 1e-30) || !std::isfinite((float)k.eps)) return fail(DN_E_INVALID_ARG, "eps must be 1e-30 or more, and finite in fp32");
     if (!std::isfinite(k.lr) || !std::isfinite(k.weight_decay) || !std::isfinite(k.grad_scale))
       return fail(DN_E_INVALID_ARG, "parameters must be finite");
     for (int32_t s = 0; s < k.steps; ++s) {
@@ -377,7 +378,8 @@ int densenet_muon(const dn_muon_tensor* tensors, int32_t count, dn_dtype p_dtype
     for (int32_t i = 0; i < count; ++i) {
       const dn_muon_tensor& t = tensors[i];
       if (t.rows <= 0 || t.cols <= 0) return fail(DN_E_INVALID_ARG, "a matrix's rows and cols must be positive");
-      if (t.rows > (1 << 22) || t.cols > (1 << 22) || std::min(t.rows, t.cols) > (1 << 15))
+      // (256 rows of the larger side in fp16 are within the 31 bits of a buffer's offsets)
+      if (t.rows > (1 << 21) || t.cols > (1 << 21) || std::min(t.rows, t.cols) > (1 << 15))
         return fail(DN_E_TOO_LARGE, "a matrix's rows or cols");
       if (!std::isfinite(t.rate)) return fail(DN_E_INVALID_ARG, "a matrix's rate must be finite");
       // (more workgroups than any launch has for it: pieces of 2048 values, and twice the tiles of 64 x 64 of its smaller side)

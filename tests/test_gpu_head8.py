@@ -554,3 +554,10 @@ def test_muon_plan_memory(D):
         with pytest.raises(D.DenseNetError):
             plan()
     D.MuonPlan([mem[0], mem[2]], [mem[1], mem[1]])  # one gradient for two is fine
+
+
+def test_muon_of_zeros_with_the_smallest_eps(D):
+    for shape in ((40, 50), (300, 500)):
+        p = torch.ones(shape, device="cuda")
+        D.densenet_muon(D.MuonPlan([p], [torch.zeros(shape, device="cuda")]), lr=0.1, eps=1e-30)
+        assert bool((p == 1).all())

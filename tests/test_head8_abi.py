@@ -76,7 +76,8 @@ def muon(rows=10, cols=20, rate=1.0, count=1, p=4096, g=4096, copy=None, m=4096,
     (muon, dict(momentum=1.0), INV), (muon, dict(momentum=-0.1), INV), (muon, dict(momentum=NAN), INV), (muon, dict(eps=0.0), INV),
     (muon, dict(eps=1e-60), INV), (muon, dict(eps=INF), INV), (muon, dict(lr=NAN), INV), (muon, dict(grad_scale=INF), INV),
     (muon, dict(weight_decay=NAN), INV), (muon, dict(rate=NAN), INV), (muon, dict(coef=(NAN, 0, 0)), INV), (muon, dict(coef=(1, 1, 65)), INV),
-    (muon, dict(size=8), SMALL), (muon, dict(work=ctypes.c_void_p(4100)), INV),
+    (muon, dict(size=8), SMALL), (muon, dict(work=ctypes.c_void_p(4100)), INV), (muon, dict(eps=1e-31), INV), (muon, dict(eps=1e40), INV),
+    (muon, dict(rows=300, cols=(1 << 21) + 1), LARGE),
 ])
 def test_refuses(call, kw, status):
     assert call(**kw) == status
