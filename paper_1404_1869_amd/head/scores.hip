@@ -216,6 +216,25 @@ __device__ inline Stats scan(const T* row, int64_t first, int64_t step, int end,
   return z;
 }
 
+// The first `top` of four waves' sorted keys, in order; their number.  s_count is written, a barrier before.
+__device__ inline int best_of(const Key (*s_keys)[CAP], const int* s_count, const Candidates& cand, Key* s_best) {
+  const int lane = threadIdx.x & 63;
+  int count = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) count += s_count[w];
+  if (lane < cand.count) {
+    const Key mine = cand.buf[lane];
+    int rank = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll 8
+      for (int j = 0; j < s_count[w]; ++j) rank += s_keys[w][j] > mine;
+    if (rank < cand.top) s_best[rank] = mine;
+  }
+  __syncthreads();
+  return min(count, cand.top);
+}
+
 // A workgroup of a split row leaves its statistics, and behind all rows' statistics `top` sorted keys (0: none).
 __device__ inline Key* part_keys(const ScoresArgs& a, int64_t row) {
   return (Key*)((Stats*)a.work + (a.n * a.parts + 1) / 2 * 2) + row * a.parts * a.top;
@@ -253,21 +272,7 @@ __global__ __launch_bounds__(256) void scores_kernel(ScoresArgs a) {
   if (lane == 0) s_stats[wave] = z, s_count[wave] = cand.count;
   __syncthreads();
   int count = 0;
-  if constexpr (TOP) {  // ranks among all waves' keys
-#pragma unroll
-    for (int w = 0; w < 4; ++w) count += s_count[w];
-    if (lane < cand.count) {
-      const Key mine = cand.buf[lane];
-      int rank = 0;
-#pragma unroll
-      for (int w = 0; w < 4; ++w)
-#pragma unroll 8
-        for (int j = 0; j < s_count[w]; ++j) rank += s_keys[w][j] > mine;
-      if (rank < a.top) s_best[rank] = mine;
-    }
-    count = min(count, a.top);
-    __syncthreads();
-  }
+  if constexpr (TOP) count = best_of(s_keys, s_count, cand, s_best);
   if (wave) return;
 #pragma unroll
   for (int w = 1; w < 4; ++w) z = join(z, s_stats[w], c);
@@ -279,34 +284,41 @@ __global__ __launch_bounds__(256) void scores_kernel(ScoresArgs a) {
   }
 }
 
-// Joins the parts of a row; one wave per row.
+// Joins the parts of a row: a workgroup per row, whose waves rank a quarter of the keys each (one wave with all of them took 10.5 us
+// for 16 parts with 20 alternatives).
 template <typename T>
-__global__ __launch_bounds__(64) void join_scores_kernel(ScoresArgs a) {
-  __shared__ Key s_keys[CAP];
-  const int lane = threadIdx.x;
+__global__ __launch_bounds__(256) void join_scores_kernel(ScoresArgs a) {
+  __shared__ Key s_keys[4][CAP];
+  __shared__ Key s_best[MOST];
+  __shared__ int s_count[4];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t row = blockIdx.x;
   const Stats* p = (const Stats*)a.work + row * a.parts;
   const float c = a.scale * LOG2E;
-  Stats z{-INFINITY, 0.f, 0.f};
-  Candidates cand;
-  cand.init(s_keys, nullptr, a.top);
-  for (int q = lane; q < a.parts; q += 64) z = join(z, p[q], c);
-  z = lanes_join(z, c);
+  const Stats mine = lane < a.parts ? p[lane] : Stats{-INFINITY, 0.f, 0.f};  // (at most 64 parts)
+  const int64_t token = a.token ? a.token[row] : -1;
+  const bool has = token >= 0 && token < a.V;
+  const float logit = has ? (float)((const T*)a.x + row * a.x_stride)[token] : 0.f;
+  int count = 0;
   if (a.top) {
+    Candidates cand;
+    cand.init(s_keys[wave], nullptr, a.top);
     const Key* keys = part_keys(a, row);
     const int all = a.parts * a.top;
-    for (int i = 0; i < all; i += 256) {  // four loads at a time
+    for (int i = 64 * wave; i < all; i += 1024) {  // four loads at a time
       Key k[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) k[j] = i + 64 * j + lane < all ? keys[i + 64 * j + lane] : 0;
+      for (int j = 0; j < 4; ++j) k[j] = i + 256 * j + lane < all ? keys[i + 256 * j + lane] : 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) cand.offer(k[j]);
     }
     cand.cut();
+    if (lane == 0) s_count[wave] = cand.count;
+    __syncthreads();
+    count = best_of(s_keys, s_count, cand, s_best);
   }
-  const int64_t token = a.token ? a.token[row] : -1;
-  const bool has = token >= 0 && token < a.V;
-  write_row(a, row, z, has ? (float)((const T*)a.x + row * a.x_stride)[token] : 0.f, has, s_keys, cand.count);
+  if (wave) return;
+  write_row(a, row, lanes_join(mine, c), logit, has, s_best, count);
 }
 
 // Gradient: a workgroup takes SEGMENT elements of a row, or (WAVE: rows of up to SEGMENT / 4) each of its waves a row.  The
@@ -439,7 +451,7 @@ int launch_token_scores(const ScoresArgs& all, dn_dtype dt, void* stream) {
       else run(std::false_type{});
       if (const int err = (int)hipGetLastError()) return err;
       if (a.parts > 1) {
-        join_scores_kernel<T><<<dim3((unsigned)a.n), 64, 0, st>>>(a);
+        join_scores_kernel<T><<<dim3((unsigned)a.n), 256, 0, st>>>(a);
         if (const int err = (int)hipGetLastError()) return err;
       }
     }
