@@ -22,7 +22,7 @@ LIB_PATH = os.path.join(_HERE, "libdensenet.so")
 DN_OK, DN_E_INVALID_ARG, DN_E_TOO_LARGE, DN_E_BUFFER_TOO_SMALL = 0, -1, -2, -3
 DN_E_UNSUPPORTED, DN_E_HIP, DN_E_INTERNAL = -4, -5, -6
 DN_F32, DN_F16, DN_BF16 = 0, 1, 2
-DN_F8 = 3   # e4m3: 8-bit outputs and optimiser states only
+DN_F8 = 3   # e4m3: 8-bit outputs, operands with scales for blocks, and optimiser states only
 DN_PAD_ZERO, DN_PAD_RAMP = 0, 1
 DN_MAX_SCALES, DN_MAX_PLANES_PER_IMAGE, DN_MAX_WARP_SIDE, DN_MAX_ASPECTS = 64, 64, 1024, 8
 DN_MAX_BATCH_ITEMS = 65536

@@ -1,4 +1,4 @@
-// Internal declarations of the head's operators (norm, loss, optimiser): the launchers, and the device helpers they
+// Internal declarations of the head's operators (norm, loss, optimisers, 8-bit products, scores): the launchers, and the device helpers they
 // share.  Conventions (errors, streams, ownership) are the library's: see densenet.h.
 #pragma once
 

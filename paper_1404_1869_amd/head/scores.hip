@@ -1,7 +1,9 @@
 // Scores of rows of logits: log probability of a given token, entropy and best alternatives, and their gradient.
 //   x = scale l;  lse = log sum exp x;  logp_v = x_v - lse;  H = -sum p log p;  the `top` largest logits, lower index first among equals
 //   gradient: with A = dlse - dlogp - sum dtop - dH H,  dl_v = scale (p_v (A - dH log p_v) + dlogp [v = token] + dtop_j [v = id_j])
-// Bound by memory: a row is read once (the gradient: read once and written once).  Every lane keeps its own maximum m, sum S of
+// A row is read once (the gradient: read once and written once).  The gradient is bound by memory (4096 x 32000 in bf16 92 us, 333 x
+// 50257 in fp32 with 8 alternatives 27), the scores by the vector unit (2000 x 50257 in fp16 46 us, with 5 alternatives 62), and one
+// row by the chain of its two launches (131072 logits with 20 alternatives 19 us).  Every lane keeps its own maximum m, sum S of
 // exp(x - m) and T of exp(x - m) (x - m) and rescales them where the maximum grows; lanes, waves and workgroups join theirs at
 // the end, in a fixed order.  H = log S - T / S, and a logit's part is taken as (x - m), so large logits lose no digits.
 // Alternatives: a wave keeps candidates above a bound that `top` values of the row are known to reach.  The top-th largest of the

@@ -40,7 +40,6 @@ class RegionHead:
         self.muon = D.MuonPlan([self.w], [self.dw], copies=copies, rates=[1.0]) if muon else None
         self.plans = (() if muon else (D.AdamWPlan([self.w], [self.dw], copies=copies, state_bits=state_bits),)) + \
             (D.AdamWPlan([self.gamma], [self.dgamma], state_bits=32),)
-        self._eight = None  # w in 8 bits, as it lies and turned, until the next step
 
     def loss(self, descriptors, labels):
         """Loss of each row (0 where its label is outside the vocabulary)."""
@@ -63,13 +62,10 @@ class RegionHead:
             D.densenet_adamw(plan, lr=lr, step=self.steps, weight_decay=weight_decay, grad_scale=1 / self.scale, seed=self.steps)
         if self.muon:
             D.densenet_muon(self.muon, lr=lr, weight_decay=weight_decay, grad_scale=1 / self.scale)
-        self._eight = None
 
-    def _words_8bit(self):
-        """w's codes and scales in squares of 128, as it lies and turned, made once after each step."""
-        if self._eight is None:
-            self._eight = D.densenet_quantize_blocks(self.products, rows=D.DN_SCALE_BLOCK, turned=True)
-        return self._eight
+    def words_8bit(self, turned: bool = False):
+        """w's codes and scales in squares of 128 (and turned, for dy), for answers until w changes."""
+        return D.densenet_quantize_blocks(self.products, rows=D.DN_SCALE_BLOCK, turned=turned)
 
     def step_8bit(self, descriptors, labels, lr: float = 2e-4, weight_decay: float = 0.01):
         """As ``step``, all products reading 8-bit operands: logits of the rows' codes and w's, dy of the logits' gradient's codes
@@ -78,7 +74,7 @@ class RegionHead:
         y, _, _ = D.densenet_rms_norm(descriptors, self.gamma, eps=self.eps, out_dtype=self.dtype)
         codes, scale, _, _ = D.densenet_quantize_blocks(y)
         _, _, turned, turned_scale = D.densenet_quantize_blocks(y, rows=D.DN_SCALE_BLOCK, codes=False, turned=True)
-        w, w_scale, wt, wt_scale = self._words_8bit()
+        w, w_scale, wt, wt_scale = self.words_8bit(turned=True)
         logits = D.densenet_block_product(codes, scale, w, w_scale, out_dtype=self.dtype)
         logp, _, lse, _, _ = D.densenet_token_scores(logits, labels)
         has = (labels >= 0) & (labels < self.w.shape[0])
@@ -90,11 +86,12 @@ class RegionHead:
         self._update(dy, descriptors, lr, weight_decay)
         return -logp
 
-    def answer(self, descriptors, top: int = 5):
+    def answer(self, descriptors, top: int = 5, words=None):
         """Each row's `top` most probable words, their log probabilities, and the entropy of its distribution, from products in 8
-        bits of normalised rows that are 8-bit codes from the start."""
+        bits of normalised rows that are 8-bit codes from the start.  words: of ``words_8bit``, which a caller keeps between answers
+        (by default made anew)."""
         codes, _, scale = D.densenet_rms_norm(descriptors, self.gamma, eps=self.eps, out_dtype=D.DN_F8, block=D.DN_SCALE_BLOCK)
-        w, w_scale, _, _ = self._words_8bit()
+        w, w_scale = (words or self.words_8bit())[:2]
         logits = D.densenet_block_product(codes, scale, w, w_scale, out_dtype=self.dtype)
         _, entropy, _, ids, logp = D.densenet_token_scores(logits, top=top)
         return ids, logp, entropy

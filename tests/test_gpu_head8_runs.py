@@ -282,3 +282,19 @@ def test_scores_of_many_rows(D):
         for first in (0, (1 << 26) // period * period - period):
             assert torch.equal(a[first:first + period], b)
         assert torch.equal(a[-5:], b[torch.arange(n - 5, n, device="cuda") % period])
+
+
+def test_answers_follow_the_weights(D):
+    """Words that a caller keeps give the same answers; without them an answer is of the weights as they are now."""
+    from paper_1404_1869_amd.region_head import RegionHead
+    head = RegionHead(256, 500, seed=3)  # two squares of rows, which change places when the rows are turned about
+    desc = torch.randn(40, 500, generator=gen(51), device="cuda")
+    kept = head.words_8bit()
+    ids, logp, H = head.answer(desc, top=3)
+    again = head.answer(desc, top=3, words=kept)
+    assert torch.equal(ids, again[0]) and torch.equal(logp, again[1]) and torch.equal(H, again[2])
+    head.products.copy_(head.products.flip(0))
+    alone = logp[:, 0] > logp[:, 1]  # (of equal logits, which bf16 has many of, the lower index comes first before and after)
+    assert int(alone.sum()) > 10
+    assert torch.equal(head.answer(desc, top=1)[0][alone], 255 - ids[alone, :1])
+    assert torch.equal(head.answer(desc, top=3, words=kept)[0], ids)
