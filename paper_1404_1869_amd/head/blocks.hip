@@ -586,7 +586,8 @@ int tile_n(Tile t) { return t == T256 ? 256 : t == T128 ? 128 : t == T64 ? 64 : 
 int64_t tiles_of(Tile t, int64_t n, int64_t V) { return (up(V, tile_m(t)) / tile_m(t)) * (up(n, tile_n(t)) / tile_n(t)); }
 int round_of(Tile t) { return t == T256 ? 256 : 512; }  // workgroups that run together
 
-// What is computed how: the first `full` tiles a workgroup each, the rest in `splits` workgroups along k, whose sums a launch joins.
+// What is computed how: the first `full` tiles a workgroup each, the rest in `splits` workgroups along k, whose sums a launch joins
+// (2000 x 9216 over 10007, 320 tiles for 256 CUs: 198 us, all whole 262).
 struct Plan8 {
   Tile tile;
   int64_t full, rest;

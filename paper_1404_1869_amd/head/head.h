@@ -91,7 +91,7 @@ struct ScoresArgs {
   float* top_logp;
   void* work;
 };
-int32_t scores_parts(int64_t n, int32_t V);
+int32_t scores_parts(int64_t n, int32_t V, int32_t top);
 size_t scores_bytes(int64_t n, int32_t V, int32_t top);
 int launch_token_scores(const ScoresArgs& a, dn_dtype dt, void* stream);
 struct ScoresBackArgs {

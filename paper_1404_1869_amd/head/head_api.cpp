@@ -320,7 +320,7 @@ int densenet_token_scores(const void* d_logits, int64_t stride, const int64_t* d
     if ((uintptr_t)d_logp % 4 || (uintptr_t)d_entropy % 4 || (uintptr_t)d_lse % 4 || (uintptr_t)d_top_logp % 4 ||
         (uintptr_t)d_top_id % 8)
       return fail(DN_E_INVALID_ARG, "an output is not aligned to its elements");
-    ScoresArgs a{d_logits, d_token, stride,    n,     V,        top,        scores_parts(n, V), scale,
+    ScoresArgs a{d_logits, d_token, stride,    n,     V,        top,        scores_parts(n, V, top), scale,
                  d_logp,   d_entropy, d_lse, d_top_id, d_top_logp, d_workspace};
     return run_step("token_scores", stream, [&] { return launch_token_scores(a, dtype, stream); });
   } catch (...) {

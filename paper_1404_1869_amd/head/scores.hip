@@ -2,7 +2,7 @@
 //   x = scale l;  lse = log sum exp x;  logp_v = x_v - lse;  H = -sum p log p;  the `top` largest logits, lower index first among equals
 //   gradient: with A = dlse - dlogp - sum dtop - dH H,  dl_v = scale (p_v (A - dH log p_v) + dlogp [v = token] + dtop_j [v = id_j])
 // A row is read once (the gradient: read once and written once).  The gradient is bound by memory (4096 x 32000 in bf16 92 us, 333 x
-// 50257 in fp32 with 8 alternatives 27), the scores by the vector unit (2000 x 50257 in fp16 46 us, with 5 alternatives 62), and one
+// 50257 in fp32 with 8 alternatives 27), the scores by the vector unit (2000 x 50257 in fp16 45 us, with 5 alternatives 57), and one
 // row by the chain of its two launches (131072 logits with 20 alternatives 19 us).  Every lane keeps its own maximum m, sum S of
 // exp(x - m) and T of exp(x - m) (x - m) and rescales them where the maximum grows; lanes, waves and workgroups join theirs at
 // the end, in a fixed order.  H = log S - T / S, and a logit's part is taken as (x - m), so large logits lose no digits.
@@ -326,10 +326,11 @@ __global__ __launch_bounds__(256) void join_scores_kernel(ScoresArgs a) {
 // Gradient: a workgroup takes SEGMENT elements of a row, or (WAVE: rows of up to SEGMENT / 4) each of its waves a row.  The
 // gradients of the token's and the alternatives' own logits wait in LDS at their elements' places, eights of elements that hold one
 // marked in a bitmap, so that an element is written once (the result may be the logits' own memory) and no other is looked at.
+// (of 4096 elements where a row has no more: 16384 x 4096 in bf16 43 us, of 8192 64).
 constexpr int SEGMENT = 8192;
-template <typename T, bool WAVE>
+template <typename T, bool WAVE, int LEN>
 __global__ __launch_bounds__(256) void scores_back_kernel(ScoresBackArgs a) {
-  constexpr int TPR = WAVE ? 64 : 256, LEN = WAVE ? SEGMENT / 4 : SEGMENT, WORDS = LEN / 8 / 32, STEPS = LEN / 8 / TPR;
+  constexpr int TPR = WAVE ? 64 : 256, WORDS = LEN / 8 / 32, STEPS = LEN / 8 / TPR;
   __shared__ __align__(16) float s_own[WAVE ? 4 : 1][LEN];
   __shared__ uint32_t s_bits[WAVE ? 4 : 1][WORDS];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, t = threadIdx.x % TPR, sub = WAVE ? wave : 0;
@@ -411,17 +412,24 @@ int with_type(dn_dtype dt, F&& f) {
   return f(__bf16{});
 }
 
-constexpr int SHORT = 2048;  // rows of up to so many logits: a wave each
+// Which rows have a wave each, not a workgroup: those of up to SHORT logits (16384 x 1000 with 5 alternatives 19 us, else 61), and
+// longer ones where there are seven for a CU and more, since fewer bounds are looked for and joined (with 5 alternatives 2000 x 50257 58
+// us, else 64, 5000 x 50257 103 and 136, 16384 x 8192 67 and 120; without 5000 x 50257 92 and 107).  Of fewer, SIMDs without a row
+// wait as long as the last one takes (1536 x 131072 117 us, else 100).
+constexpr int SHORT = 2048, MANY = 1792;
+bool wave_each(int64_t n, int32_t V) { return V <= SHORT || n >= MANY; }
 
 }  // namespace
 
-// Workgroups of a row: enough of them for the chip where there are few rows, of at least two blocks a wave.
-int32_t scores_parts(int64_t n, int32_t V) {
-  if (V <= SHORT || n >= 1024 || n == 0) return 1;
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({(1024 + n - 1) / n, V / (8 * WAVE_BLOCK), 64}));
+// Workgroups of a row: enough of them for the chip where there are few rows, of at least two blocks a wave.  The launch that joins
+// them costs 3 us, so only long rows are split: with 20 alternatives 8 x 50257 takes 20 us, in one workgroup 30 (400 rows 31 and 35,
+// 700 rows 48 and 38), and 8 x 16384 20 and 17; without alternatives 8 x 131072 takes 16 us either way.
+int32_t scores_parts(int64_t n, int32_t V, int32_t top) {
+  if (V <= (top ? 1 << 15 : 1 << 17) || n >= 512 || n == 0) return 1;
+  return (int32_t)std::min<int64_t>({(1024 + n - 1) / n, V / (8 * WAVE_BLOCK), 64});
 }
 size_t scores_bytes(int64_t n, int32_t V, int32_t top) {
-  const int64_t parts = scores_parts(n, V);
+  const int64_t parts = scores_parts(n, V, top);
   return parts == 1 ? 0 : sizeof(Stats) * (size_t)((n * parts + 1) / 2 * 2) + sizeof(Key) * (size_t)(n * parts) * top;
 }
 
@@ -429,7 +437,7 @@ int launch_token_scores(const ScoresArgs& all, dn_dtype dt, void* stream) {
   return with_type(dt, [&](auto v) {
     using T = decltype(v);
     const hipStream_t st = (hipStream_t)stream;
-    const bool wave = all.V <= SHORT;
+    const bool wave = wave_each(all.n, all.V);
     const int64_t most = MAX_LAUNCH_THREADS / 256 / all.parts * (wave ? 4 : 1);
     for (int64_t at = 0; at < all.n; at += most) {  // (more than one launch's rows: never split)
       ScoresArgs a = all;
@@ -465,6 +473,7 @@ int launch_token_scores_backward(const ScoresBackArgs& all, dn_dtype dt, void* s
   return with_type(dt, [&](auto v) {
     using T = decltype(v);
     const bool wave = all.V <= SHORT;
+    const bool half = all.V <= SEGMENT / 2;
     const int64_t segments = wave ? 1 : ((int64_t)all.V + SEGMENT - 1) / SEGMENT;
     const int64_t most = MAX_LAUNCH_THREADS / 256 / segments * (wave ? 4 : 1);
     for (int64_t at = 0; at < all.n; at += most) {
@@ -479,9 +488,11 @@ int launch_token_scores_backward(const ScoresBackArgs& all, dn_dtype dt, void* s
       if (all.dlse) a.dlse = all.dlse + at;
       if (all.dtop) a.dtop = all.dtop + at * all.top, a.top_id = all.top_id + at * all.top;
       if (wave)
-        scores_back_kernel<T, true><<<dim3((unsigned)((a.n + 3) / 4)), 256, 0, (hipStream_t)stream>>>(a);
+        scores_back_kernel<T, true, SHORT><<<dim3((unsigned)((a.n + 3) / 4)), 256, 0, (hipStream_t)stream>>>(a);
+      else if (half)
+        scores_back_kernel<T, false, SEGMENT / 2><<<dim3((unsigned)a.n), 256, 0, (hipStream_t)stream>>>(a);
       else
-        scores_back_kernel<T, false><<<dim3((unsigned)(a.n * segments)), 256, 0, (hipStream_t)stream>>>(a);
+        scores_back_kernel<T, false, SEGMENT><<<dim3((unsigned)(a.n * segments)), 256, 0, (hipStream_t)stream>>>(a);
       if (const int err = (int)hipGetLastError()) return err;
     }
     return 0;

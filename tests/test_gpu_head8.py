@@ -250,6 +250,9 @@ SCORES = [  # n, V, type, top, scale, masked, row padding, first element
     (1100, 2500, "bf16", 3, 1.0, 0.0, 0, 0), (2, 50257, "f32", 64, 1.0, 0.9, 0, 0), (33, 16385, "f16", 1, 1.0, 0.0, 5, 0),
     (5, 32000, "bf16", 0, 1.0, 0.0, 0, 0), (70, 300, "f32", 0, 3.0, 0.0, 1, 1), (1, 1000003, "bf16", 64, 1.0, 0.0, 0, 0),
     (4, 65, "f32", 64, 1.0, 0.99, 0, 0),
+    # a wave a row: many rows of any length; few long ones: split, or where nothing is looked for only longer ones
+    (1792, 2500, "bf16", 5, 1.0, 0.1, 0, 0), (1800, 9001, "f16", 20, 1.0, 0.0, 3, 1), (2000, 5000, "f32", 0, 1.0, 0.0, 0, 0),
+    (2, 140001, "f32", 0, 1.0, 0.1, 0, 0), (300, 40001, "bf16", 7, 1.0, 0.0, 0, 0), (511, 32769, "f16", 2, 1.0, 0.0, 0, 0),
 ]
 
 
@@ -297,6 +300,14 @@ def test_scores_ties_and_order(D, V):
     _, _, _, ids, best = D.densenet_token_scores(x, top=64)
     v = x.gather(1, ids)
     assert bool(((v[:, :-1] != v[:, 1:]) | (best[:, :-1] == best[:, 1:])).all()) and bool((best[:, :-1] >= best[:, 1:]).all())
+
+
+def test_scores_ties_of_many_rows(D):
+    g = gen(77)
+    x = (torch.randn(1800, 3000, generator=g, device="cuda") * 2).round().bfloat16()
+    token = torch.zeros(1800, dtype=torch.int64, device="cuda")
+    for top in (1, 7, 64):
+        assert torch.equal(D.densenet_token_scores(x, token, top=top)[3], plain_scores(x, token, 1.0, top)[3])
 
 
 @pytest.mark.parametrize("V", [10, 5000, 40000])
@@ -352,7 +363,8 @@ def plain_back(x, token, lse, H, dlogp, dH, dlse, ids, dtop, scale):
 
 BACK = [(1, 1, "f32", 1, 1.0, 0.0, 0, 0), (3, 7, "f16", 4, 1.0, 0.0, 1, 0), (130, 100, "bf16", 64, 0.5, 0.3, 3, 0), (9, 2048, "f32", 5, 2.0, 0.0, 0, 0),
         (6, 2049, "f16", 64, 1.0, 0.5, 7, 3), (5, 8193, "bf16", 3, 1.0, 0.0, 0, 0), (2, 50257, "f32", 0, 1.0, 0.1, 0, 1),
-        (1, 131072, "bf16", 20, 1.25, 0.1, 0, 0)]
+        (1, 131072, "bf16", 20, 1.25, 0.1, 0, 0), (40, 3000, "bf16", 5, 1.0, 0.1, 0, 0), (3, 4096, "f32", 64, 1.0, 0.0, 0, 0),
+        (2, 4097, "f16", 2, 1.0, 0.0, 5, 1)]
 
 
 @pytest.mark.parametrize("n,V,dt,top,scale,masked,pad,off", BACK)
