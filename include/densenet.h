@@ -411,8 +411,10 @@ int densenet_adamw(const dn_adamw_tensor* tensors, int32_t count, dn_dtype p_dty
                    float* d_m_scale, float* d_v_scale, int64_t n_blocks, void* stream);
 
 /* Operators of a head that learns and answers in 8 bits: rows and weights as DN_F8 codes with a scale for every block of
- * DN_SCALE_BLOCK, products of such operands, scores of the logits that they give, and Muon's step. */
+ * DN_SCALE_BLOCK, products of such operands, scores of the logits that they give, and Muon's step.  Where a size query of theirs
+ * gives DN_NO_WORKSPACE, the call wants a workspace of so many bytes and leaves it alone: calls at the same time may share it. */
 #define DN_SCALE_BLOCK 128
+#define DN_NO_WORKSPACE 256
 
 /* Rows x [n][C] as codes with scales: x = code * scale.  rows 1: a scale for every DN_SCALE_BLOCK values of a row,
  * d_scale[n][ceil(C / 128)]; rows DN_SCALE_BLOCK: for every square of 128 rows x 128 values, d_scale[ceil(n / 128)][ceil(C / 128)];

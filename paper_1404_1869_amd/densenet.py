@@ -28,7 +28,7 @@ DN_MAX_SCALES, DN_MAX_PLANES_PER_IMAGE, DN_MAX_WARP_SIDE, DN_MAX_ASPECTS = 64, 6
 DN_MAX_BATCH_ITEMS = 65536
 DN_STATIC_SCRATCH_BYTES = 64 << 20
 DN_MAX_NORM_C = 32768
-DN_SCALE_BLOCK, DN_MAX_TOP, DN_MAX_NS_STEPS = 128, 64, 16
+DN_SCALE_BLOCK, DN_MAX_TOP, DN_MAX_NS_STEPS, DN_NO_WORKSPACE = 128, 64, 16, 256
 ADAMW_BLOCK = 256
 DTYPES = {"f32": DN_F32, "f16": DN_F16, "bf16": DN_BF16}
 
@@ -907,6 +907,16 @@ def densenet_adamw(plan: AdamWPlan, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, 
 # ------------------------------------------------------------------------------------------------
 # A head in 8 bits
 # ------------------------------------------------------------------------------------------------
+@functools.lru_cache(maxsize=None)
+def _no_workspace(device):
+    return _torch().empty(DN_NO_WORKSPACE, dtype=_torch().uint8, device=device)
+
+
+def _workspace(need, device):
+    """A call's workspace: one for all calls that leave it alone."""
+    return _no_workspace(device) if need == DN_NO_WORKSPACE else _torch().empty(need, dtype=_torch().uint8, device=device)
+
+
 def _codes(shape, device):
     """Codes in rows that start on 16 bytes, which products read as they lie."""
     torch = _torch()
@@ -986,7 +996,7 @@ def densenet_block_product(a, a_scale, w, w_scale, out_dtype=DN_BF16, out=None):
     # (the size depends on the codes' alignment: addresses of the same one in place of their own)
     need = _work_bytes("densenet_block_product", 4096 + ap % 16 if ap else None, as_, None, 4096 + wp % 16, ws_, None, n, C, V, None, 0,
                        out_dtype)
-    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    ws = _workspace(need, dev)
     check(lib().densenet_block_product(ap, as_, a_scale.data_ptr(), wp, ws_, w_scale.data_ptr(), n, C, V, yp, ys, out_dtype,
                                        ws.data_ptr(), need, None, _on(dev)))
     return out
@@ -1027,7 +1037,7 @@ def densenet_token_scores(logits, tokens=None, top=0, scale=1.0, logp=None, entr
     vec = lambda t, what: _vector(t, what, n, torch.float32, dev)  # noqa: E731
     ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     need = _work_bytes("densenet_token_scores", 4096, V, None, n, V, dt, 1.0, top, None, None, None, None, None)
-    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    ws = _workspace(need, dev)
     check(lib().densenet_token_scores(xp, xs, _vector(tokens, "tokens", n, torch.int64, dev), n, V, dt, scale, top, vec(logp, "logp"),
                                       vec(entropy, "entropy"), vec(lse, "lse"), ptr(top_id), ptr(top_logp), ws.data_ptr(), need, None,
                                       _on(dev)))
@@ -1089,6 +1099,7 @@ class MuonPlan:
         rates = [0.2 * max(p.shape) ** 0.5 if p.dim() == 2 else 0.0 for p in self.params] if rates is None else list(rates)
         if len(self.momentum) != len(self.params) or len(rates) != len(self.params):
             raise _bad("as much momentum and as many rates as parameters expected")
+        self.work_bytes = {}  # of each number of parts, once it has been asked for
         self.table = (dn_muon_tensor * len(self.params))()
         for e, p, c, m, rate in zip(self.table, self.params, self.copies, self.momentum, rates):
             if p.dim() != 2 or p.numel() == 0:
@@ -1141,9 +1152,11 @@ def densenet_muon(plan: MuonPlan, lr, momentum=0.95, nesterov=True, weight_decay
         k.coefficients[i][:] = c
     k.steps, k.nesterov, k.parts = steps, int(nesterov), plan.parts
     on = _on(plan.device)
-    torch = _torch()
     args = (plan.table, len(plan.table), plan.p_dtype, plan.g_dtype, plan.copy_dtype, ctypes.byref(k))
-    need = ctypes.c_size_t()
-    check(lib().densenet_muon(*args, None, 0, ctypes.byref(need), None))
-    ws = torch.empty(need.value, dtype=torch.uint8, device=plan.device)
-    check(lib().densenet_muon(*args, ws.data_ptr(), need.value, None, on))
+    need = plan.work_bytes.get(plan.parts)
+    if need is None:
+        asked = ctypes.c_size_t()
+        check(lib().densenet_muon(*args, None, 0, ctypes.byref(asked), None))
+        need = plan.work_bytes[plan.parts] = asked.value
+    ws = _workspace(need, plan.device)
+    check(lib().densenet_muon(*args, ws.data_ptr(), need, None, on))

@@ -43,6 +43,9 @@ int check_work(const void* work, size_t bytes, size_t need, size_t* needed) {
 constexpr int64_t MAX_ROWS = (1LL << 31) - 256;
 constexpr int64_t MAX_BACK_ROWS = (1LL << 30) - 256;  // twice their number is a product's k in fp32
 constexpr int64_t MAX_TILES = MAX_LAUNCH_THREADS / 256;
+// What a call of the 8-bit head's asks for: never 0, so that a caller's workspace is never the null pointer of a size query, and
+// DN_NO_WORKSPACE exactly where nothing is written there.
+size_t at_least(size_t bytes) { return bytes ? bytes + DN_NO_WORKSPACE : DN_NO_WORKSPACE; }
 
 int check_loss(const LossArgs& a, dn_dtype dtype, bool backward) {
   if (!valid_dtype(dtype)) return fail(DN_E_UNSUPPORTED, "unknown dtype");
@@ -293,8 +296,7 @@ int densenet_block_product(const void* d_a, int64_t a_stride, const float* d_a_s
     int st;
     if ((st = check_rows("a", d_a, a_stride, n, C, 1))) return st;
     if ((st = check_rows("w", d_w, w_stride, V, C, 1))) return st;
-    // (never 0, so that a caller's workspace is never the null pointer of a size query)
-    const size_t need = std::max<size_t>(n ? block_product_bytes(a, y_dtype) : 0, 256);
+    const size_t need = at_least(n ? block_product_bytes(a, y_dtype) : 0);
     if ((st = check_work(d_workspace, workspace_bytes, need, bytes_needed)) || !d_workspace) return st;
     if (n == 0) return DN_OK;
     if (!d_a_scale || !d_w_scale) return fail(DN_E_INVALID_ARG, "null scale pointer");
@@ -312,7 +314,7 @@ int densenet_token_scores(const void* d_logits, int64_t stride, const int64_t* d
   try {
     int st;
     if ((st = check_scores(d_logits, stride, d_token, n, V, dtype, scale, top))) return st;
-    const size_t need = std::max<size_t>(scores_bytes(n, V, top), 256);
+    const size_t need = at_least(scores_bytes(n, V, top));
     if ((st = check_work(d_workspace, workspace_bytes, need, bytes_needed)) || !d_workspace) return st;
     if (n == 0) return DN_OK;
     if (!d_lse) return fail(DN_E_INVALID_ARG, "null lse pointer");

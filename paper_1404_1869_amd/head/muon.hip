@@ -784,7 +784,7 @@ int run_small(const dn_muon_tensor* const* ts, int count, const dn_muon_params& 
 }  // namespace
 
 size_t muon_bytes(const dn_muon_tensor* tensors, int32_t count, dn_dtype p_dt, const dn_muon_params& k) {
-  size_t most = 256;
+  size_t most = DN_NO_WORKSPACE;  // (a group's is more: it has five pieces of 256 bytes at least)
   Group gr;
   const int parts = parts_of(k, p_dt);
   dn_muon_tensor large[MATS];

@@ -92,6 +92,17 @@ def test_nothing_to_do():
     assert muon(count=0) == D.DN_OK
 
 
+def test_workspaces_that_are_left_alone():
+    need = ctypes.c_size_t()
+    q = dict(work=None, need=ctypes.byref(need))
+    some = dict(ids=P, best=P, top=20)
+    for call, nothing in ((lambda: scores(**q), True), (lambda: scores(n=1, V=32768, xs=32768, **some, **q), True),
+                          (lambda: scores(n=1, V=32769, xs=32769, **some, **q), False), (lambda: scores(n=2000, V=65536, xs=65536, **some, **q), True),
+                          (lambda: product(**q), True), (lambda: product(n=1, C=5, as_=5, V=3, ws=16, ys=3, **q), False),
+                          (lambda: muon(**q), True), (lambda: muon(rows=300, cols=300, **q), False)):
+        assert call() == D.DN_OK and (need.value == D.DN_NO_WORKSPACE) == nothing and need.value >= D.DN_NO_WORKSPACE
+
+
 def test_size_queries():
     need = ctypes.c_size_t(77)
     q = dict(work=None, need=ctypes.byref(need))
