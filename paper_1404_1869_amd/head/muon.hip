@@ -9,7 +9,7 @@
 //   roundings are of either sign and come to about 2^-11 of the update in all, below half a unit of a bf16 weight.  Two parts
 //   (fp32 and fp16 weights) are 22 bits, in three products of parts, as the loss's logits in fp32.
 // Bound by the matrix cores: six matrices of 2048 x 8192 in bf16 take 3.8 ms (0.86 PFLOP/s), one of 1000 x 9216 in two parts 0.81 ms
-// (0.53: its 144 tiles leave CUs idle), four of 512 x 512 300 us in two parts and 176 in one, which are launches more than work.
+// (0.53: its 144 tiles leave CUs idle), four of 512 x 512 278 us in two parts and 164 in one, which are launches more than work.
 // All matrices of a call go through the same launches.  Sums over k go to slabs in fp32, one for each split, and a launch adds
 // them in order, so results do not depend on what ran first.
 #include <hip/hip_runtime.h>
@@ -144,18 +144,17 @@ __global__ __launch_bounds__(256) void start_kernel(MuonLaunch l) {
   }
 }
 
-// Tile shapes: 256 x 256 by eight waves, a workgroup per CU, or 128 x 128 by four, two per CU.
-template <int T>
+// Tile shapes: 256 x 256 by eight waves, a workgroup per CU, 128 x 128 by four, two per CU, or 128 x 64 by four, three per CU.
+template <int BM, int BN = BM>
 struct Shape {
-  static constexpr int WM = 2, WN = T == 256 ? 4 : 2, NW = WM * WN, NST = 2, STAGE = 2 * T * BK * 2;
-  static constexpr int WCOLS = T / WM, WROWS = T / WN, TM = WCOLS / 32, TN = WROWS / 32;
+  static constexpr int WM = 2, WN = BM == 256 ? 4 : 2, NW = WM * WN, NST = 2, STAGE = (BM + BN) * BK * 2;
+  static constexpr int WCOLS = BM / WM, WROWS = BN / WN, TM = WCOLS / 32, TN = WROWS / 32;
   static constexpr int OUT_ROW = WCOLS * 4 + 16, OUT = NW * 32 * OUT_ROW;
   static constexpr int LDS = NST * STAGE > OUT ? NST * STAGE : OUT;
 };
 // The tile's rows n on their way out, through LDS: `row(n, c, v)` gets eight values of row n of the tile from column c on.
-template <int T, typename F>
-__device__ inline void rows_out(char* s_mem, int wave, int lane, const f32x16 (&acc)[Shape<T>::TM][Shape<T>::TN], F&& row) {
-  using S = Shape<T>;
+template <typename S, typename F>
+__device__ inline void rows_out(char* s_mem, int wave, int lane, const f32x16 (&acc)[S::TM][S::TN], F&& row) {
   const int l32 = lane & 31, half = lane >> 5, wm = wave % S::WM, wn = wave / S::WM;
   constexpr int LANES = S::WCOLS / 8, LINES = 64 / LANES;
   __syncthreads();
@@ -267,7 +266,7 @@ __global__ __launch_bounds__(64 * Shape<T>::NW) void gram_kernel(MuonLaunch l) {
   if constexpr (SLABS) {
     const int64_t slab_ld = (int64_t)tiles * T;
     float* out = (float*)(l.work + t.slab) + split * r * slab_ld;
-    rows_out<T>(s_mem, wave, lane, acc, [&](int n, int m, const float (&v)[8]) {
+    rows_out<S>(s_mem, wave, lane, acc, [&](int n, int m, const float (&v)[8]) {
       if (n0 + n < r) store8(out + (n0 + n) * slab_ld + m0 + m, v);
     });
   } else {
@@ -286,7 +285,7 @@ __global__ __launch_bounds__(64 * Shape<T>::NW) void gram_kernel(MuonLaunch l) {
         for (int j = 0; j < 8; ++j) v[j] = entry(v[j], a[j]);
         store_parts<PARTS>(to + at, apart, v);
       });
-    rows_out<T>(s_mem, wave, lane, acc, [&](int n, int m, float (&v)[8]) {
+    rows_out<S>(s_mem, wave, lane, acc, [&](int n, int m, float (&v)[8]) {
       n += n0, m += m0;
       if (n >= r || m >= lda) return;
       const int64_t at = (int64_t)n * lda + m;
@@ -343,33 +342,33 @@ __global__ __launch_bounds__(1024) void mirror_kernel(MuonLaunch l) {
 }
 
 // X = a X + P X (of a tall matrix a X + X P), into the other buffer, or (LAST) p's step.
-template <int PARTS, int T, bool LAST, typename P, typename O>
-__global__ __launch_bounds__(64 * Shape<T>::NW) void update_kernel(MuonLaunch l) {
-  using S = Shape<T>;
+template <int PARTS, int BM, int BN, bool LAST, typename P, typename O>
+__global__ __launch_bounds__((64 * Shape<BM, BN>::NW)) void update_kernel(MuonLaunch l) {
+  using S = Shape<BM, BN>;
   __shared__ __align__(1024) char s_mem[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int all = gridDim.x, xcd = blockIdx.x % 8, per = all / 8, rem = all % 8;
   const int job = xcd * per + min(xcd, rem) + blockIdx.x / 8;
   const Mat& t = mat_of(l, job);
-  const int r = min(t.rows, t.cols), tiles_m = (t.cols + T - 1) / T, tiles_n = (t.rows + T - 1) / T;
+  const int r = min(t.rows, t.cols), tiles_m = (t.cols + BM - 1) / BM, tiles_n = (t.rows + BN - 1) / BN;
   constexpr int COL = 6;
   const int id = job - t.first, col = id / (COL * tiles_m), width = min(COL, tiles_n - col * COL), in = id - col * COL * tiles_m;
-  const int m0 = in / width * T, n0 = (col * COL + in % width) * T;  // m: columns of X, n: rows
+  const int m0 = in / width * BM, n0 = (col * COL + in % width) * BN;  // m: columns of X, n: rows
   const int ld = up8(t.cols), ldp = up8(r);
   const int64_t part = (int64_t)t.rows * ld, ppart = (int64_t)r * ldp;
   const _Float16* x = (const _Float16*)(l.work + t.x[l.from]);
   const void* poly = l.work + t.poly;
   f32x16 acc[S::TM][S::TN];
   if (t.rows <= t.cols)
-    multiply<_Float16, true, false, T, T, S::WM, S::WN, S::NST, PARTS == 2>(
+    multiply<_Float16, true, false, BM, BN, S::WM, S::WN, S::NST, PARTS == 2>(
         s_mem, Multiplied{x, poly, ld, ldp, part, ppart, ld, r, r, PARTS == 2 ? 3 : 1}, m0, n0, 0, 1, wave, lane, acc);
   else
-    multiply<_Float16, false, false, T, T, S::WM, S::WN, S::NST, PARTS == 2>(
+    multiply<_Float16, false, false, BM, BN, S::WM, S::WN, S::NST, PARTS == 2>(
         s_mem, Multiplied{poly, x, ldp, ld, ppart, part, r, t.rows, ldp, PARTS == 2 ? 3 : 1}, m0, n0, 0, 1, wave, lane, acc);
 
   const float unscale = ldexpf(1.f, -l.poly_shift), rate = ldexpf(l.lr * t.rate, -XS);
   _Float16* to = (_Float16*)(l.work + t.x[l.from ^ 1]);
-  rows_out<T>(s_mem, wave, lane, acc, [&](int n, int m, float (&v)[8]) {
+  rows_out<S>(s_mem, wave, lane, acc, [&](int n, int m, float (&v)[8]) {
     n += n0, m += m0;
     if (n >= t.rows || m >= ld) return;
     const int64_t at = (int64_t)n * ld + m;
@@ -611,12 +610,20 @@ int64_t half_tiles(int64_t r, int64_t side) {
   const int64_t tiles = (r + side - 1) / side;
   return tiles * (tiles + 1) / 2;
 }
-int64_t all_tiles(int64_t rows, int64_t cols, int64_t side) { return ((rows + side - 1) / side) * ((cols + side - 1) / side); }
+// The update's tiles: 256 x 256, or 64 rows x 128 columns, of which three workgroups share a CU (one of 512 x 512 in two parts 231 us a
+// step, with tiles of 128 x 128 251; 1000 x 1000 391 and 431).
+enum Update { U256, U64 };
+int64_t update_tiles(Update u, int64_t rows, int64_t cols) {
+  const int64_t m = u == U256 ? 256 : 128, n = u == U256 ? 256 : 64;
+  return (rows + n - 1) / n * ((cols + m - 1) / m);
+}
 
 // The time of a launch of `jobs` tiles of `stages` of 64 k in us, by what launches of many shapes took: a stage of 256 x 256 takes
-// 1.25 us on an idle chip and 1.75 on a full one, of 128 x 128 0.62 alone on a CU and 1.15 for two.
+// 1.25 us on an idle chip and 1.75 on a full one, of 128 x 128 0.62 alone on a CU and 1.15 for two, of 128 x 64
+// 0.4 and 0.8 for three.
 double launch_us(int T, double jobs, double stages) {
   if (T == 256) return std::ceil(jobs / 256) * (stages * (1.25 + 0.5 * std::min(1.0, jobs / 256)) + 8);
+  if (T == 64) return std::ceil(jobs / 768) * (stages * (0.4 + 0.4 * std::min(1.0, jobs / 768)) + 5);
   if (jobs <= 256) return stages * (0.62 + 0.25 * jobs / 256) + 5;
   return std::ceil(jobs / 512) * (stages * 1.15 + 6);
 }
@@ -647,7 +654,7 @@ Tiling choose(const dn_muon_tensor* ts, int count, int products, bool square) {
 struct Group {
   MuonLaunch l;
   Tiling gram, square;
-  int update;  // tiles of the update
+  Update update;
   size_t total;
 };
 void plan_group(const dn_muon_tensor* ts, int count, int parts, Group& gr) {
@@ -655,16 +662,16 @@ void plan_group(const dn_muon_tensor* ts, int count, int parts, Group& gr) {
   Work w;
   const int products = parts == 2 ? 3 : 1;
   gr.gram = choose(ts, count, products, false), gr.square = choose(ts, count, products, true);
-  double us[2] = {};
-  for (int k = 0; k < 2; ++k) {
+  double least = 1e300;
+  for (const Update u : {U256, U64}) {
     double jobs = 0, stages = 0;
     for (int i = 0; i < count; ++i) {
-      jobs += (double)all_tiles(ts[i].rows, ts[i].cols, k ? 128 : 256);
+      jobs += (double)update_tiles(u, ts[i].rows, ts[i].cols);
       stages = std::max(stages, (double)((std::min(ts[i].rows, ts[i].cols) + BK - 1) / BK * products));
     }
-    us[k] = launch_us(k ? 128 : 256, jobs, stages);
+    const double us = launch_us(u == U256 ? 256 : 64, jobs, stages);
+    if (us < least) least = us, gr.update = u;
   }
-  gr.update = us[0] < us[1] ? 256 : 128;
   int32_t sums = 0;
   for (int i = 0; i < count; ++i) {
     Mat& t = gr.l.t[i];
@@ -714,10 +721,10 @@ int run_gram(MuonLaunch& l, const Tiling& k, hipStream_t st) {
   return (int)hipGetLastError();
 }
 template <int PARTS, bool LAST, typename P, typename O>
-int run_update(MuonLaunch& l, int T, hipStream_t st) {
-  const dim3 grid((unsigned)spread(l, [&](const Mat& t) { return all_tiles(t.rows, t.cols, T); }));
-  if (T == 256) update_kernel<PARTS, 256, LAST, P, O><<<grid, 512, 0, st>>>(l);
-  else update_kernel<PARTS, 128, LAST, P, O><<<grid, 256, 0, st>>>(l);
+int run_update(MuonLaunch& l, Update u, hipStream_t st) {
+  const dim3 grid((unsigned)spread(l, [&](const Mat& t) { return update_tiles(u, t.rows, t.cols); }));
+  if (u == U256) update_kernel<PARTS, 256, 256, LAST, P, O><<<grid, 512, 0, st>>>(l);
+  else update_kernel<PARTS, 128, 64, LAST, P, O><<<grid, 256, 0, st>>>(l);
   return (int)hipGetLastError();
 }
 
