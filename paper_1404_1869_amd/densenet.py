@@ -1141,7 +1141,8 @@ NS_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 def densenet_muon(plan: MuonPlan, lr, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5, coefficients=NS_COEFFICIENTS, eps=1e-7,
                   grad_scale=1.0):
     """One Muon step over a plan's matrices: p = p (1 - lr weight_decay) - lr rate X, X the update orthogonalised by `steps`
-    Newton-Schulz steps.  coefficients: (a, b, c) of all steps, or one such triple for each."""
+    Newton-Schulz steps.  coefficients: (a, b, c) of all steps, or one such triple for each; they have to keep the update's singular
+    values, at most 1 at first, below 4."""
     if not 1 <= steps <= DN_MAX_NS_STEPS:
         raise DenseNetError(DN_E_UNSUPPORTED, f"steps: 1 .. {DN_MAX_NS_STEPS}")
     each = [tuple(c) for c in coefficients] if hasattr(coefficients[0], "__len__") else [tuple(coefficients)] * steps

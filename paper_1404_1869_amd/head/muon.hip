@@ -4,8 +4,8 @@
 //   p = p (1 - lr weight_decay) - lr rate X
 // A, P and A^2 have the smaller side r of the matrix, and are symmetric: half their tiles are computed and mirrored.  A step is
 // 3 r^2 c + r^3 operations (c: the larger side), on the matrix cores, in one or two fp16 parts of every value:
-//   X, A are held times 2^13, P times a power of two that its coefficients allow, all of them below fp16's largest (the singular
-//   values of X are at most about 1.2 with the usual coefficients).  One part is 11 bits of a value down to 2^-27: the steps'
+//   X is held times 2^13, A and P times powers of two that the singular values of X and the coefficients allow (steps_of), all of
+//   them below fp16's largest (singular values are at most about 1.2 with the usual coefficients, and A times 2^13 too).  One part is 11 bits of a value down to 2^-27: the steps'
 //   roundings are of either sign and come to about 2^-11 of the update in all, below half a unit of a bf16 weight.  Two parts
 //   (fp32 and fp16 weights) are 22 bits, in three products of parts, as the loss's logits in fp32.
 // Bound by the matrix cores: six matrices of 2048 x 8192 in bf16 take 3.8 ms (0.86 PFLOP/s), one of 1000 x 9216 in two parts 0.81 ms
@@ -23,7 +23,7 @@ namespace dn {
 namespace head {
 namespace {
 
-constexpr int XS = 13;  // X and A are held times 2^XS
+constexpr int XS = 13;  // X is held times 2^XS, which singular values below 4 allow
 constexpr int SUMS = 1024;  // partial sums of a matrix's norm
 
 // A matrix in a launch, passed by value.
@@ -45,7 +45,7 @@ struct MuonLaunch {
   float* sums;
   float beta, grad_scale, eps, lr, decay;
   float a, b, c;  // of the step
-  int32_t poly_shift;  // P is held times 2^poly_shift
+  int32_t a_shift, poly_shift;  // A and P are held times 2^these
   int32_t nesterov, from;  // from: the buffer that X is in
 };
 
@@ -224,13 +224,13 @@ __device__ inline void load_parts(const _Float16* p, int64_t part, float (&v)[8]
     for (int j = 0; j < 8; ++j) v[j] += lo[j];
   }
 }
-// An entry of A (held times 2^XS) from X X', or (SQUARE) of P = b A + c A^2 from A's and A A's.
+// An entry of A from X X', or (SQUARE) of P = b A + c A^2 from A's and A A's.
 template <bool SQUARE>
 struct Entry {
   float fa, fs;
   __device__ inline Entry(const MuonLaunch& l) {
-    fa = SQUARE ? ldexpf(l.b, l.poly_shift - XS) : 0.f;
-    fs = SQUARE ? ldexpf(l.c, l.poly_shift - 2 * XS) : ldexpf(1.f, -XS);
+    fa = SQUARE ? ldexpf(l.b, l.poly_shift - l.a_shift) : 0.f;
+    fs = SQUARE ? ldexpf(l.c, l.poly_shift - 2 * l.a_shift) : ldexpf(1.f, l.a_shift - 2 * XS);
   }
   __device__ inline float operator()(float sum, float a) const { return SQUARE ? __builtin_fmaf(fa, a, fs * sum) : fs * sum; }
 };
@@ -415,7 +415,7 @@ struct SmallLaunch {
   float beta, grad_scale, eps, lr, decay;
   int32_t nesterov, steps;
   float coef[DN_MAX_NS_STEPS][3];
-  int32_t poly_shift[DN_MAX_NS_STEPS];
+  int32_t a_shift[DN_MAX_NS_STEPS], poly_shift[DN_MAX_NS_STEPS];
 };
 template <int PARTS, typename P, typename G, typename O>
 __global__ __launch_bounds__(64 * SMALL_WAVES) void small_kernel(SmallLaunch l) {
@@ -495,7 +495,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void small_kernel(SmallLaunch l) 
       f32x16 acc{};
       rows_product(X, lx, xpart, i0, j0, c32, acc);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) put(A + (i0 + 8 * (e / 4) + 4 * half + e % 4) * la + j0 + l32, apart, ldexpf(acc[e], -XS));
+      for (int e = 0; e < 16; ++e) put(A + (i0 + 8 * (e / 4) + 4 * half + e % 4) * la + j0 + l32, apart, ldexpf(acc[e], l.a_shift[s] - 2 * XS));
     }
     __syncthreads();
     // P = b A + c A A, over A once all waves have read it (16 waves: a tile each)
@@ -505,7 +505,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void small_kernel(SmallLaunch l) 
     if (is) rows_product(A, la, apart, i0, j0, r32, square);
     __syncthreads();
     if (is) {
-      const float fa = ldexpf(l.coef[s][1], l.poly_shift[s] - XS), fs = ldexpf(l.coef[s][2], l.poly_shift[s] - 2 * XS);
+      const float fa = ldexpf(l.coef[s][1], l.poly_shift[s] - l.a_shift[s]), fs = ldexpf(l.coef[s][2], l.poly_shift[s] - 2 * l.a_shift[s]);
       const auto place = [&](int e) { return A + (i0 + 8 * (e / 4) + 4 * half + e % 4) * la + j0 + l32; };
 #pragma unroll
       for (int e = 0; e < 16; ++e) square[e] = __builtin_fmaf(fa, get(place(e), apart), fs * square[e]);
@@ -599,10 +599,31 @@ struct Work {  // offsets in the workspace, 256-byte aligned
   }
 };
 
-int poly_shift_of(const double* c) {
-  // |P| <= |b| |A| + |c| |A|^2, which is at most 2.25 |c| + 1.5 |b| for singular values up to 1.22, and twice that to spare
-  const double most = 2 * (1.5 * std::fabs(c[1]) + 2.25 * std::fabs(c[2]));
-  return std::min(XS, (int)std::floor(std::log2(65504 / std::max(most, 1e-6))));
+// Powers of two that each step's A and P are held times, so that fp16 holds the largest that they can be.  X's singular values are at
+// most 1 before the first step, and after a step at most the largest |a s + b s^3 + c s^5| of those before it (and 4, by what
+// coefficients have to keep); |A| is at most the largest of them squared, and |P| the largest |b t + c t^2| up to there.  2 % are left
+// for roundings, and P has at least twice 1.5 |b| + 2.25 |c|, which is more than the usual coefficients need.
+struct StepShifts {
+  int32_t a, poly;
+};
+void steps_of(const dn_muon_params& k, StepShifts (&to)[DN_MAX_NS_STEPS]) {
+  const auto shift = [](double most) { return (int32_t)std::min<double>(XS, std::floor(std::log2(65504 / std::max(most, 1e-6)))); };
+  double top = 1;
+  for (int32_t i = 0; i < k.steps; ++i) {
+    const double a = k.coefficients[i][0], b = k.coefficients[i][1], c = k.coefficients[i][2], t = top * top;
+    const auto p = [&](double t) { return std::fabs(b * t + c * t * t); };
+    const auto x = [&](double t) { return std::sqrt(t) * std::fabs(a + b * t + c * t * t); };
+    double most_p = p(t), most_x = x(t);
+    const auto inside = [&](double at) { return at > 0 && at < t; };  // (false for NaN)
+    if (const double at = -b / (2 * c); inside(at)) most_p = std::max(most_p, p(at));
+    // where a + 3 b t + 5 c t^2, the derivative by the singular value, is 0
+    const double root = std::sqrt(9 * b * b - 20 * a * c);
+    for (const double at : {(-3 * b + root) / (10 * c), (-3 * b - root) / (10 * c), -a / (3 * b)})
+      if (inside(at)) most_x = std::max(most_x, x(at));
+    to[i].a = shift(1.02 * t);
+    to[i].poly = shift(std::max(1.02 * most_p, 2 * (1.5 * std::fabs(b) + 2.25 * std::fabs(c))));
+    top = std::min(4.0, 1.01 * most_x);
+  }
 }
 
 int parts_of(const dn_muon_params& k, dn_dtype p_dt) { return k.parts ? k.parts : p_dt == DN_BF16 ? 1 : 2; }
@@ -742,9 +763,11 @@ int run_group(Group& gr, const dn_muon_params& k, dn_dtype p_dt, dn_dtype g_dt, 
     start_kernel<decltype(g), PARTS><<<dim3((unsigned)n), 256, 0, st>>>(l);
     return (int)hipGetLastError();
   });
+  StepShifts shifts[DN_MAX_NS_STEPS];
+  steps_of(k, shifts);
   for (int s = 0; s < k.steps && !err; ++s) {
     l.a = (float)k.coefficients[s][0], l.b = (float)k.coefficients[s][1], l.c = (float)k.coefficients[s][2];
-    l.poly_shift = poly_shift_of(k.coefficients[s]);
+    l.a_shift = shifts[s].a, l.poly_shift = shifts[s].poly;
     l.from = s & 1;
     if ((err = run_gram<false, PARTS>(l, gr.gram, st)) || (err = run_gram<true, PARTS>(l, gr.square, st))) return err;
     err = s + 1 < k.steps ? run_update<PARTS, false, float, __bf16>(l, gr.update, st) : with_type(p_dt, [&](auto p) {
@@ -764,9 +787,11 @@ int run_small(const dn_muon_tensor* const* ts, int count, const dn_muon_params& 
   SmallLaunch l{};
   l.beta = (float)k.momentum, l.grad_scale = (float)k.grad_scale, l.eps = (float)k.eps, l.lr = (float)k.lr;
   l.decay = (float)(1 - k.lr * k.weight_decay), l.nesterov = k.nesterov, l.steps = k.steps;
+  StepShifts shifts[DN_MAX_NS_STEPS];
+  steps_of(k, shifts);
   for (int s = 0; s < k.steps; ++s) {
     for (int j = 0; j < 3; ++j) l.coef[s][j] = (float)k.coefficients[s][j];
-    l.poly_shift[s] = poly_shift_of(k.coefficients[s]);
+    l.a_shift[s] = shifts[s].a, l.poly_shift[s] = shifts[s].poly;
   }
   int64_t bytes = 0;
   for (int i = 0; i < count; ++i) {
