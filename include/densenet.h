@@ -433,8 +433,11 @@ int densenet_quantize_blocks(const void* d_x, int64_t x_stride, int64_t n, int32
  * every square (d_w_scale[ceil(V / 128)][ceil(C / 128)], rows 128).  A layer's forward pass takes w's codes; its gradients are
  * products too: dx from the codes of dy (rows 1) and w's turned ones (rows 128), dw [V][C] from dy's turned codes (rows 1) and x's
  * turned ones (rows 128).
- * A block's products are summed in 32 bits and multiplied by the product of its two scales (which has to be in fp32's range).
- * d_y [n][V]: `y_dtype`, any of DN_F32, DN_F16, DN_BF16.  d_workspace: NULL for a size query into *bytes_needed (which depends on
+ * A block's sum is multiplied by the product of its two scales (which has to be in fp32's range), and blocks are added in 32 bits.
+ * d_y [n][V]: `y_dtype`, any of DN_F32, DN_F16, DN_BF16.  For DN_F32 all of a block is summed in 32 bits too, at half the rate.  For
+ * results in 16 bits the products of each eight codes (8 j .. 8 j + 7 of a row) are added with those of their bits only that are
+ * worth 2^-13 of the largest one's leading bit or more: each such sum is off by up to 7 times 2^-13 of its largest product (where
+ * products cancel, 448 448 - 448 448 + 1 = 0), and sums of eight are added in 32 bits.  d_workspace: NULL for a size query into *bytes_needed (which depends on
  * the codes' alignment and strides: pass the same).  Codes whose rows start on 16 bytes are read as they lie, others are copied to
  * such rows first.  Limits (DN_E_TOO_LARGE): C <= 2^20; n, V <= 2^31 - 256; n V in tiles of 128 x 128 below 2^24. */
 int densenet_block_product(const void* d_a, int64_t a_stride, const float* d_a_scale, const void* d_w,

@@ -972,7 +972,8 @@ def densenet_quantize_blocks(x, rows=1, codes=True, turned=False, out=None, scal
 def densenet_block_product(a, a_scale, w, w_scale, out_dtype=DN_BF16, out=None):
     """y [n][V] = a w^T of e4m3 codes a [n][C] and w [V][C]: a_scale [n][ceil(C / 128)], a scale for every 128 values of a row;
     w_scale [ceil(V / 128)][ceil(C / 128)], one for every square of 128 x 128 (densenet_quantize_blocks with rows 1 and 128).
-    out_dtype: DN_F32, DN_F16 or DN_BF16."""
+    out_dtype: DN_F32, summed in 32 bits all through, or DN_F16 or DN_BF16: of each eight products bits below 2^-13 of the largest
+    one are left out, so that a sum of eight is off by up to 7 times that."""
     torch = _torch()
     f8 = torch.float8_e4m3fn
     ap, as_ = _rows(a, "a", None, f8)

@@ -1,5 +1,7 @@
-"""Muon's steps over all the coefficients that it takes: singular values of X up to 4, where A and P reach 16 and more.  Against the
-64-bit form, with the bound that its roundings grow to (half a unit of 11 or 22 bits for each value held)."""
+"""What the 8-bit head's operators hold of their sums and states, at the ends of the ranges that they take.
+
+Products: of codes far apart in size.  Muon: singular values of X up to 4, where A and P reach 16 and more, against the 64-bit form,
+with the bound that its roundings grow to (half a unit of 11 or 22 bits for each value held)."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -14,6 +16,44 @@ def D():
     assert torch.cuda.is_available()
     densenet.lib()
     return densenet
+
+
+def codes(D, x):
+    """Values that e4m3 holds, as codes in rows that start on 16 bytes."""
+    q = D._codes(x.shape, x.device)
+    q.copy_(x.to(torch.float8_e4m3fn))
+    assert torch.equal(q.float(), x)
+    return q
+
+
+@pytest.mark.parametrize("n", [1, 40, 300, 3000])
+@pytest.mark.parametrize("yt", ["f32", "f16", "bf16"])
+def test_products_of_codes_that_cancel(D, n, yt):
+    """448 448 - 448 448 + 1: in 32 bits 1; of three of one eight, results in 16 bits may be off by 7 times 2^-13 of 448 448; of three
+    different eights, or where no product is below 2^-12 of the largest, they are exact."""
+    V, C, dev = 3001 if n == 3000 else 130, 300, "cuda"
+    g = gen(n)
+    one = lambda m: torch.ones(m, -(-C // 128), device=dev)  # noqa: E731
+    wk = one(-(-V // 128))
+    run = lambda a, w: D.densenet_block_product(codes(D, a), one(n), codes(D, w), wk, out_dtype=D.DTYPES[yt])  # noqa: E731
+    a, w = torch.zeros(n, C, device=dev), torch.zeros(V, C, device=dev)
+    a[:, 136:139] = torch.tensor([448.0, 448.0, 1.0])
+    w[:, 136:139] = torch.tensor([448.0, -448.0, 1.0])
+    y = run(a, w).float()
+    assert float((y - 1).abs().max()) <= (0 if yt == "f32" else 7 * 2.0 ** -13 * 448 * 448)
+    # each row's three in eights of its own: w has 448 in even ones, -448 in odd ones of the first 64 codes, 1 in the eights of the next
+    a, w = torch.zeros(n, C, device=dev), torch.zeros(V, C, device=dev)
+    w[:, :64] = torch.where(torch.arange(64, device=dev) // 8 % 2 == 0, 448.0, -448.0)
+    w[:, 64:128] = 1.0
+    r = torch.arange(n, device=dev)
+    for first in (0, 8):
+        a[r, torch.randint(0, 4, (n,), generator=g, device=dev) * 16 + first + torch.randint(0, 8, (n,), generator=g, device=dev)] = 448.0
+    a[r, 64 + torch.randint(0, 64, (n,), generator=g, device=dev)] = 1.0
+    assert bool((run(a, w) == 1).all())
+    # products of 1, 2^-6 and 2^-12: sums of 300 of them are whole numbers of 2^-12 below 2^9, and rounded once
+    pick = lambda m: torch.where(torch.rand(m, C, generator=g, device=dev) < 0.5, 1.0, 2.0 ** -6) * (torch.randint(0, 3, (m, C), generator=g, device=dev) - 1)  # noqa: E731,E501
+    a, w = pick(n), pick(V)
+    assert torch.equal(run(a, w), (a.double() @ w.double().T).to(DT[yt]))
 
 
 def plain(u, coefs, unit):
