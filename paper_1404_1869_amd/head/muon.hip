@@ -37,7 +37,7 @@ struct Mat {
   int32_t norm;
   float rate;
 };
-constexpr int MATS = 32;  // 96 bytes each
+constexpr int MATS = 32;
 struct MuonLaunch {
   Mat t[MATS];
   int32_t count;
@@ -48,6 +48,8 @@ struct MuonLaunch {
   int32_t a_shift, poly_shift;  // A and P are held times 2^these
   int32_t nesterov, from;  // from: the buffer that X is in
 };
+constexpr size_t MAX_ARGUMENTS = 4096;  // bytes of a launch
+static_assert(sizeof(MuonLaunch) <= MAX_ARGUMENTS, "the matrices of a launch are its arguments");
 
 __host__ __device__ inline int32_t up8(int32_t x) { return (x + 7) / 8 * 8; }
 __device__ inline const Mat& mat_of(const MuonLaunch& l, int block) {
@@ -417,6 +419,7 @@ struct SmallLaunch {
   float coef[DN_MAX_NS_STEPS][3];
   int32_t a_shift[DN_MAX_NS_STEPS], poly_shift[DN_MAX_NS_STEPS];
 };
+static_assert(sizeof(SmallLaunch) <= MAX_ARGUMENTS, "the matrices of a launch are its arguments");
 template <int PARTS, typename P, typename G, typename O>
 __global__ __launch_bounds__(64 * SMALL_WAVES) void small_kernel(SmallLaunch l) {
   extern __shared__ __align__(16) char s_mem[];
