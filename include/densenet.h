@@ -477,7 +477,7 @@ int densenet_token_scores_backward(const void* d_logits, int64_t stride, const i
  *   p = p (1 - lr weight_decay) - lr rate X
  * p, g: contiguous [rows][cols] of p_dtype and g_dtype; copy (or NULL): the new p in copy_dtype (DN_F16 or DN_BF16); m: fp32
  * [rows][cols], or NULL with momentum 0.  No two tensors of a call may meet in memory.  |u| is taken in fp32: squares have to be in
- * its range.  eps: 1e-30 at least.
+ * its range.  eps: 1e-30 at least.  Parameters, rates, lr rate and lr weight_decay have to be finite in fp32.
  * steps: 1 .. DN_MAX_NS_STEPS; step s takes coefficients[s] = (a, b, c), each in [-64, 64], which have to keep the singular values of
  * X (at most 1 before the first step) below 4, as the usual ones (3.4445, -4.775, 2.0315) do.
  * parts: fp16 parts of a value in the products, 1 (11 bits) or 2 (22 bits); 0: 1 for DN_BF16 weights, 2 for others.

@@ -369,8 +369,10 @@ int densenet_muon(const dn_muon_tensor* tensors, int32_t count, dn_dtype p_dtype
     if (!(k.momentum >= 0 && k.momentum < 1)) return fail(DN_E_INVALID_ARG, "momentum must be in [0, 1)");
     // (2^13 / eps, which an update of zeros is multiplied by, has to be finite)
     if (!(k.eps >= 1e-30) || !std::isfinite((float)k.eps)) return fail(DN_E_INVALID_ARG, "eps must be 1e-30 or more, and finite in fp32");
-    if (!std::isfinite(k.lr) || !std::isfinite(k.weight_decay) || !std::isfinite(k.grad_scale))
-      return fail(DN_E_INVALID_ARG, "parameters must be finite");
+    // (in fp32, which the step is computed in)
+    const auto finite = [](double v) { return std::isfinite((float)v); };
+    if (!finite(k.lr) || !finite(k.weight_decay) || !finite(k.grad_scale) || !finite(1 - k.lr * k.weight_decay))
+      return fail(DN_E_INVALID_ARG, "parameters must be finite in fp32");
     for (int32_t s = 0; s < k.steps; ++s) {
       const double* c = k.coefficients[s];
       if (!(std::fabs(c[0]) <= 64) || !(std::fabs(c[1]) <= 64) || !(std::fabs(c[2]) <= 64))
@@ -383,7 +385,7 @@ int densenet_muon(const dn_muon_tensor* tensors, int32_t count, dn_dtype p_dtype
       // (256 rows of the larger side in fp16 are within the 31 bits of a buffer's offsets)
       if (t.rows > (1 << 21) || t.cols > (1 << 21) || std::min(t.rows, t.cols) > (1 << 15))
         return fail(DN_E_TOO_LARGE, "a matrix's rows or cols");
-      if (!std::isfinite(t.rate)) return fail(DN_E_INVALID_ARG, "a matrix's rate must be finite");
+      if (!finite(t.rate) || !finite(k.lr * t.rate)) return fail(DN_E_INVALID_ARG, "a matrix's rate, and lr times it, must be finite in fp32");
       // (more workgroups than any launch has for it: pieces of 2048 values, and twice the tiles of 64 x 64 of its smaller side)
       tiles += (t.rows * t.cols + 2047) / 2048 + ((std::min(t.rows, t.cols) + 63) / 64) * ((std::min(t.rows, t.cols) + 127) / 64) + 16384;
     }

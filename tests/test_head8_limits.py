@@ -39,3 +39,12 @@ def test_matrices_past_a_launch_share_its_workspace():
     assert muon_bytes((2000, 3000), *[small] * 100, *[wide, tall] * 32) == first  # or the first, with 31 others
     same = muon_bytes(*[wide] * 32)
     assert muon(rows=130, cols=140, count=33, size=same - 1) == D.DN_E_BUFFER_TOO_SMALL
+
+
+@pytest.mark.parametrize("kw", [dict(lr=1e39), dict(grad_scale=-1e39), dict(rate=1e39), dict(lr=1e30, weight_decay=1e30), dict(lr=1e30, rate=1e30),
+                                dict(lr=1e-30, rate=-1e300)])
+def test_muon_refuses_what_fp32_does_not_hold(kw):
+    """Parameters that are finite, and infinite where the step is computed: the weights would be NaN."""
+    need = ctypes.c_size_t()
+    assert muon(work=None, need=ctypes.byref(need)) == D.DN_OK
+    assert muon(work=None, need=ctypes.byref(need), **kw) == D.DN_E_INVALID_ARG and D.last_error()
