@@ -445,7 +445,7 @@ int densenet_block_product(const void* d_a, int64_t a_stride, const float* d_a_s
                            void* d_y, int64_t y_stride, dn_dtype y_dtype, void* d_workspace,
                            size_t workspace_bytes, size_t* bytes_needed, void* stream);
 
-/* Scores of rows of logits l [n][V] (`dtype`): with x = scale l (scale > 0, the inverse temperature),
+/* Scores of rows of logits l [n][V] (`dtype`): with x = scale l (0 < scale <= 2^127, the inverse temperature),
  *   lse = log sum_v exp x_v;  logp = x_token - lse;  entropy = -sum_v p_v log p_v, p = exp(x - lse);
  *   the `top` (0 .. DN_MAX_TOP) largest logits, of equal ones the lower index first: their indices and log probabilities.
  * d_token: int64 [n], or NULL; of a row whose token lies outside [0, V), logp is 0.  d_logp, d_entropy (NULL: not wanted), d_lse:

@@ -71,7 +71,8 @@ int check_scores(const void* logits, int64_t stride, const int64_t* token, int64
   if (!valid_dtype(dtype)) return fail(DN_E_UNSUPPORTED, "unknown dtype");
   if (n < 0 || V <= 0) return fail(DN_E_INVALID_ARG, "n must be >= 0 and V positive");
   if (n > MAX_ROWS || V >= MAX_ROWS) return fail(DN_E_TOO_LARGE, "n or V");
-  if (!(scale > 0) || std::isinf(scale)) return fail(DN_E_INVALID_ARG, "scale must be positive and finite");
+  // (times log2 e, which the exponentials take, it has to be finite too)
+  if (!(scale > 0) || scale > 0x1p127f) return fail(DN_E_INVALID_ARG, "scale must be positive and at most 2^127");
   if (top < 0 || top > DN_MAX_TOP) return fail(DN_E_UNSUPPORTED, "top must be 0 .. DN_MAX_TOP");
   if ((uintptr_t)token % 8) return fail(DN_E_INVALID_ARG, "tokens: not aligned");
   return check_rows("logits", logits, stride, n, V, dtype_size(dtype));
