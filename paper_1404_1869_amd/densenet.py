@@ -825,8 +825,9 @@ def densenet_softmax_loss_backward(h, w, labels, lse, dloss=None, scale=1.0, dh=
 
 class AdamWPlan:
     """Tensors that step together: parameters (one type, updated in place), their gradients' buffers (one type), 16-bit
-    copies of the parameters (optional; None entries allowed), and the optimiser's states.  state_bits: 32, or 8 (DN_F8
-    codes with a scale per 256 values); states are made as zeros, or given (m, v, and m_scale, v_scale in 8 bits): tensor
+    copies of the parameters (optional; None entries allowed, and so is a parameter that is its own copy, as
+    `p.to(torch.bfloat16)` gives of a bf16 one: nothing else is written for it; copies in fp32 are refused here), and the
+    optimiser's states.  state_bits: 32, or 8 (DN_F8 codes with a scale per 256 values); states are made as zeros, or given (m, v, and m_scale, v_scale in 8 bits): tensor
     i's start at value ADAMW_BLOCK * blocks[i]."""
 
     def __init__(self, params, grads, m=None, v=None, m_scale=None, v_scale=None, copies=None, state_bits=None):
