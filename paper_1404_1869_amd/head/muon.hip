@@ -8,8 +8,8 @@
 //   them below fp16's largest (singular values are at most about 1.2 with the usual coefficients, and A times 2^13 too).  One part is 11 bits of a value down to 2^-27: the steps'
 //   roundings are of either sign and come to about 2^-11 of the update in all, below half a unit of a bf16 weight.  Two parts
 //   (fp32 and fp16 weights) are 22 bits, in three products of parts, as the loss's logits in fp32.
-// Bound by the matrix cores: six matrices of 2048 x 8192 in bf16 take 3.8 ms (0.86 PFLOP/s), one of 1000 x 9216 in two parts 0.81 ms
-// (0.53: its 144 tiles leave CUs idle), four of 512 x 512 278 us in two parts and 164 in one, which are launches more than work.
+// Bound by the matrix cores: six matrices of 2048 x 8192 in bf16 take 3.7 to 4.2 ms by machine and clock (0.89 to 0.79 PFLOP/s), one of
+// 1000 x 9216 in two parts 0.75 to 0.83 ms (0.57 to 0.52: its 144 tiles leave CUs idle), four of 512 x 512 278 us in two parts and 164 in one, which are launches more than work.
 // All matrices of a call go through the same launches.  Sums over k go to slabs in fp32, one for each split, and a launch adds
 // them in order, so results do not depend on what ran first.
 #include <hip/hip_runtime.h>

@@ -3,7 +3,7 @@
 //   gradient: with A = dlse - dlogp - sum dtop - dH H,  dl_v = scale (p_v (A - dH log p_v) + dlogp [v = token] + dtop_j [v = id_j])
 // A row is read once (the gradient: read once and written once).  The gradient is bound by memory (4096 x 32000 in bf16 92 us, 333 x
 // 50257 in fp32 with 8 alternatives 27), the scores by the vector unit (2000 x 50257 in fp16 45 us, with 5 alternatives 57), and one
-// row by the chain of its two launches (131072 logits with 20 alternatives 19 us).  Every lane keeps its own maximum m, sum S of
+// row by the chain of its two launches (131072 logits with 20 alternatives 19 to 21 us).  Every lane keeps its own maximum m, sum S of
 // exp(x - m) and T of exp(x - m) (x - m) and rescales them where the maximum grows; lanes, waves and workgroups join theirs at
 // the end, in a fixed order.  H = log S - T / S, and a logit's part is taken as (x - m), so large logits lose no digits.
 // Alternatives: a wave keeps candidates above a bound that `top` values of the row are known to reach.  The top-th largest of the
@@ -422,8 +422,8 @@ bool wave_each(int64_t n, int32_t V) { return V <= SHORT || n >= MANY; }
 }  // namespace
 
 // Workgroups of a row: enough of them for the chip where there are few rows, of at least two blocks a wave.  The launch that joins
-// them costs 3 us, so only long rows are split: with 20 alternatives 8 x 50257 takes 20 us, in one workgroup 30 (400 rows 31 and 35,
-// 700 rows 48 and 38), and 8 x 16384 20 and 17; without alternatives 8 x 131072 takes 16 us either way.
+// them costs 3 us, so only long rows are split.  In parts and in one workgroup: with 20 alternatives 8 x 50257 takes 20 and 30 us, 400
+// x 50257 31 and 35, 700 x 50257 48 and 38, 8 x 16384 20 and 17; without alternatives 8 x 50257 16 and 12, 8 x 131072 16 and 16.
 int32_t scores_parts(int64_t n, int32_t V, int32_t top) {
   if (V <= (top ? 1 << 15 : 1 << 17) || n >= 512 || n == 0) return 1;
   return (int32_t)std::min<int64_t>({(1024 + n - 1) / n, V / (8 * WAVE_BLOCK), 64});
