@@ -2,6 +2,8 @@
 
 Products: of codes far apart in size.  Muon: singular values of X up to 4, where A and P reach 16 and more, against the 64-bit form,
 with the bound that its roundings grow to (half a unit of 11 or 22 bits for each value held)."""
+import math
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -107,3 +109,71 @@ def test_muon_of_singular_values_up_to_4(D, coefs, pt):
         want = -want
         assert float(torch.linalg.matrix_norm(want, 2)) < 4
         within(q, want, err + (UNIT[pt] + 4 * E24) * (want.abs() + err), f"{tuple(q.shape)}")
+
+
+def test_scores_of_the_longest_row(D):
+    """2^31 - 257 logits, the most that a row may have: six above the rest, at the end and past 2^30 too, equal ones by place."""
+    V = (1 << 31) - 257
+    at = {5: 3.0, V - 1: 4.0, V - 2: 4.0, 1 << 30: 2.0, (1 << 30) + 1: 2.0, V - 300: 1.0}
+    x = torch.full((1, V), -20.0, dtype=torch.bfloat16, device="cuda")
+    for place, value in at.items():
+        x[0, place] = value
+    token = torch.tensor([V - 1], device="cuda")
+    logp, H, lse, ids, best = D.densenet_token_scores(x, token, top=8)
+    assert ids.tolist() == [[V - 2, V - 1, 5, 1 << 30, (1 << 30) + 1, V - 300, 0, 1]]
+    z = (V - 6) * math.exp(-20) + sum(math.exp(v) for v in at.values())
+    want = math.log(z)
+    # equal logits count in whole numbers, below 2^24 in a lane; the exponents (at most 24) of 24 joins are off by 3 roundings each
+    # where they have weight: d1, the mean distance to the maximum
+    d1 = ((V - 6) * math.exp(-20) * 24 + sum(math.exp(v) * (4 - v) for v in at.values())) / z
+    off = E24 * (4 * d1 + 64)
+    assert abs(float(lse) - want) <= off + 4 * E24 * want and abs(float(logp) - (4 - want)) <= off + 4 * E24 * want
+    for got, place in zip(best[0].tolist(), ids[0].tolist()):
+        assert abs(got - (at.get(place, -20.0) - want)) <= off + 4 * E24 * 26
+    dx = D.densenet_token_scores_backward(x, token, lse, dlogp=torch.ones(1, device="cuda"), out=x)  # in the logits' own memory
+    for place, value in [*at.items(), (0, -20.0), (V - 301, -20.0), (V // 2 + 99, -20.0)]:
+        p = math.exp(value - want)
+        g = (place == V - 1) - p
+        # p is off by what lse is, and by two roundings of an exponent of at most 26 and of the exponential; bf16 rounds once
+        assert abs(float(dx[0, place]) - g) <= UNIT["bf16"] * abs(g) * 1.01 + p * (off + E24 * (4 * 26 + 4)), place
+    del x, dx
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("tall", [True, False])
+def test_muon_past_32_bits(D, tall):
+    """A matrix of 65537 x 32768 (2^31 values and more, the smaller side the largest that there may be) whose update is 0 but for 6 x 5
+    places spread to its ends: there the step is that of the 6 x 5 matrix, and elsewhere weights stay 0."""
+    r, c = torch.tensor([0, 300, 32768, 50001, 65535, 65536], device="cuda"), torch.tensor([0, 1, 20000, 32766, 32767], device="cuda")
+    u = torch.randn(6, 5, generator=gen(31), device="cuda").bfloat16()
+    shape = (65537, 32768)
+    if not tall:
+        r, c, u, shape = c, r, u.T, shape[::-1]
+    g = torch.zeros(shape, dtype=torch.bfloat16, device="cuda")
+    g[r[:, None], c] = u
+    p = torch.zeros(shape, dtype=torch.bfloat16, device="cuda")
+    D.densenet_muon(D.MuonPlan([p], [g], rates=[1.0]), lr=-1.0, momentum=0.0, steps=3)
+    want, err = plain(u, [(3.4445, -4.775, 2.0315)] * 3, 2.0 ** -11)
+    within(p[r[:, None], c], want, err + UNIT["bf16"] * (want.abs() + err), "p")
+    p[r[:, None], c] = 0
+    assert not any(bool(t.any()) for t in p.split(4096))
+    del g, p
+    torch.cuda.empty_cache()
+
+
+def test_quantize_more_rows_than_a_launch_holds(D):
+    """2^28 rows of one value and a few (a launch has 2^24 workgroups of 16 rows): codes and scales repeat with the rows."""
+    n, period = (1 << 28) + 77, 1009
+    base = torch.randn(period, 1, generator=gen(32), device="cuda").bfloat16()
+    x = base.repeat(-(-n // period), 1)[:n]
+    out = torch.empty(n, 1, dtype=torch.float8_e4m3fn, device="cuda")
+    q, k, _, _ = D.densenet_quantize_blocks(x, out=out)
+    want, wk, _, _ = D.densenet_quantize_blocks(base)
+    last = (1 << 28) // period * period  # the last period, cut short, has row 2^28 among its first
+    for first in (0, last - period, last - 5 * period):
+        part = slice(first, first + period)
+        assert torch.equal(q[part].view(torch.uint8), want.contiguous().view(torch.uint8)) and torch.equal(k[part], wk)
+    rest = n - last
+    assert rest > 77 and torch.equal(q[last:].view(torch.uint8), want[:rest].contiguous().view(torch.uint8)) and torch.equal(k[last:], wk[:rest])
+    del x, out, q, k
+    torch.cuda.empty_cache()
